@@ -330,6 +330,108 @@ samkv_status_t samkv_align(samkv_handle_t h, const samkv_shape_t* shape, const i
                            int32_t R, uint8_t* flags_out, int32_t* merged_ids, int32_t* merged_len, int32_t* run_ids,
                            int32_t run_capacity, int32_t* run_len, void* stream);
 
+/* ---- packed sequences and the paged cache ------------------------------------------------------------ */
+
+/* The calls below serve what lies around the sparsified cache: the prefill that produces the documents' caches in the
+ * first place (every document on its own, Sec. 2: "precomputed independently"), and conversations that go on in a
+ * cache of pages.  They take sequences of different lengths packed behind one another and have no context table.
+ *
+ * Sequence s owns the rows seq_offsets[s] .. seq_offsets[s+1]-1 of every packed tensor (row = token).  Sequences may be
+ * empty.  Rows of outputs behind the last sequence are left as they were; input rows there are not used.
+ * Offsets and lengths are DEVICE data (a captured call may be replayed with others); the kernels clamp what they read to
+ * the bounds below and record a device check (samkv_poll_status) where a value had to be clamped. */
+#define SAMKV_MAX_SEQ 65536
+
+typedef struct {
+  int32_t n_q_heads, n_kv_heads, head_dim, dtype;  /* as in samkv_shape_t; n_q_heads / n_kv_heads <= 32 */
+  int32_t n_seq;               /* sequences, 1 .. SAMKV_MAX_SEQ */
+  int32_t n_tokens;            /* rows of the packed tensors (0: the call does nothing) */
+  int32_t max_seq_tokens;      /* expected longest sequence of the call, 0 = unknown; chooses the kernel, never the result */
+  const int32_t* seq_offsets;  /* device [n_seq+1], ascending from >= 0 to <= n_tokens */
+} samkv_packed_t;
+
+/* A packed tensor [n_tokens, heads, head_dim]: element (t, h, e) at data[t * token_stride + h * head_stride + e].
+ * Strides in elements, multiples of 16 bytes and >= head_dim (ignored along an axis of extent 1); data 16-byte aligned.
+ * Slices of one fused projection matrix and the library's own [heads, tokens, head_dim] slabs both fit.  Rows of an
+ * output must not overlap one another (SAMKV_ERR_INVALID_ARG). */
+typedef struct {
+  void* data;
+  int64_t token_stride, head_stride;
+} samkv_rows_t;
+
+/* A cache of pages: slot i of sequence s lives in page block_table[s * table_width + i / page_size], at row
+ * i % page_size.  Table entries of pages that no visible or appended slot needs are not used (any value).  A needed
+ * entry outside [0, n_pages) is recorded as a device check: an append skips the slot, attention reads page 0 instead
+ * (that sequence's output is then meaningless). */
+typedef struct {
+  void *K, *V;                 /* [n_pages, n_kv_heads, page_size, head_dim] each, contiguous, 16-byte aligned */
+  const int32_t* block_table;  /* device [n_seq, table_width] */
+  int32_t page_size;           /* 16, 32, 64, 128 or 256 slots */
+  int32_t n_pages, table_width; /* table_width * page_size <= 2^30; n_pages * n_kv_heads * page_size < 2^31 */
+} samkv_pages_t;
+
+/* Rotary position encoding of the first rot_dim elements of a row: pair i is (i, i + rot_dim/2), or (2i, 2i+1) when
+ * interleaved; (a, b) -> (a cos - b sin, b cos + a sin), angle = position * base^(-2i/rot_dim), or position *
+ * inv_freq[i] when inv_freq is given (host double [rot_dim/2], finite, read during the call).  Angles are reduced
+ * exactly (64-bit fixed point), so positions may be as large as int32 allows, or negative. */
+typedef struct {
+  int32_t rot_dim;             /* multiple of 16, 16 .. head_dim */
+  int32_t interleaved;
+  double base;                 /* > 0; ignored when inv_freq is given */
+  const double* inv_freq;
+} samkv_rope_t;
+
+/* Bytes of workspace that samkv_prefill and samkv_paged_attn need in the handle they are called with (partial results
+ * of key ranges that are split between CTAs; does not depend on the lengths).  0 on a bad description.  Such a handle is
+ * made by samkv_create like any other; one workspace of the larger size serves both kinds of calls.  A captured graph
+ * keeps using the workspace of the handle it was captured with: graphs that share a handle must not run at the same
+ * time. */
+size_t samkv_packed_workspace_bytes(const samkv_packed_t* packed);
+
+/* Causal attention of whole prompts over themselves, e.g. of the documents whose caches the calls above take:
+ *   O[t, hq] = sum_{j <= t, same sequence} softmax(scale * <Q[t, hq], K[j, hq/G]>) V[j, hq/G]
+ *   Q, O   packed with n_q_heads; K, V packed with n_kv_heads.  O must not overlap the inputs.
+ *   scale  <= 0 selects 1/sqrt(d)
+ *   lse    fp32 [n_tokens, n_q_heads] optional: log of the softmax denominator
+ * K and V may be the [n_kv_heads, L_tot, d] slabs of one request that samkv_score and samkv_compact read later.
+ * Values of K and V behind a row's own position never reach that row, infinities and NaN included.
+ * Precision as for samkv_attn.  SAMKV_ERR_WORKSPACE if the handle's workspace is too small. */
+samkv_status_t samkv_prefill(samkv_handle_t h, const samkv_packed_t* packed, const samkv_rows_t* Q,
+                             const samkv_rows_t* K, const samkv_rows_t* V, float scale, const samkv_rows_t* O,
+                             float* lse, void* stream);
+
+/* Position rotation and cache append in one pass over the new rows.  Token t of sequence s (t counted from the
+ * sequence's first row) is written to slot cache_len[s] + t of its pages and rotated by its position:
+ *   K, V        packed with n_kv_heads: the projections' output (K not rotated yet)
+ *   rope        NULL: no rotation
+ *   positions   int32 [n_tokens] device, NULL: position = cache_len[s] + t
+ *   pages       destination pages, NULL: none.  V goes there unchanged, K rotated
+ *   cache_len   int32 [n_seq] device, NULL: 0 for every sequence.  Not changed: every layer of a step appends with the
+ *               same lengths, the caller advances them afterwards
+ *   K_out,V_out packed destinations next to, or instead of, the pages (both or neither, NULL: none); e.g. the slabs
+ *               samkv_prefill and samkv_score read
+ *   Q, Q_out    optional (both or neither): Q rows, rotated by the same positions
+ * Q_out, K_out, V_out may be the very same rows as Q, K, V; otherwise outputs must not overlap inputs.
+ * A slot at or behind table_width * page_size, or one whose page is invalid, is skipped and recorded as a device check.
+ * Rotation in fp32, one rounding to dtype; rows that are not rotated are copied bit-exactly.  No workspace. */
+samkv_status_t samkv_append(samkv_handle_t h, const samkv_packed_t* packed, const samkv_rows_t* K,
+                            const samkv_rows_t* V, const samkv_pages_t* pages, const int32_t* cache_len,
+                            const samkv_rope_t* rope, const int32_t* positions, const samkv_rows_t* Q,
+                            const samkv_rows_t* Q_out, const samkv_rows_t* K_out, const samkv_rows_t* V_out,
+                            void* stream);
+
+/* Attention of new tokens over a paged cache: decode steps (one token per sequence), chunks, or both mixed.
+ *   cache_len  int32 [n_seq] device: slots in the cache before this step, as given to samkv_append
+ *   causal     != 0: the new tokens' own rows have been appended; token t sees slots < cache_len[s] + t + 1
+ *              == 0: every token sees the slots < cache_len[s] (a row that sees none: O = 0, lse = -inf)
+ *   Q, O       packed with n_q_heads; O must not overlap Q
+ *   scale, lse as for samkv_prefill
+ * Slots that no token sees are never used, whatever they hold.  A sequence whose slots would pass table_width *
+ * page_size is cut off there and recorded as a device check. */
+samkv_status_t samkv_paged_attn(samkv_handle_t h, const samkv_packed_t* packed, const samkv_pages_t* pages,
+                                const int32_t* cache_len, const samkv_rows_t* Q, float scale, int32_t causal,
+                                const samkv_rows_t* O, float* lse, void* stream);
+
 /* ---- scoring without any allocation ------------------------------------------------------ */
 
 /* (No counterpart in the paper: this entry point exists for deployment reasons only.)

@@ -28,7 +28,7 @@ EXPORTS = ["samkv_workspace_bytes", "samkv_create", "samkv_destroy", "samkv_poll
            "samkv_attn", "samkv_score_static", "samkv_topp", "samkv_topp_plan", "samkv_select_cross",
            "samkv_select_cross_scratch_bytes", "samkv_compact_units", "samkv_align", "samkv_compact_protected",
            "samkv_block_means", "samkv_score_blocks", "samkv_attn_kernel_count", "samkv_attn_share_sm", "samkv_attn_layers", "samkv_select_compact",
-           "samkv_sparsify"]
+           "samkv_sparsify", "samkv_packed_workspace_bytes", "samkv_prefill", "samkv_append", "samkv_paged_attn"]
 
 
 class SamkvError(RuntimeError):
@@ -43,6 +43,26 @@ class samkv_shape_t(ctypes.Structure):
                 ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("n_ctx", ctypes.c_int32),
                 ("ctx_offsets", ctypes.POINTER(ctypes.c_int32)), ("block_size", ctypes.c_int32),
                 ("n_init", ctypes.c_int32), ("n_local", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class samkv_packed_t(ctypes.Structure):
+    _fields_ = [("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("n_seq", ctypes.c_int32), ("n_tokens", ctypes.c_int32),
+                ("max_seq_tokens", ctypes.c_int32), ("seq_offsets", ctypes.c_void_p)]
+
+
+class samkv_rows_t(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class samkv_pages_t(ctypes.Structure):
+    _fields_ = [("K", ctypes.c_void_p), ("V", ctypes.c_void_p), ("block_table", ctypes.c_void_p),
+                ("page_size", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("table_width", ctypes.c_int32)]
+
+
+class samkv_rope_t(ctypes.Structure):
+    _fields_ = [("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("base", ctypes.c_double),
+                ("inv_freq", ctypes.POINTER(ctypes.c_double))]
 
 
 def lib() -> ctypes.CDLL:
@@ -102,8 +122,15 @@ def load_library(path: str) -> ctypes.CDLL:
     L.samkv_block_means.argtypes = [vp, shp, vp, vp, vp]
     L.samkv_score_blocks.argtypes = L.samkv_score.argtypes
     L.samkv_compact_units.argtypes = [vp, shp, vp, vp, vp, i32, vp, vp, i32, vp, vp, vp]
+    rows, packed, pages = (ctypes.POINTER(t) for t in (samkv_rows_t, samkv_packed_t, samkv_pages_t))
+    L.samkv_packed_workspace_bytes.argtypes = [packed]
+    L.samkv_packed_workspace_bytes.restype = sz
+    L.samkv_prefill.argtypes = [vp, packed, rows, rows, rows, f32, rows, vp, vp]
+    L.samkv_append.argtypes = [vp, packed, rows, rows, pages, vp, ctypes.POINTER(samkv_rope_t), vp, rows, rows, rows, rows, vp]
+    L.samkv_paged_attn.argtypes = [vp, packed, pages, vp, rows, f32, i32, rows, vp, vp]
     for name in EXPORTS:
-        if name not in ("samkv_status_string", "samkv_workspace_bytes", "samkv_select_cross_scratch_bytes"):
+        if name not in ("samkv_status_string", "samkv_workspace_bytes", "samkv_select_cross_scratch_bytes",
+                        "samkv_packed_workspace_bytes"):
             getattr(L, name).restype = ctypes.c_int
     if hasattr(L, "samkv_debug_score_with_lost_copy"):          # only the debug build exports it
         L.samkv_debug_score_with_lost_copy.argtypes = [vp, shp, vp, vp, i32, vp, i32, i32, vp, ctypes.c_uint32, vp]
@@ -196,6 +223,20 @@ class Handle:
         self._h = ctypes.c_void_p()
         with torch.cuda.device(dev):
             _check(lib().samkv_create(ctypes.byref(self._h), dev, self.workspace.data_ptr(), nbytes), "samkv_create")
+
+    @classmethod
+    def for_packed(cls, packed: "Packed", device: Optional[int] = None) -> "Handle":
+        """A handle whose workspace fits samkv_prefill and samkv_paged_attn with these heads."""
+        dev = torch.cuda.current_device() if device is None else device
+        nbytes = samkv_packed_workspace_bytes(packed)
+        if nbytes == 0:
+            raise SamkvError(1, "samkv_packed_workspace_bytes")
+        self = cls.__new__(cls)
+        self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=f"cuda:{dev}")
+        self._h = ctypes.c_void_p()
+        with torch.cuda.device(dev):
+            _check(lib().samkv_create(ctypes.byref(self._h), dev, self.workspace.data_ptr(), nbytes), "samkv_create")
+        return self
 
     def close(self):
         if self._h:
@@ -352,3 +393,124 @@ def samkv_attn_share_sm(handle: Handle, on: bool) -> None:
 def samkv_attn_kernel_count(handle: Handle, shape: Shape, T_q: int, cache_capacity: int, appended: bool) -> int:
     """Kernels one samkv_attn call with these sizes launches (for launch accounting)."""
     return int(lib().samkv_attn_kernel_count(handle.h, shape.ref(), T_q, cache_capacity, int(bool(appended))))
+
+
+# ------------------------------------------------------------------ packed sequences and the paged cache
+_TORCH_DTYPES = {SAMKV_F32: torch.float32, SAMKV_BF16: torch.bfloat16}
+
+
+def _device_ptr(t: Optional[torch.Tensor], what: str, dtype: torch.dtype, shape: Sequence[int]) -> Optional[int]:
+    """Pointer of a contiguous CUDA tensor of this dtype and shape on the current device (None stays None)."""
+    if t is None:
+        return None
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{what}: expected a CUDA tensor on the current device")
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what}: expected {dtype} of shape {tuple(shape)}, got {t.dtype} of shape {tuple(t.shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{what}: expected a contiguous tensor")
+    return t.data_ptr()
+
+
+class Packed:
+    """A samkv_packed_t: sequences packed behind one another.  seq_offsets is an int32 CUDA tensor [n_seq + 1] and is
+    kept alive here; its values may change between calls."""
+
+    def __init__(self, n_q_heads: int, n_kv_heads: int, head_dim: int, seq_offsets: torch.Tensor, n_tokens: int,
+                 max_seq_tokens: int = 0, dtype="bf16"):
+        if seq_offsets.dtype != torch.int32 or seq_offsets.dim() != 1 or not seq_offsets.is_contiguous():
+            raise ValueError("seq_offsets: expected a contiguous int32 tensor [n_seq + 1]")
+        code = {"f32": SAMKV_F32, "bf16": SAMKV_BF16}[dtype] if isinstance(dtype, str) else int(dtype)
+        self.seq_offsets = seq_offsets
+        self.n_q_heads, self.n_kv_heads, self.head_dim, self.n_tokens = n_q_heads, n_kv_heads, head_dim, n_tokens
+        self.n_seq = seq_offsets.shape[0] - 1
+        self.c = samkv_packed_t(n_q_heads, n_kv_heads, head_dim, code, self.n_seq, n_tokens, max_seq_tokens,
+                                seq_offsets.data_ptr())
+
+    def ref(self):
+        return ctypes.byref(self.c)
+
+    def checked(self):
+        """The description for a call: the offsets have to be on the current device."""
+        _device_ptr(self.seq_offsets, "seq_offsets", torch.int32, (self.n_seq + 1,))
+        return ctypes.byref(self.c)
+
+    def rows(self, t: Optional[torch.Tensor], heads: int, what: str):
+        """samkv_rows_t of a tensor [n_tokens, heads, head_dim] with any token and head strides."""
+        if t is None:
+            return None
+        if not t.is_cuda or t.device.index != torch.cuda.current_device():
+            raise ValueError(f"{what}: expected a CUDA tensor on the current device")
+        want = (self.n_tokens, heads, self.head_dim)
+        if t.dtype != _TORCH_DTYPES.get(self.c.dtype) or tuple(t.shape) != want:
+            raise ValueError(f"{what}: expected {_TORCH_DTYPES.get(self.c.dtype)} of shape {want}, got {t.dtype} of shape "
+                             f"{tuple(t.shape)}")
+        if t.stride(2) != 1:
+            raise ValueError(f"{what}: the head dimension must be contiguous")
+        return ctypes.byref(samkv_rows_t(t.data_ptr(), t.stride(0), t.stride(1)))
+
+
+class Pages:
+    """A samkv_pages_t: K and V pools [n_pages, n_kv_heads, page_size, head_dim], int32 block_table [n_seq, width]."""
+
+    def __init__(self, K: torch.Tensor, V: torch.Tensor, block_table: torch.Tensor):
+        if K.dim() != 4 or block_table.dim() != 2:
+            raise ValueError("pages: expected pools of four dimensions and a table of two")
+        self.K, self.V, self.block_table = K, V, block_table
+
+    def checked(self, packed: Packed):
+        n_pages, _, page_size, _ = self.K.shape
+        pool = (n_pages, packed.n_kv_heads, page_size, packed.head_dim)
+        dt = _TORCH_DTYPES.get(packed.c.dtype)
+        width = self.block_table.shape[1]
+        return ctypes.byref(samkv_pages_t(_device_ptr(self.K, "K pages", dt, pool), _device_ptr(self.V, "V pages", dt, pool),
+                                          _device_ptr(self.block_table, "block_table", torch.int32, (packed.n_seq, width)),
+                                          page_size, n_pages, width))
+
+
+class Rope:
+    """A samkv_rope_t; inv_freq (rot_dim/2 floats per position) replaces base^(-2i/rot_dim) where given."""
+
+    def __init__(self, rot_dim: int, base: float = 10000.0, interleaved: bool = False,
+                 inv_freq: Optional[Sequence[float]] = None):
+        if inv_freq is not None and len(inv_freq) != rot_dim // 2:
+            raise ValueError("inv_freq: expected rot_dim / 2 values")
+        self._freq = None if inv_freq is None else (ctypes.c_double * len(inv_freq))(*[float(f) for f in inv_freq])
+        self.c = samkv_rope_t(rot_dim, int(bool(interleaved)), float(base),
+                              None if self._freq is None else ctypes.cast(self._freq, ctypes.POINTER(ctypes.c_double)))
+
+    def ref(self):
+        return ctypes.byref(self.c)
+
+
+def samkv_packed_workspace_bytes(packed: Packed) -> int:
+    return int(lib().samkv_packed_workspace_bytes(packed.ref()))
+
+
+def samkv_prefill(handle: Handle, packed: Packed, Q, K, V, scale: float, O, lse=None):
+    _check(lib().samkv_prefill(handle.h, packed.checked(), packed.rows(Q, packed.n_q_heads, "Q"),
+                               packed.rows(K, packed.n_kv_heads, "K"), packed.rows(V, packed.n_kv_heads, "V"),
+                               float(scale), packed.rows(O, packed.n_q_heads, "O"),
+                               _device_ptr(lse, "lse", torch.float32, (packed.n_tokens, packed.n_q_heads)), _stream()),
+           "samkv_prefill")
+
+
+def samkv_append(handle: Handle, packed: Packed, K, V, pages: Optional[Pages] = None, cache_len=None,
+                 rope: Optional[Rope] = None, positions=None, Q=None, Q_out=None, K_out=None, V_out=None):
+    _check(lib().samkv_append(handle.h, packed.checked(), packed.rows(K, packed.n_kv_heads, "K"),
+                              packed.rows(V, packed.n_kv_heads, "V"), None if pages is None else pages.checked(packed),
+                              _device_ptr(cache_len, "cache_len", torch.int32, (packed.n_seq,)),
+                              None if rope is None else rope.ref(),
+                              _device_ptr(positions, "positions", torch.int32, (packed.n_tokens,)),
+                              packed.rows(Q, packed.n_q_heads, "Q"), packed.rows(Q_out, packed.n_q_heads, "Q_out"),
+                              packed.rows(K_out, packed.n_kv_heads, "K_out"),
+                              packed.rows(V_out, packed.n_kv_heads, "V_out"), _stream()), "samkv_append")
+
+
+def samkv_paged_attn(handle: Handle, packed: Packed, pages: Pages, cache_len, Q, scale: float, causal: bool, O, lse=None):
+    _check(lib().samkv_paged_attn(handle.h, packed.checked(), pages.checked(packed),
+                                  _device_ptr(cache_len, "cache_len", torch.int32, (packed.n_seq,)),
+                                  packed.rows(Q, packed.n_q_heads, "Q"), float(scale), int(bool(causal)),
+                                  packed.rows(O, packed.n_q_heads, "O"),
+                                  _device_ptr(lse, "lse", torch.float32, (packed.n_tokens, packed.n_q_heads)), _stream()),
+           "samkv_paged_attn")

@@ -5,17 +5,12 @@
 
 #include <new>
 
-#include <stdio.h>
-
 #include "common.cuh"
 
 using namespace samkv;
 
 namespace {
 
-constexpr size_t kStatusBytes = 256;   // first bytes of the workspace: device status word
-
-inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 inline size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 inline int elem_bytes(const samkv_shape_t& s) { return s.dtype == SAMKV_BF16 ? 2 : 4; }
 
@@ -102,21 +97,6 @@ samkv_status_t make_sel_table(const samkv_shape_t* s, const Layout& lo, const in
 
 size_t qhat_bytes(const samkv_shape_t& s) {
   return round_up((size_t)s.n_layers * s.batch * s.n_ctx * s.n_kv_heads * s.head_dim * sizeof(float), 256);
-}
-
-samkv_status_t check_handle(samkv_ctx_impl* h) {
-  if (h == nullptr) return SAMKV_ERR_INVALID_ARG;
-  int dev = -1;
-  if (cudaGetDevice(&dev) != cudaSuccess) return SAMKV_ERR_CUDA;
-  if (dev != h->device) return SAMKV_ERR_CUDA;
-  return SAMKV_OK;
-}
-
-inline samkv_status_t from_cuda(cudaError_t e) {
-#ifdef SAMKV_DEBUG_CHECKS
-  if (e != cudaSuccess) fprintf(stderr, "samkv (debug build): CUDA error %d: %s\n", (int)e, cudaGetErrorString(e));
-#endif
-  return e == cudaSuccess ? SAMKV_OK : SAMKV_ERR_CUDA;
 }
 
 }  // namespace

@@ -4,6 +4,7 @@
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
+#include <stdio.h>
 
 #include "samkv.h"
 
@@ -35,6 +36,26 @@ struct samkv_ctx_impl {
   int* d_status;  // first word of the workspace
   int attn_share_sm;  // samkv_attn_share_sm(): prefer the prefill attention kernel that leaves room on its SM
 };
+
+constexpr size_t kStatusBytes = 256;   // first bytes of the workspace: device status word
+
+inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+// The handle's device must be the current one.
+inline samkv_status_t check_handle(const samkv_ctx_impl* h) {
+  if (h == nullptr) return SAMKV_ERR_INVALID_ARG;
+  int dev = -1;
+  if (cudaGetDevice(&dev) != cudaSuccess) return SAMKV_ERR_CUDA;
+  if (dev != h->device) return SAMKV_ERR_CUDA;
+  return SAMKV_OK;
+}
+
+inline samkv_status_t from_cuda(cudaError_t e) {
+#ifdef SAMKV_DEBUG_CHECKS
+  if (e != cudaSuccess) fprintf(stderr, "samkv (debug build): CUDA error %d: %s\n", (int)e, cudaGetErrorString(e));
+#endif
+  return e == cudaSuccess ? SAMKV_OK : SAMKV_ERR_CUDA;
+}
 
 // ----- launchers implemented in the .cu files (all enqueue on `stream`, return cudaGetLastError) -------
 cudaError_t launch_qhat(const samkv_shape_t& s, const void* Q, int T_q, const void* Qloc, int T_loc, int use_bias,
@@ -112,7 +133,9 @@ enum DeviceCheck : int {
   CHECK_APPEND_CAPACITY = 2, // cache_len + T_q exceeds the cache capacity
   CHECK_WAIT_TIMEOUT = 3,    // a bounded wait on an mbarrier ran out
   CHECK_SMEM_ALIGNMENT = 4,  // dynamic shared memory not aligned as the tensor-core tiles need
-  CHECK_LIST_CAPACITY = 5    // an output list is longer than the capacity the caller gave (it was truncated)
+  CHECK_LIST_CAPACITY = 5,   // an output list is longer than the capacity the caller gave (it was truncated)
+  CHECK_SEQ_RANGE = 6,       // a sequence offset or a cache length lies outside its bounds (it was clamped)
+  CHECK_PAGE_RANGE = 7       // a needed block-table entry is not a page
 };
 
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
