@@ -189,7 +189,8 @@ samkv_status_t samkv_poll_status(samkv_handle_t handle, void* stream) {
   if (cudaMemcpyAsync(&v, h->d_status, sizeof(int), cudaMemcpyDeviceToHost, s) != cudaSuccess) return SAMKV_ERR_CUDA;
   if (cudaStreamSynchronize(s) != cudaSuccess) return SAMKV_ERR_CUDA;
   if (v != 0) {
-    if (cudaMemsetAsync(h->d_status, 0, sizeof(int), s) != cudaSuccess) return SAMKV_ERR_CUDA;
+    // (a kernel that gave up may have left tickets behind: the whole block goes back to zero)
+    if (cudaMemsetAsync(h->d_status, 0, kStatusBytes, s) != cudaSuccess) return SAMKV_ERR_CUDA;
     return SAMKV_ERR_DEVICE_CHECK;
   }
   return SAMKV_OK;

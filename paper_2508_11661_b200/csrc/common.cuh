@@ -37,7 +37,7 @@ struct samkv_ctx_impl {
   int attn_share_sm;  // samkv_attn_share_sm(): prefer the prefill attention kernel that leaves room on its SM
 };
 
-constexpr size_t kStatusBytes = 256;   // first bytes of the workspace: device status word
+constexpr size_t kStatusBytes = 256;   // first bytes of the workspace: device status word and tickets, zero between calls
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
@@ -102,7 +102,7 @@ AttnPlan plan_attn(const samkv_shape_t& s, int T_q, int capacity, int sm_count, 
 // The 128-row tcgen05 kernel with exactly two KV splits merges them inside a two-CTA cluster: no merge kernel.
 inline bool attn_merges_in_cluster(const AttnPlan& p) { return p.rows_per_cta == 128 && p.n_splits == 2; }
 // Status block of the workspace (256 bytes, zero between calls): int 0 is the device check word, this int counts the
-// finished CTAs of an attention grid that bumps cache_len itself.
+// finished CTAs of an attention grid that bumps cache_len itself; the others hold the tickets of packed_plan.cuh.
 constexpr int kAttnTicketInt = 32;
 cudaError_t launch_attn(const samkv_shape_t& s, int layer, void* Kc, void* Vc, int capacity, int32_t* cache_len,
                         const void* Q, int T_q, const void* Kq, const void* Vq, float scale, void* O, float* lse,

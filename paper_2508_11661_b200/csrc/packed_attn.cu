@@ -76,20 +76,21 @@ packed_simple_kernel(const Seqs seqs, const KvSource kv, const Rows Q, const Row
   if (lse != nullptr && lane == 0) lse[(size_t)tok * Hq + hq] = l == 0.f ? -INFINITY : m + logf(l);
 }
 
-size_t packed_scratch_bytes(const samkv_packed_t&) { return 0; }
+size_t packed_tc_scratch_bytes(int d);
+cudaError_t launch_packed_tc(const samkv_packed_t& d, const Seqs& seqs, const KvSource& kv, const Rows& Q, float scale,
+                             const Rows& O, float* lse, const samkv_ctx_impl& h, cudaStream_t stream);
+
+size_t packed_scratch_bytes(const samkv_packed_t& p) { return p.dtype == SAMKV_BF16 ? packed_tc_scratch_bytes(p.head_dim) : 0; }
 
 cudaError_t launch_packed_attn(const samkv_packed_t& p, const Seqs& seqs, const KvSource& kv, const Rows& Q, float scale,
                                const Rows& O, float* lse, const samkv_ctx_impl& h, cudaStream_t stream) {
   if (scale <= 0.f) scale = 1.0f / sqrtf((float)p.head_dim);
+  if (p.dtype == SAMKV_BF16) return launch_packed_tc(p, seqs, kv, Q, scale, O, lse, h, stream);
   const long long blocks = ((long long)p.n_tokens * p.n_q_heads + 3) / 4;
   if (blocks > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
 #define SAMKV_SIMPLE(T, D) \
   packed_simple_kernel<T, D><<<(unsigned)blocks, 128, 0, stream>>>(seqs, kv, Q, O, lse, scale, p.n_q_heads, p.n_kv_heads, h.d_status)
-  if (p.dtype == SAMKV_BF16) {
-    if (p.head_dim == 128) SAMKV_SIMPLE(__nv_bfloat16, 128); else SAMKV_SIMPLE(__nv_bfloat16, 64);
-  } else {
-    if (p.head_dim == 128) SAMKV_SIMPLE(float, 128); else SAMKV_SIMPLE(float, 64);
-  }
+  if (p.head_dim == 128) SAMKV_SIMPLE(float, 128); else SAMKV_SIMPLE(float, 64);
 #undef SAMKV_SIMPLE
   return cudaGetLastError();
 }
