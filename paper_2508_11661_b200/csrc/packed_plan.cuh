@@ -66,6 +66,7 @@ __device__ __forceinline__ void plan_block(const Seqs& q, const SplitCfg& c, Pla
   long long len = 0;
   int items = 0;
   bool clamped = false;
+#pragma unroll 1
   for (int s = s0; s < s1; ++s) {
     const Seq sq = load_seq(q, s);
     const int R = row_tiles(c, sq.n);
@@ -183,6 +184,7 @@ struct Walker {
     h = (int)(rem / per_head);
     rem -= h * per_head;
     int lo = 0, hi = R - 1;                  // largest r whose items before it are no longer than rem
+#pragma unroll 1
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
       if (items_length(c, q.causal, cur.base, mid) <= rem) lo = mid; else hi = mid - 1;
@@ -193,6 +195,7 @@ struct Walker {
   }
   // Next piece; false when the CTA's stretch is done.
   __device__ __forceinline__ bool next(const Seqs& q, const SplitCfg& c, Piece* out) {
+#pragma unroll 1
     while (more) {
       const int nt = tiles(q, c);
       const long long end = item_start + item_length(q, c);
@@ -219,7 +222,9 @@ struct Walker {
         if (starts_inside || ends_inside) {
           // borders inside the item, after they have been moved to tile borders
           long long ca = item_start / chunk + 1, cb = (end - 1) / chunk;
+#pragma unroll 1
           while (ca <= cb && border(c, ca * chunk, nt) == 0) ++ca;
+#pragma unroll 1
           while (cb >= ca && border(c, cb * chunk, nt) >= nt) --cb;
           out->slot = 2 * (int)blockIdx.x + (starts_inside ? 0 : 1);
           out->ticket = (int)ca;
@@ -235,6 +240,7 @@ struct Walker {
           r = 0;
           if (++h == c.Hkv) {
             h = 0;
+#pragma unroll 1
             do {
               ++s;
               if (s >= q.n_seq) { more = false; break; }

@@ -28,11 +28,14 @@ namespace ptc {
 using namespace tc;
 
 constexpr int kBM = 128, kBN = 128;
-constexpr int kKStages = 3, kVStages = 2, kQStages = 2, kRing = 4;
-constexpr int kThreads = 384;
-constexpr int kRegsSoftmax = 216, kRegsOther = 72;     // 256 x 216 + 128 x 72 = 384 x 168, the launch's registers
+constexpr int kKStages = 2, kVStages = 3, kQStages = 2, kRing = 3;
+constexpr int kGroups = 3;                             // softmax groups, and score buffers
+constexpr int kThreads = (4 * kGroups + 4) * 32;
+constexpr int kWarpMma = 4 * kGroups, kWarpK = kWarpMma + 1, kWarpV = kWarpMma + 2;   // the last warp fills the warpgroup
+constexpr int kRegsSoftmax = 144, kRegsOther = 80;     // 384 x 144 + 128 x 80 = 512 x 128, the launch's registers
+constexpr uint32_t kIdleLimit = 1u << 24;              // polls of the issuing warp without progress (a second or so)
 constexpr float kGrow = 64.0f;                         // log2
-constexpr uint32_t kTmemCols = 512, kColO = 256, kColP = 384;
+constexpr uint32_t kTmemCols = 512, kColO = 384;       // three score buffers of 128 columns, then O
 
 template <int kD>
 struct Smem {
@@ -40,42 +43,26 @@ struct Smem {
   static constexpr int kQ = 0;
   static constexpr int kK = kQ + kQStages * kTile;
   static constexpr int kV = kK + kKStages * kTile;
-  static constexpr int kRef = kV + kVStages * kTile;   // reference maxima, 128 fp32
-  static constexpr int kSum = kRef + 512;              // denominators of both groups, [2][128] fp32
-  static constexpr int kPieces = kSum + 1024;          // kRing descriptors
-  static constexpr int kCur = kPieces + kRing * 64;    // the softmax warps' copy
-  static constexpr int kBar = kCur + 64;
-  static constexpr int kMisc = kBar + 256;             // tensor memory address, failure flag, "merge" flag
-  static constexpr int kBytes = kMisc + 64;
+  static constexpr int kRef = kV + kVStages * kTile;   // reference maxima, [128] fp32
+  static constexpr int kSum = kRef + 512;              // denominators handed to the finishing group, [2 (piece parity)][2][128]
+  static constexpr int kPieces = kSum + 2048;          // kRing descriptors
+  static constexpr int kBar = kPieces + 160;
+  static constexpr int kMisc = kBar + 320;             // tensor memory address, failure flag, "merge" and "scrub" flags
+  static constexpr int kBytes = kMisc + 32;
 };
-static_assert(sizeof(Piece) <= 64, "descriptor size");
+static_assert(kRing * sizeof(Piece) <= 160, "descriptors");
+static_assert(2 + kGroups + kRing <= 8, "flags");
 static_assert(Smem<128>::kBytes <= 232448, "shared memory of one CTA");
 
 enum Bar {
   FR_FULL = 0, FR_FREE = FR_FULL + kRing, Q_FULL = FR_FREE + kRing, Q_FREE = Q_FULL + kQStages, K_FULL = Q_FREE + kQStages,
-  K_FREE = K_FULL + kKStages, V_FULL = K_FREE + kKStages, V_TMA = V_FULL + kVStages, S_FULL = V_TMA + 1, S_FREE = S_FULL + 2,
-  P_READY = S_FREE + 2, PV_DONE = P_READY + 2, O_FREE = PV_DONE + 2, kBars = O_FREE + 1
+  V_FULL = K_FULL + kKStages, V_TMA = V_FULL + kVStages, S_FULL = V_TMA + 1,
+  P_READY = S_FULL + kGroups, PV_DONE = P_READY + kGroups, TURN = PV_DONE + kGroups, O_FREE = TURN + kGroups,
+  PARTS = O_FREE + 1, MERGE = PARTS + kGroups, kBars = MERGE + kGroups
 };
-static_assert(kBars * 8 <= 256, "barrier area");
+static_assert(kBars * 8 <= 320, "barrier area");
+static_assert(kVStages == kGroups, "a V stage is free when the value product of its group has completed");
 
-__device__ __forceinline__ uint64_t pack2(float a, float b) {
-  uint64_t r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
-  return r;
-}
-__device__ __forceinline__ void unpack2(uint64_t v, float& a, float& b) {
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v));
-}
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-  return r;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
 // maximum that keeps NaN
 __device__ __forceinline__ float max3_nan(float a, float b, float c) {
   float r;
@@ -96,19 +83,36 @@ __device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity) {
                : "=r"(done) : "r"(bar), "r"(parity) : "memory");
   return done != 0;
 }
+__device__ __forceinline__ bool test_bar(uint32_t bar, uint32_t parity) {
+  uint32_t done;
+  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+               : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+  return done != 0;
+}
 // Bounded; gives up as soon as another role has failed.
 __device__ __forceinline__ bool wait_bar(uint32_t bar, uint32_t parity, volatile uint32_t* fail) {
+#pragma unroll 1
   for (uint32_t i = 0; i < kSpinLimit; ++i) {
     if (try_wait(bar, parity)) return true;
-    if (*fail) return false;
+    if ((i & 63u) == 63u && *fail) return false;
   }
   *fail = 1;
   return false;
 }
 // For copies in flight at the end: bounded, whatever has failed.
 __device__ __forceinline__ void drain_bar(uint32_t bar, uint32_t parity) {
+#pragma unroll 1
   for (uint32_t i = 0; i < kSpinLimit; ++i)
     if (try_wait(bar, parity)) return;
+}
+
+// Pins registers that tcgen05.ld filled behind the wait for it.
+template <int kN>
+__device__ __forceinline__ void settle(float* v) {
+#pragma unroll
+  for (int i = 0; i < kN; i += 8)
+    asm volatile("" : "+f"(v[i]), "+f"(v[i + 1]), "+f"(v[i + 2]), "+f"(v[i + 3]), "+f"(v[i + 4]), "+f"(v[i + 5]),
+                 "+f"(v[i + 6]), "+f"(v[i + 7]));
 }
 
 struct Params {
@@ -132,6 +136,21 @@ __device__ __forceinline__ const __nv_bfloat16* kv_row(const Params& p, const Ro
     return base + page_offset(p.pages, pc.s, j, pc.h, p.cfg.Hkv, kD, &bad);
   }
   return base + (size_t)(pc.first + j) * rows.ts + (size_t)pc.h * rows.hs;
+}
+
+// 32 normalised columns of a row into a 128-byte-swizzled tile, from 16-byte piece `piece` on.
+__device__ __forceinline__ void stage_row(const float* o, float inv, bool empty, uint32_t tile, int row, int piece) {
+#pragma unroll
+  for (int i = 0; i < 32; i += 8) {
+    uint4 v;
+    v.x = pack_bf16(o[i] * inv, o[i + 1] * inv);
+    v.y = pack_bf16(o[i + 2] * inv, o[i + 3] * inv);
+    v.z = pack_bf16(o[i + 4] * inv, o[i + 5] * inv);
+    v.w = pack_bf16(o[i + 6] * inv, o[i + 7] * inv);
+    if (empty) v = make_uint4(0, 0, 0, 0);
+    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(tile + blk_off(row, piece + (i >> 3))), "r"(v.x), "r"(v.y),
+                 "r"(v.z), "r"(v.w) : "memory");
+  }
 }
 
 // Loads the boxes of one key or value tile; `pages` holds this tile's page numbers in the lanes.
@@ -173,15 +192,18 @@ __device__ __forceinline__ int tile_page(const Params& p, const Piece& pc, int t
   }
   return page;
 }
-// Whether a value row of slots [j0, j1) holds an infinity or NaN (one warp, global memory).
+// Whether rows [r0, r1) of a landed value tile hold an infinity or NaN (one warp).
 template <int kD>
-__device__ __forceinline__ bool any_nonfinite(const Params& p, const Piece& pc, int j0, int j1) {
+__device__ __forceinline__ bool any_nonfinite(uint32_t tile, int r0, int r1) {
   const int lane = threadIdx.x & 31;
   constexpr int kChunks = kD / 8;
   uint32_t hit = 0;
 #pragma unroll 4
-  for (int i = lane; i < (j1 - j0) * kChunks; i += 32) {
-    const uint4 v = __ldg(reinterpret_cast<const uint4*>(kv_row(p, p.V, pc, j0 + i / kChunks, kD)) + i % kChunks);
+  for (int i = lane; i < (r1 - r0) * kChunks; i += 32) {
+    const int r = r0 + i / kChunks, c = i % kChunks;
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                 : "r"(tile + (c >> 3) * (kBN * 128) + blk_off(r, c & 7)) : "memory");
     // an exponent of all ones carries into the sign's place
     hit |= ((v.x & 0x7f807f80u) + 0x00800080u) | ((v.y & 0x7f807f80u) + 0x00800080u) |
            ((v.z & 0x7f807f80u) + 0x00800080u) | ((v.w & 0x7f807f80u) + 0x00800080u);
@@ -205,30 +227,32 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
   volatile uint32_t* s_tmem = reinterpret_cast<volatile uint32_t*>(smem_raw + L::kMisc);
   volatile uint32_t* s_fail = s_tmem + 1;
   volatile uint32_t* s_merge = s_tmem + 2;
-  volatile uint32_t* s_scrub = s_tmem + 4;   // per ring entry
-  float* sums = reinterpret_cast<float*>(smem_raw + L::kSum);
+  volatile uint32_t* s_scrub = s_merge + kGroups;            // per ring entry
+  float* x_l = reinterpret_cast<float*>(smem_raw + L::kSum);
   Piece* ring = reinterpret_cast<Piece*>(smem_raw + L::kPieces);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int G = p.cfg.G;
 
   if (tid == 0) {
-    for (int i = 0; i < kRing; ++i) { mbar_init(bar(FR_FULL + i), 1); mbar_init(bar(FR_FREE + i), 4); }
-    for (int i = 0; i < kQStages; ++i) { mbar_init(bar(Q_FULL + i), 1); mbar_init(bar(Q_FREE + i), 1); }
-    for (int i = 0; i < kKStages; ++i) { mbar_init(bar(K_FULL + i), 1); mbar_init(bar(K_FREE + i), 1); }
+    for (int i = 0; i < kRing; ++i) { mbar_init(bar(FR_FULL + i), 1); mbar_init(bar(FR_FREE + i), 2 + 4 * kGroups); }
+    for (int i = 0; i < kQStages; ++i) { mbar_init(bar(Q_FULL + i), 1); mbar_init(bar(Q_FREE + i), 4); }
+    for (int i = 0; i < kKStages; ++i) mbar_init(bar(K_FULL + i), 1);
     for (int i = 0; i < kVStages; ++i) mbar_init(bar(V_FULL + i), 1);
     mbar_init(bar(V_TMA), 1);
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < kGroups; ++i) {
       mbar_init(bar(S_FULL + i), 1);
-      mbar_init(bar(S_FREE + i), 4);
       mbar_init(bar(P_READY + i), 4);
       mbar_init(bar(PV_DONE + i), 1);
+      mbar_init(bar(TURN + i), 4);
+      mbar_init(bar(PARTS + i), 4);
+      mbar_init(bar(MERGE + i), 1);
     }
-    mbar_init(bar(O_FREE), 8);
+    mbar_init(bar(O_FREE), 4);
     *s_fail = (base & 1023u) != 0;          // (never seen: the declaration asks for 1024 bytes)
     if (*s_fail) atomicMax(p.d_status, (int)CHECK_SMEM_ALIGNMENT);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 8) {
+  if (warp == kWarpMma) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(base + L::kMisc), "r"(kTmemCols)
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -243,9 +267,9 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
 
   auto wait = [&](int i, uint32_t phase) { return wait_bar(bar(i), phase & 1u, s_fail); };
 
-  if (warp >= 8) {
+  if (warp >= kWarpMma) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOther));
-    if (warp == 10) {
+    if (warp == kWarpK) {
       // ================= plan, Q and K =================
       Walker w;
       w.init(p.seqs, p.cfg, &plan, chunk);
@@ -273,11 +297,12 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
             tma_load_3d(dst + (x >> 6) * (kBM * 128), &tmQ, x, pc.h * G, pc.first + pc.r * p.cfg.tokens, q);
         }
         __syncwarp();
+#pragma unroll 1
         for (int t = pc.tile0; t < pc.tile1; ++t, ++T) {
           int next = 0;
           if constexpr (kPaged) { if (t + 1 < pc.tile1) next = tile_page(p, pc, t + 1, &bad); }
           const uint32_t st = T % kKStages;
-          if (T >= kKStages) wait(K_FREE + st, T / kKStages - 1);
+          if (T >= kKStages) wait(S_FULL + (T - kKStages) % kGroups, (T - kKStages) / kGroups);   // its score product is done
           load_tile<kD, kPaged>(p, &tmK, pc, t, base + L::kK + st * L::kTile, bar(K_FULL + st), page);
           page = next;
         }
@@ -288,8 +313,90 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         if (T > i) drain_bar(bar(K_FULL + (T - 1 - i) % kKStages), ((T - 1 - i) / kKStages) & 1u);
       for (uint32_t i = 0; i < kQStages; ++i)
         if (f > i) drain_bar(bar(Q_FULL + (f - 1 - i) % kQStages), ((f - 1 - i) / kQStages) & 1u);
-    } else {
-      // warps 8, 9, 11 follow the ring of pieces
+    } else if (warp == kWarpMma) {
+      // ================= products: S = Q K^T, O += P V =================
+      // One thread issues both, so the pipe runs them in its order: the scores of tile T + 3 may overwrite the buffer of
+      // T's probabilities right behind the product that reads them.  Neither kind waits for the other's inputs.
+      constexpr uint32_t kIdescS = instr_desc(kBM, kBN, false), kIdescO = instr_desc(kBM, kD, true);
+      const uint64_t dQ0 = smem_desc(base + L::kQ, 16, 1024), dK0 = smem_desc(base + L::kK, 16, 1024);
+      const uint64_t dV0 = smem_desc(base + L::kV, kBN * 128, 1024);
+      uint32_t fs = 0, Ts = 0, fp = 0, Tp = 0;             // pieces and tiles of the score and of the value products
+      int s_left = 0, p_tile = 0, p_first = 0, p_end = 0, p_seen = 0;
+      bool s_query = false, s_done = false, p_output = false, p_have = false;
+      uint32_t idle = 0;
+      if (lane == 0) while (!(s_done && Tp == Ts)) {
+        bool moved = false;
+        // value product of tile Tp
+        if (Tp < Ts) {
+          if (!p_have) {
+            const Piece& pc = ring[fp % kRing];            // (the score side has seen it arrive)
+            p_first = p_tile = pc.tile0;
+            p_end = pc.tile1;
+            p_seen = pc.seen;
+            p_have = true;
+            p_output = fp == 0;
+            mbar_arrive(bar(FR_FREE + fp % kRing));
+          }
+          const uint32_t g = Tp % kGroups;
+          if (!p_output) p_output = test_bar(bar(O_FREE), (fp - 1) & 1u);
+          if (p_output && test_bar(bar(P_READY + g), (Tp / kGroups) & 1u) && test_bar(bar(V_FULL + g), (Tp / kGroups) & 1u)) {
+            tc_fence_after();
+            {
+              const uint64_t dV = dV0 + (uint64_t)(g * (L::kTile >> 4));
+              const int slots = p_seen - p_tile * kBN;     // steps of 16 slots that some row sees
+#pragma unroll
+              for (int ks = 0; ks < kBN / 16; ++ks)
+                if (ks == 0 || ks * 16 < slots)
+                  mma_ts(tmem + kColO, tmem + g * kBN + ks * 8, dV + ((ks * 16 * 128) >> 4), kIdescO, (p_tile > p_first) | (ks > 0));
+              mma_commit(bar(PV_DONE + g));
+            }
+            ++Tp;
+            if (++p_tile == p_end) {
+              p_have = false;
+              ++fp;
+            }
+            moved = true;
+          }
+        }
+        // score product of tile Ts
+        if (!s_done && Ts < Tp + kGroups) {
+          if (s_left == 0 && test_bar(bar(FR_FULL + fs % kRing), (fs / kRing) & 1u)) {
+            const Piece& pc = ring[fs % kRing];
+            if (pc.tile0 < 0) {
+              s_done = true;
+              moved = true;
+            } else {
+              s_left = pc.tile1 - pc.tile0;
+              s_query = false;
+            }
+          }
+          if (s_left > 0 && !s_query) s_query = test_bar(bar(Q_FULL + fs % kQStages), (fs / kQStages) & 1u);
+          const uint32_t st = Ts % kKStages;
+          if (s_left > 0 && s_query && test_bar(bar(K_FULL + st), (Ts / kKStages) & 1u)) {
+            tc_fence_after();
+            {
+              const uint64_t dQ = dQ0 + (uint64_t)((fs % kQStages) * (L::kTile >> 4)), dK = dK0 + (uint64_t)(st * (L::kTile >> 4));
+#pragma unroll
+              for (int ks = 0; ks < kD / 16; ++ks) {
+                const uint32_t aoff = ((ks >> 2) * (kBM * 128) + (ks & 3) * 32) >> 4;
+                const uint32_t boff = ((ks >> 2) * (kBN * 128) + (ks & 3) * 32) >> 4;
+                mma_ss(tmem + (Ts % kGroups) * kBN, dQ + aoff, dK + boff, kIdescS, ks > 0);
+              }
+              mma_commit(bar(S_FULL + Ts % kGroups));
+            }
+            ++Ts;
+            if (--s_left == 0) ++fs;
+            moved = true;
+          }
+        }
+        idle = moved ? 0 : idle + 1;
+        if ((idle & 63u) == 63u) {
+          if (*s_fail) break;
+          if (idle > kIdleLimit) *s_fail = 1;
+        }
+      }
+      __syncwarp();
+    } else if (warp == kWarpV) {
       uint32_t f = 0, T = 0, partial_tiles = 0;
       while (true) {
         if (!wait(FR_FULL + f % kRing, f / kRing)) break;
@@ -297,91 +404,44 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(FR_FREE + f % kRing));
         if (pc.tile0 < 0) break;
-        if (warp == 8) {
-          // ================= S = Q K^T =================
-          constexpr uint32_t kIdesc = instr_desc(kBM, kBN, false);
-          const uint64_t dQ = smem_desc(base + L::kQ + (f % kQStages) * L::kTile, 16, 1024);
-          wait(Q_FULL + f % kQStages, f / kQStages);
-          for (int t = pc.tile0; t < pc.tile1; ++t, ++T) {
-            const uint32_t st = T % kKStages, g = T & 1u;
-            wait(K_FULL + st, T / kKStages);
-            if (T >= 2) wait(S_FREE + g, (T >> 1) - 1);
-            tc_fence_after();
-            if (lane == 0) {
-              const uint64_t dK = smem_desc(base + L::kK, 16, 1024) + (uint64_t)(st * (L::kTile >> 4));
-#pragma unroll
-              for (int ks = 0; ks < kD / 16; ++ks) {
-                const uint32_t aoff = ((ks >> 2) * (kBM * 128) + (ks & 3) * 32) >> 4;
-                const uint32_t boff = ((ks >> 2) * (kBN * 128) + (ks & 3) * 32) >> 4;
-                mma_ss(tmem + g * kBN, dQ + aoff, dK + boff, kIdesc, ks > 0);
-              }
-              mma_commit(bar(S_FULL + g));
-              mma_commit(bar(K_FREE + st));
-              if (t + 1 == pc.tile1) mma_commit(bar(Q_FREE + f % kQStages));
-            }
-            __syncwarp();
-          }
-        } else if (warp == 9) {
-          // ================= O += P V =================
-          constexpr uint32_t kIdesc = instr_desc(kBM, kD, true);
-          for (int t = pc.tile0; t < pc.tile1; ++t, ++T) {
-            const uint32_t g = T & 1u;
-            wait(V_FULL + g, T >> 1);
-            if (t == pc.tile0 && f > 0) wait(O_FREE, f - 1);
-            wait(P_READY + g, T >> 1);
-            tc_fence_after();
-            if (lane == 0) {
-              const uint64_t dV = smem_desc(base + L::kV, kBN * 128, 1024) + (uint64_t)(g * (L::kTile >> 4));
-              const int slots = pc.seen - t * kBN;                 // steps of 16 slots that some row sees
-#pragma unroll
-              for (int ks = 0; ks < kBN / 16; ++ks)
-                if (ks == 0 || ks * 16 < slots) mma_ts(tmem + kColO, tmem + kColP + g * 64 + ks * 8, dV + ((ks * 16 * 128) >> 4), kIdesc,
-                       (t > pc.tile0) | (ks > 0));
-              mma_commit(bar(PV_DONE + g));
-            }
-            __syncwarp();
-          }
-        } else {
+        {
           // ================= V =================
           // Of the slots that only some rows of the tile see, infinities and NaN must not meet the zero weights of the
-          // others: they are looked for ahead of time (L2 reads of at most 127 rows), and in the rare case that there are
-          // any they are cleared in shared memory and added back, row by row, when the result is written.
+          // others: they are looked for in the landed tile (at most 127 rows of it), and in the rare case that there are
+          // any they are cleared there and added back, row by row, when the result is written.
           int page = 0;
           bool bad = false;                                        // (reported by the K loader)
           if constexpr (kPaged) page = tile_page(p, pc, pc.tile0, &bad);
-          bool scrub = false;
           const int zone0 = max(pc.seen0, pc.tile0 * kBN), zone1 = min(pc.seen, pc.tile1 * kBN);
-          const int scan_at = max(pc.tile0, zone0 / kBN - 1);
           if (lane == 0) s_scrub[f % kRing] = 0;
           __syncwarp();
+#pragma unroll 1
           for (int t = pc.tile0; t < pc.tile1; ++t, ++T) {
             int next = 0;
             if constexpr (kPaged) { if (t + 1 < pc.tile1) next = tile_page(p, pc, t + 1, &bad); }
-            if (t == scan_at && zone0 < zone1) {
-              scrub = any_nonfinite<kD>(p, pc, zone0, zone1);
-              if (scrub && lane == 0) s_scrub[f % kRing] = 1;
-              __syncwarp();
-            }
-            const uint32_t g = T & 1u, dst = base + L::kV + g * L::kTile;
-            if (T >= 2) wait(PV_DONE + g, (T >> 1) - 1);
+            const uint32_t st = T % kVStages, dst = base + L::kV + st * L::kTile;
+            if (T >= kVStages) wait(PV_DONE + st, T / kVStages - 1);
             const int slots = pc.seen - t * kBN;                   // slots behind `seen` that a step of 16 still covers
             const bool clear = slots < kBN && (slots & 15) != 0 || slots <= 0;
-            const bool wash = scrub && t * kBN + kBN > zone0;
-            if (!clear && !wash) {
-              load_tile<kD, kPaged>(p, &tmV, pc, t, dst, bar(V_FULL + g), page);
+            const int r0 = max(zone0 - t * kBN, 0), r1 = min(zone1 - t * kBN, kBN);
+            const bool look = r0 < r1;
+            if (!clear && !look) {
+              load_tile<kD, kPaged>(p, &tmV, pc, t, dst, bar(V_FULL + st), page);
             } else {
               load_tile<kD, kPaged>(p, &tmV, pc, t, dst, bar(V_TMA), page);
               wait(V_TMA, partial_tiles++);
               if (clear) {
                 const int first = max(slots, 0), end = max((first + 15) & ~15, 16);
+#pragma unroll 1
                 for (int i = lane; i < (end - first) * (kD / 8); i += 32) {
                   const int r = first + i / (kD / 8), c = i % (kD / 8);
                   asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(dst + (c >> 3) * (kBN * 128) + blk_off(r, c & 7)),
                                "r"(0) : "memory");
                 }
               }
-              if (wash) {
-                const int r0 = max(zone0 - t * kBN, 0), r1 = min(zone1 - t * kBN, kBN);
+              if (look && any_nonfinite<kD>(dst, r0, r1)) {
+                if (lane == 0) s_scrub[f % kRing] = 1;
+#pragma unroll 1
                 for (int i = lane; i < (r1 - r0) * (kD / 2); i += 32) {
                   const int r = r0 + i / (kD / 2), w = i % (kD / 2);
                   const uint32_t at = dst + (w >> 5) * (kBN * 128) + blk_off(r, (w >> 2) & 7) + (w & 3) * 4;
@@ -394,7 +454,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
               }
               fence_proxy_async();
               __syncwarp();
-              if (lane == 0) mbar_arrive(bar(V_FULL + g));
+              if (lane == 0) mbar_arrive(bar(V_FULL + st));
               __syncwarp();
             }
             page = next;
@@ -402,7 +462,6 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         }
         ++f;
       }
-      if (warp == 11)
         for (uint32_t i = 0; i < kVStages; ++i)
           if (T > i) drain_bar(bar(V_FULL + (T - 1 - i) % kVStages), ((T - 1 - i) / kVStages) & 1u);
     }
@@ -411,77 +470,83 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
     const int g = warp >> 2, row = (warp & 3) * 32 + lane;
     const uint32_t lane_addr = tmem + ((uint32_t)((warp & 3) * 32) << 16);
-    const uint32_t tS = lane_addr + g * kBN, tO = lane_addr + kColO, tP = lane_addr + kColP + g * 64;
+    const uint32_t tS = lane_addr + g * kBN, tO = lane_addr + kColO;      // P overlays the first half of the scores
     const float sl2 = p.scale * kLog2e;
-    const uint64_t sl2_2 = pack2(sl2, sl2);
     const int t_local = row / G, member = row - t_local * G;
-    auto bar_sync = [&](int id) { asm volatile("bar.sync %0, 256;" ::"r"(id) : "memory"); };
-    uint32_t f = 0, T = 0;
-    Piece* cur = reinterpret_cast<Piece*>(smem_raw + L::kCur);
+    uint32_t f = 0, T = 0, n_merged = 0;
     while (true) {
-      if (tid == 0) {                                    // one decision for all eight warps
-        const bool ok = wait(FR_FULL + f % kRing, f / kRing);
-        *cur = ring[f % kRing];
-        if (!ok) cur->tile0 = -1;
-        mbar_arrive(bar(FR_FREE + f % kRing));
-      }
-      bar_sync(1);
-      const Piece pc = *cur;
+      if (!wait(FR_FULL + f % kRing, f / kRing)) break;
+      const Piece pc = ring[f % kRing];
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(FR_FREE + f % kRing));
       if (pc.tile0 < 0) break;
+      const uint32_t Tend = T + (uint32_t)(pc.tile1 - pc.tile0);
+      // The group with the piece's last tile finishes it; the others go on to the next piece at once.
+      const bool finishes = (Tend - 1) % kGroups == (uint32_t)g;
       const int t_seq = pc.r * p.cfg.tokens + t_local;
       const bool valid = t_local < p.cfg.tokens && t_seq < pc.n;
       Seq sq;
       sq.first = pc.first; sq.n = pc.n; sq.base = pc.base;
       // rows without a token follow the last one: their results are dropped
       const int vis = visible(p.seqs, sq, min(t_seq, min((pc.r + 1) * p.cfg.tokens, pc.n) - 1));
+      float* ref_row = ref_max + row;
+      float* l_row = x_l + (f & 1u) * 256 + row;         // [0]: of the tile before the last, [128]: of the one before that
       float m = -INFINITY, l = 0.f;
+      float m_other = -INFINITY;                         // what the other groups' denominators refer to
       bool poison = false;
-      for (int t = pc.tile0; t < pc.tile1; ++t, ++T) {
-        if ((T & 1u) != (uint32_t)g) continue;
-        wait(S_FULL + g, T >> 1);
+#pragma unroll 1
+      for (int t = pc.tile0 + (int)((kGroups + g - T % kGroups) % kGroups); t < pc.tile1; t += kGroups) {
+        const uint32_t Tt = T + (uint32_t)(t - pc.tile0);
+        wait(S_FULL + g, Tt / kGroups);
         tc_fence_after();
-        float sv[kBN];
-#pragma unroll
-        for (int c0 = 0; c0 < kBN; c0 += 32) tmem_ld32_nowait(tS + c0, sv + c0);
-        tmem_wait_ld();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(S_FREE + g));     // the next score product may overwrite the buffer
+        // first pass over the scores: their maximum (64 columns at a time; the loops stay rolled so that the whole
+        // softmax fits the instruction cache next to the other roles' code)
         const int limit = vis - t * kBN;
-        if (__any_sync(0xffffffffu, limit < kBN)) {
-#pragma unroll
-          for (int i = 0; i < kBN; ++i)
-            if (i >= limit) sv[i] = -INFINITY;
-        }
+        const int width = min(pc.seen - t * kBN, kBN);   // slots that some row sees
+        const bool masked = __any_sync(0xffffffffu, limit < kBN);
         float mx0 = -INFINITY, mx1 = -INFINITY, mx2 = -INFINITY, mx3 = -INFINITY;
+#pragma unroll 1
+        for (int c0 = 0; c0 < kBN; c0 += 64) {
+          float sv[64];
+          tmem_ld32_nowait(tS + c0, sv);
+          tmem_ld32_nowait(tS + c0 + 32, sv + 32);
+          tmem_wait_ld();
+          settle<64>(sv);
+          if (masked) {
 #pragma unroll
-        for (int i = 0; i < kBN; i += 8) {
-          mx0 = max3_nan(mx0, sv[i], sv[i + 1]);
-          mx1 = max3_nan(mx1, sv[i + 2], sv[i + 3]);
-          mx2 = max3_nan(mx2, sv[i + 4], sv[i + 5]);
-          mx3 = max3_nan(mx3, sv[i + 6], sv[i + 7]);
+            for (int i = 0; i < 64; ++i)
+              if (c0 + i >= limit) sv[i] = -INFINITY;
+          }
+#pragma unroll
+          for (int i = 0; i < 64; i += 8) {
+            mx0 = max3_nan(mx0, sv[i], sv[i + 1]);
+            mx1 = max3_nan(mx1, sv[i + 2], sv[i + 3]);
+            mx2 = max3_nan(mx2, sv[i + 4], sv[i + 5]);
+            mx3 = max3_nan(mx3, sv[i + 6], sv[i + 7]);
+          }
         }
         const float cand = max3_nan(max3_nan(mx0, mx1, mx2), mx3, mx3) * sl2;
         poison |= !(cand < INFINITY);                    // NaN or +infinity among the row's scores
         // the reference maximum, handed on from tile to tile
-        float ref = -INFINITY;
-        if (t > pc.tile0) {
-          bar_sync(2 + g);
-          ref = ref_max[row];
-        }
+        if (Tt > 0) wait(TURN + g, (Tt - 1) / kGroups);
+        const bool first = t == pc.tile0;
+        const float ref = first ? -INFINITY : *ref_row;
         const bool grow = cand - ref > kGrow || (ref == -INFINITY && cand > -INFINITY);
         const float ref_new = grow ? cand : ref;
-        if (grow || t == pc.tile0) ref_max[row] = ref_new;
-        if (t + 1 < pc.tile1) asm volatile("bar.arrive %0, 256;" ::"r"(2 + (g ^ 1)) : "memory");
+        if (grow || first) *ref_row = ref_new;
+        m_other = ref;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(TURN + (g + 1) % kGroups));
         if (m != ref_new) {                              // (also when the other group moved it)
           l = l > 0.f ? l * fast_exp2(m - ref_new) : l;
           m = ref_new;
         }
-        if (T >= 2) wait(PV_DONE + g, (T >> 1) - 1);     // this group's P buffer is free
-        if (t > pc.tile0 && __any_sync(0xffffffffu, grow)) {
-          wait(PV_DONE + (g ^ 1), (T - 1) >> 1);         // O holds everything before this tile, at the old reference
+        if (!first && __any_sync(0xffffffffu, grow)) {
+          wait(PV_DONE + (g + kGroups - 1) % kGroups, (Tt - 1) / kGroups);   // O holds everything before this tile, at the old reference
           tc_fence_after();
           const float corr = grow ? fast_exp2(ref - ref_new) : 1.0f;
+          // (a denominator that was handed over already and whose reader would not notice this step)
+          if (t + 2 == pc.tile1 && t > pc.tile0 && l_row[128] > 0.f) l_row[128] *= corr;
 #pragma unroll 1
           for (int c0 = 0; c0 < kD; c0 += 32) {
             float o[32];
@@ -492,130 +557,177 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
           }
         }
         const float mu = m == -INFINITY ? 0.f : m;
-        const uint64_t negmu2 = pack2(-mu, -mu);
-        uint64_t suma = pack2(0.f, 0.f), sumb = suma;
+        // second pass: probabilities, 32 columns at a time, the next ones under way meanwhile.  (No row sees slots behind
+        // `width`: the value product skips them.)
+        float sum0 = 0.f, sum1 = 0.f, sum2 = 0.f, sum3 = 0.f;
+        auto exponentials = [&](float* x, int c0) {
+          if (masked) {
 #pragma unroll
-        for (int c0 = 0; c0 < kBN; c0 += 32) {
-          if (c0 > 0 && c0 >= pc.seen - t * kBN) break;  // no row sees these slots: the value product skips them
+            for (int i = 0; i < 32; ++i)
+              if (c0 + i >= limit) x[i] = -INFINITY;
+          }
           uint32_t pk[16];
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            float x0, x1;
-            unpack2(fma2(pack2(sv[c0 + 2 * i], sv[c0 + 2 * i + 1]), sl2_2, negmu2), x0, x1);
-            const float p0 = fast_exp2(x0), p1 = fast_exp2(x1);
-            if (i & 1) sumb = add2(sumb, pack2(p0, p1)); else suma = add2(suma, pack2(p0, p1));
-            pk[i] = round_pair(p0, p1);
+          for (int i = 0; i < 32; i += 4) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) x[i + k] = fast_exp2(fmaf(x[i + k], sl2, -mu));
+            sum0 += x[i];
+            sum1 += x[i + 1];
+            sum2 += x[i + 2];
+            sum3 += x[i + 3];
+            pk[i / 2] = round_pair(x[i], x[i + 1]);
+            pk[i / 2 + 1] = round_pair(x[i + 2], x[i + 3]);
           }
-          tmem_st16(tP + (c0 >> 1), pk);
+          tmem_st16(tS + (c0 >> 1), pk);
+        };
+        float xa[32], xb[32];
+        tmem_ld32_nowait(tS, xa);
+#pragma unroll 1
+        for (int c0 = 0; c0 < max(width, 1); c0 += 64) {
+          tmem_wait_ld();
+          settle<32>(xa);
+          if (c0 + 32 < width) tmem_ld32_nowait(tS + c0 + 32, xb);
+          exponentials(xa, c0);
+          if (c0 + 32 >= width) break;
+          tmem_wait_ld();
+          settle<32>(xb);
+          if (c0 + 64 < width) tmem_ld32_nowait(tS + c0 + 64, xa);
+          exponentials(xb, c0 + 32);
         }
-        float a, b;
-        unpack2(add2(suma, sumb), a, b);
-        l += a + b;
+        l += (sum0 + sum1) + (sum2 + sum3);
+        if (t + 2 == pc.tile1) l_row[0] = poison ? __int_as_float(0x7fffffff) : l;
+        if (t + 3 == pc.tile1) l_row[128] = poison ? __int_as_float(0x7fffffff) : l;
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(P_READY + g));
       }
-      if (poison) l = __int_as_float(0x7fffffff);
-      // ---- the piece's result: denominators of both groups, this group's half of the columns ----
-      bar_sync(1);                                       // every tile has decided on the reference
-      const float m_fin = ref_max[row];
-      const float mu_fin = m_fin == -INFINITY ? 0.f : m_fin;
-      if (l != 0.f) l *= fast_exp2(m - mu_fin);
-      sums[g * 128 + row] = l;
-      bar_sync(1);
-      l += sums[(g ^ 1) * 128 + row];
-      const uint32_t last = T - 1;
-      wait(PV_DONE + (last & 1u), last >> 1);
-      tc_fence_after();
-      float o[kD / 2];
+      T = Tend;
+      if (finishes) {
+        // ---- the piece's result ----
+        if (poison) l = __int_as_float(0x7fffffff);
+        const float mu = m == -INFINITY ? 0.f : m;       // the last tile's group holds the final reference
+        wait(PV_DONE + g, (T - 1) / kGroups);
+        tc_fence_after();
 #pragma unroll
-      for (int c0 = 0; c0 < kD / 2; c0 += 32) tmem_ld32_nowait(tO + g * (kD / 2) + c0, o + c0);
-      tmem_wait_ld();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar(O_FREE));
-      const bool store = valid && *s_fail == 0;
-      if (s_scrub[f % kRing] != 0 && store) {
-        // infinities and NaN that were cleared from the value tile: back into the rows that see them
-        for (int j = max(pc.seen0, pc.tile0 * kBN); j < min(vis, pc.tile1 * kBN); ++j) {
-          const __nv_bfloat16* v = kv_row(p, p.V, pc, j, kD) + g * (kD / 2);
+        for (int k = 0; k < kGroups - 1; ++k) {          // (their products come before this tile's)
+          const float l_other = pc.tile1 - pc.tile0 > k + 1 ? l_row[k * 128] : 0.f;
+          if (l_other != 0.f) l += l_other * fast_exp2(m_other - mu);
+        }
+        const bool store = valid && *s_fail == 0;
+        const bool scrubbed = s_scrub[f % kRing] != 0;
+        const int tok = pc.first + t_seq, hq = pc.h * G + member;
+        const uint32_t sO = base + L::kQ + (f % kQStages) * L::kTile;       // over the piece's Q tile: no product reads it now
+        // 32 columns of the row at a time: a whole item is normalised into shared memory, a piece of a cut item goes to the
+        // workspace as it is
+        const float inv = l == 0.f ? 0.f : 1.0f / l;
+#pragma unroll 1
+        for (int c0 = 0; c0 < kD; c0 += 32) {
+          float o[32];
+          tmem_ld32_nowait(tO + c0, o);
+          tmem_wait_ld();
+          settle<32>(o);
+          if (scrubbed && store) {
+            // infinities and NaN that were cleared from the value tile: back into the rows that see them
+#pragma unroll 1
+            for (int j = max(pc.seen0, pc.tile0 * kBN); j < min(vis, pc.tile1 * kBN); ++j) {
+              const __nv_bfloat16* v = kv_row(p, p.V, pc, j, kD) + c0;
 #pragma unroll
-          for (int i = 0; i < kD / 2; ++i) {
-            const float x = __bfloat162float(v[i]);
-            if (!(fabsf(x) < INFINITY)) o[i] += x;
+              for (int i = 0; i < 32; ++i) {
+                const float y = __bfloat162float(v[i]);
+                if (!(fabsf(y) < INFINITY)) o[i] += y;
+              }
+            }
+          }
+          if (pc.slot < 0) {
+            stage_row(o, inv, l == 0.f, sO + (c0 >> 6) * (kBM * 128), row, (c0 & 63) >> 3);
+          } else {
+            float4* po = p.part_o + ((size_t)pc.slot * (kD / 4) + c0 / 4) * 128 + row;
+#pragma unroll
+            for (int i = 0; i < 32; i += 4) po[(i >> 2) * 128] = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
           }
         }
-      }
-      const int tok = pc.first + t_seq, hq = pc.h * G + member;
-      if (pc.slot < 0) {
-        if (store) {
-          const float inv = l == 0.f ? 0.f : 1.0f / l;
-          __nv_bfloat16* op = static_cast<__nv_bfloat16*>(p.O.data) + (size_t)tok * p.O.ts + (size_t)hq * p.O.hs + g * (kD / 2);
-#pragma unroll
-          for (int i = 0; i < kD / 2; i += 8) {
-            uint4 v;
-            v.x = pack_bf16(o[i] * inv, o[i + 1] * inv);
-            v.y = pack_bf16(o[i + 2] * inv, o[i + 3] * inv);
-            v.z = pack_bf16(o[i + 4] * inv, o[i + 5] * inv);
-            v.w = pack_bf16(o[i + 6] * inv, o[i + 7] * inv);
-            if (l == 0.f) v = make_uint4(0, 0, 0, 0);
-            *reinterpret_cast<uint4*>(op + i) = v;
-          }
-          if (g == 0 && p.lse != nullptr) p.lse[(size_t)tok * p.Hq + hq] = l == 0.f ? -INFINITY : m_fin * kLn2 + logf(l);
-        }
-      } else {
-        // ---- a piece of a cut item: leave (m, l, O); whoever takes the last ticket merges in order of the pieces ----
-        float4* po = p.part_o + ((size_t)pc.slot * (kD / 4) + g * (kD / 8)) * 128 + row;
-#pragma unroll
-        for (int i = 0; i < kD / 2; i += 4) po[(i >> 2) * 128] = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
-        if (g == 0) p.part_ml[pc.slot * 128 + row] = make_float2(m_fin, l);
-        __threadfence();
-        bar_sync(1);
-        if (tid == 0) *s_merge = last_piece(p.d_status, pc.ticket, pc.n_pieces);
-        bar_sync(1);
-        if (*s_merge) {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(O_FREE));
+        bool write = true;
+        float m_out = m;
+        if (pc.slot >= 0) {
+          // whoever takes the last ticket merges the item's pieces in their order
+          p.part_ml[pc.slot * 128 + row] = make_float2(m, l);
           __threadfence();
-          float M = -INFINITY;
-          for (int k = 0; k < pc.n_pieces; ++k) {
-            const float2 x = __ldcg(p.part_ml + piece_slot(pc.ticket, k) * 128 + row);
-            M = x.y == 0.f ? M : fmaxf(M, x.x);
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(PARTS + g));
+          wait(PARTS + g, n_merged);
+          if (warp == 4 * g && lane == 0) {
+            s_merge[g] = last_piece(p.d_status, pc.ticket, pc.n_pieces);
+            mbar_arrive(bar(MERGE + g));
           }
-          const float Mu = M == -INFINITY ? 0.f : M;
-          float Ls = 0.f;
-#pragma unroll
-          for (int i = 0; i < kD / 2; ++i) o[i] = 0.f;
-          for (int k = 0; k < pc.n_pieces; ++k) {
-            const int slot = piece_slot(pc.ticket, k);
-            const float2 x = __ldcg(p.part_ml + slot * 128 + row);
-            if (x.y == 0.f) continue;                    // a piece that saw nothing of this row
-            const float w = fast_exp2(x.x - Mu);
-            Ls += x.y * w;
-            const float4* src = p.part_o + ((size_t)slot * (kD / 4) + g * (kD / 8)) * 128 + row;
-#pragma unroll
-            for (int i = 0; i < kD / 2; i += 4) {
-              const float4 v = __ldcg(src + (i >> 2) * 128);
-              o[i] = fmaf(v.x, w, o[i]);
-              o[i + 1] = fmaf(v.y, w, o[i + 1]);
-              o[i + 2] = fmaf(v.z, w, o[i + 2]);
-              o[i + 3] = fmaf(v.w, w, o[i + 3]);
+          wait(MERGE + g, n_merged++);
+          write = s_merge[g] != 0;
+          if (write) {
+            __threadfence();
+            m_out = -INFINITY;
+#pragma unroll 1
+            for (int k = 0; k < pc.n_pieces; ++k) {
+              const float2 x = __ldcg(p.part_ml + piece_slot(pc.ticket, k) * 128 + row);
+              m_out = x.y == 0.f ? m_out : fmaxf(m_out, x.x);
             }
-          }
-          if (store) {
-            const float inv = Ls == 0.f ? 0.f : 1.0f / Ls;
-            __nv_bfloat16* op = static_cast<__nv_bfloat16*>(p.O.data) + (size_t)tok * p.O.ts + (size_t)hq * p.O.hs + g * (kD / 2);
-#pragma unroll
-            for (int i = 0; i < kD / 2; i += 8) {
-              uint4 v;
-              v.x = pack_bf16(o[i] * inv, o[i + 1] * inv);
-              v.y = pack_bf16(o[i + 2] * inv, o[i + 3] * inv);
-              v.z = pack_bf16(o[i + 4] * inv, o[i + 5] * inv);
-              v.w = pack_bf16(o[i + 6] * inv, o[i + 7] * inv);
-              *reinterpret_cast<uint4*>(op + i) = v;
+            const float Mu = m_out == -INFINITY ? 0.f : m_out;
+            l = 0.f;
+#pragma unroll 1
+            for (int k = 0; k < pc.n_pieces; ++k) {
+              const float2 x = __ldcg(p.part_ml + piece_slot(pc.ticket, k) * 128 + row);
+              if (x.y != 0.f) l += x.y * fast_exp2(x.x - Mu);
             }
-            if (g == 0 && p.lse != nullptr) p.lse[(size_t)tok * p.Hq + hq] = Ls == 0.f ? -INFINITY : M * kLn2 + logf(Ls);
+            const float inv_all = l == 0.f ? 0.f : 1.0f / l;
+#pragma unroll 1
+            for (int c0 = 0; c0 < kD; c0 += 32) {
+              float o[32];
+#pragma unroll
+              for (int i = 0; i < 32; ++i) o[i] = 0.f;
+#pragma unroll 2
+              for (int k = 0; k < pc.n_pieces; ++k) {
+                const int slot = piece_slot(pc.ticket, k);
+                const float2 x = __ldcg(p.part_ml + slot * 128 + row);
+                const float w = x.y == 0.f ? 0.f : fast_exp2(x.x - Mu);
+                const float4* src = p.part_o + ((size_t)slot * (kD / 4) + c0 / 4) * 128 + row;
+#pragma unroll
+                for (int i = 0; i < 32; i += 4) {
+                  const float4 v = __ldcg(src + (i >> 2) * 128);
+                  if (x.y != 0.f) {                      // (a piece that saw nothing of this row adds nothing)
+                    o[i] = fmaf(v.x, w, o[i]);
+                    o[i + 1] = fmaf(v.y, w, o[i + 1]);
+                    o[i + 2] = fmaf(v.z, w, o[i + 2]);
+                    o[i + 3] = fmaf(v.w, w, o[i + 3]);
+                  }
+                }
+              }
+              stage_row(o, inv_all, l == 0.f, sO + (c0 >> 6) * (kBM * 128), row, (c0 & 63) >> 3);
+            }
           }
         }
+        if (write) {
+          // the rows leave shared memory in whole lines
+          if (store && p.lse != nullptr) p.lse[(size_t)tok * p.Hq + hq] = l == 0.f ? -INFINITY : m_out * kLn2 + logf(l);
+          __syncwarp();
+          constexpr int kLanes = kD / 8;                 // lanes per row
+          const unsigned rows_ok = __ballot_sync(0xffffffffu, store);
+          const long long row_off = (long long)tok * p.O.ts + (long long)hq * p.O.hs;
+          const int row0 = (warp & 3) * 32;
+#pragma unroll 4
+          for (int i = 0; i < 32; i += 32 / kLanes) {
+            const int r = i + lane / kLanes, c = lane % kLanes;
+            const long long off = __shfl_sync(0xffffffffu, row_off, r);
+            uint4 v;
+            asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                         : "r"(sO + (c >> 3) * (kBM * 128) + blk_off(row0 + r, c & 7)) : "memory");
+            if (rows_ok >> r & 1u) *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.O.data) + off + c * 8) = v;
+          }
+          fence_proxy_async();
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(Q_FREE + f % kQStages));
       }
       ++f;
     }
@@ -624,7 +736,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
   __syncthreads();
   pdl_launch_dependents();
   if (tid == 0 && *s_fail) atomicMax(p.d_status, (int)CHECK_WAIT_TIMEOUT);
-  if (warp == 8) {
+  if (warp == kWarpMma) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
   }
