@@ -31,9 +31,10 @@ constexpr int kBM = 128, kBN = 128;
 constexpr int kKStages = 2, kVStages = 3, kQStages = 2, kRing = 3;
 constexpr int kGroups = 3;                             // softmax groups, and score buffers
 constexpr int kThreads = (4 * kGroups + 4) * 32;
-constexpr int kWarpMma = 4 * kGroups, kWarpK = kWarpMma + 1, kWarpV = kWarpMma + 2;   // the last warp fills the warpgroup
+constexpr int kWarpS = 4 * kGroups, kWarpPV = kWarpS + 1, kWarpK = kWarpS + 2, kWarpV = kWarpS + 3;
 constexpr int kRegsSoftmax = 144, kRegsOther = 80;     // 384 x 144 + 128 x 80 = 512 x 128, the launch's registers
-constexpr uint32_t kIdleLimit = 1u << 24;              // polls of the issuing warp without progress (a second or so)
+// Waits are within a CTA and last microseconds; a poll that suspends takes about 4 us.
+constexpr uint32_t kWaitPolls = 1u << 17, kDrainPolls = 1u << 10;
 constexpr float kGrow = 64.0f;                         // log2
 constexpr uint32_t kTmemCols = 512, kColO = 384;       // three score buffers of 128 columns, then O
 
@@ -43,24 +44,29 @@ struct Smem {
   static constexpr int kQ = 0;
   static constexpr int kK = kQ + kQStages * kTile;
   static constexpr int kV = kK + kKStages * kTile;
-  static constexpr int kRef = kV + kVStages * kTile;   // reference maxima, [128] fp32
-  static constexpr int kSum = kRef + 512;              // denominators handed to the finishing group, [2 (piece parity)][2][128]
-  static constexpr int kPieces = kSum + 2048;          // kRing descriptors
+  static constexpr int kRef = kV + kVStages * kTile;   // reference maxima, [kGroups (piece mod)][128] fp32
+  static constexpr int kSum = kRef + kGroups * 512;    // denominators handed to the finishing group, [2][128] fp32
+  static constexpr int kPieces = kSum + 1024;          // kRing descriptors
   static constexpr int kBar = kPieces + 160;
-  static constexpr int kMisc = kBar + 320;             // tensor memory address, failure flag, "merge" and "scrub" flags
-  static constexpr int kBytes = kMisc + 32;
+  static constexpr int kMisc = kBar + 288;             // tensor memory address, failure flag, "merge" and "scrub" flags
+  static constexpr int kBytes = kMisc + 64;
 };
 static_assert(kRing * sizeof(Piece) <= 160, "descriptors");
-static_assert(2 + kGroups + kRing <= 8, "flags");
+
 static_assert(Smem<128>::kBytes <= 232448, "shared memory of one CTA");
 
 enum Bar {
-  FR_FULL = 0, FR_FREE = FR_FULL + kRing, Q_FULL = FR_FREE + kRing, Q_FREE = Q_FULL + kQStages, K_FULL = Q_FREE + kQStages,
-  V_FULL = K_FULL + kKStages, V_TMA = V_FULL + kVStages, S_FULL = V_TMA + 1,
-  P_READY = S_FULL + kGroups, PV_DONE = P_READY + kGroups, TURN = PV_DONE + kGroups, O_FREE = TURN + kGroups,
-  PARTS = O_FREE + 1, MERGE = PARTS + kGroups, kBars = MERGE + kGroups
+  FR_FULL = 0, FR_FREE = FR_FULL + kRing,
+  Q_FULL = FR_FREE + kRing, Q_FREE = Q_FULL + kQStages,
+  S_GO = Q_FREE + kQStages,             // K(T) has landed, the buffer for S(T) is used up
+  GO = S_GO + kGroups,                  // P(T) complete, V(T) landed
+  V_TMA = GO + kGroups,                 // a value tile that needs touching up has landed
+  S_FULL = V_TMA + 1, PV_DONE = S_FULL + kGroups,
+  TURN = PV_DONE + kGroups,             // tile T's probabilities are final
+  REF = TURN + kGroups,                 // a piece's first tile has set the reference
+  O_FREE = REF + kGroups, PARTS = O_FREE + 1, MERGE = PARTS + kGroups, kBars = MERGE + kGroups
 };
-static_assert(kBars * 8 <= 320, "barrier area");
+static_assert(kBars * 8 <= 288, "barrier area");
 static_assert(kVStages == kGroups, "a V stage is free when the value product of its group has completed");
 
 // maximum that keeps NaN
@@ -69,30 +75,16 @@ __device__ __forceinline__ float max3_nan(float a, float b, float c) {
   asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
-// two probabilities -> packed bf16, rounded to nearest (ties away); inputs are non-negative and finite or NaN (a row
-// with a NaN is recognised by its maximum)
-__device__ __forceinline__ uint32_t round_pair(float lo, float hi) {
-  uint32_t r;
-  asm("prmt.b32 %0, %1, %2, 0x7632;" : "=r"(r) : "r"(__float_as_uint(lo) + 0x8000u), "r"(__float_as_uint(hi) + 0x8000u));
-  return r;
-}
-
 __device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity) {
   uint32_t done;
   asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
                : "=r"(done) : "r"(bar), "r"(parity) : "memory");
   return done != 0;
 }
-__device__ __forceinline__ bool test_bar(uint32_t bar, uint32_t parity) {
-  uint32_t done;
-  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-               : "=r"(done) : "r"(bar), "r"(parity) : "memory");
-  return done != 0;
-}
 // Bounded; gives up as soon as another role has failed.
 __device__ __forceinline__ bool wait_bar(uint32_t bar, uint32_t parity, volatile uint32_t* fail) {
 #pragma unroll 1
-  for (uint32_t i = 0; i < kSpinLimit; ++i) {
+  for (uint32_t i = 0; i < kWaitPolls; ++i) {
     if (try_wait(bar, parity)) return true;
     if ((i & 63u) == 63u && *fail) return false;
   }
@@ -102,8 +94,22 @@ __device__ __forceinline__ bool wait_bar(uint32_t bar, uint32_t parity, volatile
 // For copies in flight at the end: bounded, whatever has failed.
 __device__ __forceinline__ void drain_bar(uint32_t bar, uint32_t parity) {
 #pragma unroll 1
-  for (uint32_t i = 0; i < kSpinLimit; ++i)
+  for (uint32_t i = 0; i < kDrainPolls; ++i)
     if (try_wait(bar, parity)) return;
+}
+
+// 16 columns of this thread's lane.
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, float* v) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]),
+        "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
+      : "r"(taddr) : "memory");
+  tmem_wait_ld();
+#pragma unroll
+  for (int i = 0; i < 16; i += 8)
+    asm volatile("" : "+f"(v[i]), "+f"(v[i + 1]), "+f"(v[i + 2]), "+f"(v[i + 3]), "+f"(v[i + 4]), "+f"(v[i + 5]),
+                 "+f"(v[i + 6]), "+f"(v[i + 7]));
 }
 
 // Pins registers that tcgen05.ld filled behind the wait for it.
@@ -227,32 +233,34 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
   volatile uint32_t* s_tmem = reinterpret_cast<volatile uint32_t*>(smem_raw + L::kMisc);
   volatile uint32_t* s_fail = s_tmem + 1;
   volatile uint32_t* s_merge = s_tmem + 2;
-  volatile uint32_t* s_scrub = s_merge + kGroups;            // per ring entry
+  volatile uint32_t* s_scrub = s_merge + kGroups;            // [4]: number of the piece + 1 whose value tile was touched
   float* x_l = reinterpret_cast<float*>(smem_raw + L::kSum);
   Piece* ring = reinterpret_cast<Piece*>(smem_raw + L::kPieces);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int G = p.cfg.G;
 
   if (tid == 0) {
-    for (int i = 0; i < kRing; ++i) { mbar_init(bar(FR_FULL + i), 1); mbar_init(bar(FR_FREE + i), 2 + 4 * kGroups); }
+    for (int i = 0; i < kRing; ++i) { mbar_init(bar(FR_FULL + i), 1); mbar_init(bar(FR_FREE + i), 3 + 4 * kGroups); }
     for (int i = 0; i < kQStages; ++i) { mbar_init(bar(Q_FULL + i), 1); mbar_init(bar(Q_FREE + i), 4); }
-    for (int i = 0; i < kKStages; ++i) mbar_init(bar(K_FULL + i), 1);
-    for (int i = 0; i < kVStages; ++i) mbar_init(bar(V_FULL + i), 1);
     mbar_init(bar(V_TMA), 1);
     for (int i = 0; i < kGroups; ++i) {
+      mbar_init(bar(S_GO + i), 1 + 1);
+      mbar_init(bar(GO + i), 4 + 1);
       mbar_init(bar(S_FULL + i), 1);
-      mbar_init(bar(P_READY + i), 4);
       mbar_init(bar(PV_DONE + i), 1);
       mbar_init(bar(TURN + i), 4);
+      mbar_init(bar(REF + i), 4);
       mbar_init(bar(PARTS + i), 4);
       mbar_init(bar(MERGE + i), 1);
     }
     mbar_init(bar(O_FREE), 4);
+    for (int i = 0; i < 4; ++i) s_scrub[i] = 0;
     *s_fail = (base & 1023u) != 0;          // (never seen: the declaration asks for 1024 bytes)
     if (*s_fail) atomicMax(p.d_status, (int)CHECK_SMEM_ALIGNMENT);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    for (int i = 0; i < kGroups; ++i) mbar_arrive(bar(S_GO + i));      // (every score buffer starts out free)
   }
-  if (warp == kWarpMma) {
+  if (warp == kWarpS) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(base + L::kMisc), "r"(kTmemCols)
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -267,10 +275,10 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
 
   auto wait = [&](int i, uint32_t phase) { return wait_bar(bar(i), phase & 1u, s_fail); };
 
-  if (warp >= kWarpMma) {
+  if (warp >= kWarpS) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOther));
     if (warp == kWarpK) {
-      // ================= plan, Q and K =================
+      // ================= plan and K =================
       Walker w;
       w.init(p.seqs, p.cfg, &plan, chunk);
       Piece pc;
@@ -301,101 +309,86 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         for (int t = pc.tile0; t < pc.tile1; ++t, ++T) {
           int next = 0;
           if constexpr (kPaged) { if (t + 1 < pc.tile1) next = tile_page(p, pc, t + 1, &bad); }
-          const uint32_t st = T % kKStages;
-          if (T >= kKStages) wait(S_FULL + (T - kKStages) % kGroups, (T - kKStages) / kGroups);   // its score product is done
-          load_tile<kD, kPaged>(p, &tmK, pc, t, base + L::kK + st * L::kTile, bar(K_FULL + st), page);
+          if (T >= kKStages) wait(S_FULL + (T - kKStages) % kGroups, (T - kKStages) / kGroups);     // its score product is done
+          load_tile<kD, kPaged>(p, &tmK, pc, t, base + L::kK + (T % kKStages) * L::kTile, bar(S_GO + T % kGroups), page);
           page = next;
         }
         ++f;
       }
       if (__any_sync(0xffffffffu, bad) && lane == 0) atomicMax(p.d_status, (int)CHECK_PAGE_RANGE);
-      for (uint32_t i = 0; i < kKStages; ++i)                     // no copy of this CTA outlives it
-        if (T > i) drain_bar(bar(K_FULL + (T - 1 - i) % kKStages), ((T - 1 - i) / kKStages) & 1u);
+      // no copy of this CTA outlives it: the products have waited for them, unless something failed
+#pragma unroll 1
+      for (uint32_t i = 0; i < kGroups; ++i)
+        if (T > i) drain_bar(bar(S_GO + (T - 1 - i) % kGroups), ((T - 1 - i) / kGroups) & 1u);
+#pragma unroll 1
       for (uint32_t i = 0; i < kQStages; ++i)
         if (f > i) drain_bar(bar(Q_FULL + (f - 1 - i) % kQStages), ((f - 1 - i) / kQStages) & 1u);
-    } else if (warp == kWarpMma) {
-      // ================= products: S = Q K^T, O += P V =================
-      // One thread issues both, so the pipe runs them in its order: the scores of tile T + 3 may overwrite the buffer of
-      // T's probabilities right behind the product that reads them.  Neither kind waits for the other's inputs.
-      constexpr uint32_t kIdescS = instr_desc(kBM, kBN, false), kIdescO = instr_desc(kBM, kD, true);
+    } else if (warp == kWarpS) {
+      // ================= S = Q K^T =================
+      // Two warps issue, one the score products and one the value products: a poll next to running products costs 150-300
+      // cycles, which the other warp's products cover.  One barrier collects everything a product needs.
+      constexpr uint32_t kIdesc = instr_desc(kBM, kBN, false);
       const uint64_t dQ0 = smem_desc(base + L::kQ, 16, 1024), dK0 = smem_desc(base + L::kK, 16, 1024);
-      const uint64_t dV0 = smem_desc(base + L::kV, kBN * 128, 1024);
-      uint32_t fs = 0, Ts = 0, fp = 0, Tp = 0;             // pieces and tiles of the score and of the value products
-      int s_left = 0, p_tile = 0, p_first = 0, p_end = 0, p_seen = 0;
-      bool s_query = false, s_done = false, p_output = false, p_have = false;
-      uint32_t idle = 0;
-      if (lane == 0) while (!(s_done && Tp == Ts)) {
-        bool moved = false;
-        // value product of tile Tp
-        if (Tp < Ts) {
-          if (!p_have) {
-            const Piece& pc = ring[fp % kRing];            // (the score side has seen it arrive)
-            p_first = p_tile = pc.tile0;
-            p_end = pc.tile1;
-            p_seen = pc.seen;
-            p_have = true;
-            p_output = fp == 0;
-            mbar_arrive(bar(FR_FREE + fp % kRing));
-          }
-          const uint32_t g = Tp % kGroups;
-          if (!p_output) p_output = test_bar(bar(O_FREE), (fp - 1) & 1u);
-          if (p_output && test_bar(bar(P_READY + g), (Tp / kGroups) & 1u) && test_bar(bar(V_FULL + g), (Tp / kGroups) & 1u)) {
-            tc_fence_after();
-            {
-              const uint64_t dV = dV0 + (uint64_t)(g * (L::kTile >> 4));
-              const int slots = p_seen - p_tile * kBN;     // steps of 16 slots that some row sees
+      uint32_t f = 0, T = 0;
+      while (true) {
+        if (!wait(FR_FULL + f % kRing, f / kRing)) break;
+        const int t0 = ring[f % kRing].tile0, t1 = ring[f % kRing].tile1;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(FR_FREE + f % kRing));
+        if (t0 < 0) break;
+        wait(Q_FULL + f % kQStages, f / kQStages);
+        const uint64_t dQ = dQ0 + (uint64_t)((f % kQStages) * (L::kTile >> 4));
+#pragma unroll 1
+        for (int t = t0; t < t1; ++t, ++T) {
+          wait(S_GO + T % kGroups, T / kGroups);
+          tc_fence_after();
+          __syncwarp();
+          if (lane == 0) {
+            const uint64_t dK = dK0 + (uint64_t)((T % kKStages) * (L::kTile >> 4));
 #pragma unroll
-              for (int ks = 0; ks < kBN / 16; ++ks)
-                if (ks == 0 || ks * 16 < slots)
-                  mma_ts(tmem + kColO, tmem + g * kBN + ks * 8, dV + ((ks * 16 * 128) >> 4), kIdescO, (p_tile > p_first) | (ks > 0));
-              mma_commit(bar(PV_DONE + g));
+            for (int ks = 0; ks < kD / 16; ++ks) {
+              const uint32_t aoff = ((ks >> 2) * (kBM * 128) + (ks & 3) * 32) >> 4;
+              const uint32_t boff = ((ks >> 2) * (kBN * 128) + (ks & 3) * 32) >> 4;
+              mma_ss(tmem + (T % kGroups) * kBN, dQ + aoff, dK + boff, kIdesc, ks > 0);
             }
-            ++Tp;
-            if (++p_tile == p_end) {
-              p_have = false;
-              ++fp;
-            }
-            moved = true;
+            mma_commit(bar(S_FULL + T % kGroups));
           }
+          __syncwarp();
         }
-        // score product of tile Ts
-        if (!s_done && Ts < Tp + kGroups) {
-          if (s_left == 0 && test_bar(bar(FR_FULL + fs % kRing), (fs / kRing) & 1u)) {
-            const Piece& pc = ring[fs % kRing];
-            if (pc.tile0 < 0) {
-              s_done = true;
-              moved = true;
-            } else {
-              s_left = pc.tile1 - pc.tile0;
-              s_query = false;
-            }
-          }
-          if (s_left > 0 && !s_query) s_query = test_bar(bar(Q_FULL + fs % kQStages), (fs / kQStages) & 1u);
-          const uint32_t st = Ts % kKStages;
-          if (s_left > 0 && s_query && test_bar(bar(K_FULL + st), (Ts / kKStages) & 1u)) {
-            tc_fence_after();
-            {
-              const uint64_t dQ = dQ0 + (uint64_t)((fs % kQStages) * (L::kTile >> 4)), dK = dK0 + (uint64_t)(st * (L::kTile >> 4));
-#pragma unroll
-              for (int ks = 0; ks < kD / 16; ++ks) {
-                const uint32_t aoff = ((ks >> 2) * (kBM * 128) + (ks & 3) * 32) >> 4;
-                const uint32_t boff = ((ks >> 2) * (kBN * 128) + (ks & 3) * 32) >> 4;
-                mma_ss(tmem + (Ts % kGroups) * kBN, dQ + aoff, dK + boff, kIdescS, ks > 0);
-              }
-              mma_commit(bar(S_FULL + Ts % kGroups));
-            }
-            ++Ts;
-            if (--s_left == 0) ++fs;
-            moved = true;
-          }
-        }
-        idle = moved ? 0 : idle + 1;
-        if ((idle & 63u) == 63u) {
-          if (*s_fail) break;
-          if (idle > kIdleLimit) *s_fail = 1;
-        }
+        ++f;
       }
-      __syncwarp();
+    } else if (warp == kWarpPV) {
+      // ================= O += P V =================
+      constexpr uint32_t kIdesc = instr_desc(kBM, kD, true);
+      const uint64_t dV0 = smem_desc(base + L::kV, kBN * 128, 1024);
+      uint32_t f = 0, T = 0;
+      while (true) {
+        if (!wait(FR_FULL + f % kRing, f / kRing)) break;
+        const int t0 = ring[f % kRing].tile0, t1 = ring[f % kRing].tile1, seen = ring[f % kRing].seen;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(FR_FREE + f % kRing));
+        if (t0 < 0) break;
+        if (f > 0) wait(O_FREE, f - 1);
+#pragma unroll 1
+        for (int t = t0; t < t1; ++t, ++T) {
+          const uint32_t g = T % kGroups;
+          wait(GO + g, T / kGroups);
+          tc_fence_after();
+          __syncwarp();
+          if (lane == 0) {
+            const uint64_t dV = dV0 + (uint64_t)(g * (L::kTile >> 4));
+            const int slots = seen - t * kBN;              // steps of 16 slots that some row sees
+#pragma unroll
+            for (int ks = 0; ks < kBN / 16; ++ks)
+              if (ks == 0 || ks * 16 < slots)
+                mma_ts(tmem + kColO, tmem + g * kBN + ks * 8, dV + ((ks * 16 * 128) >> 4), kIdesc, (t > t0) | (ks > 0));
+            mma_commit(bar(S_GO + g));
+            mma_commit(bar(PV_DONE + g));
+          }
+          __syncwarp();
+        }
+        ++f;
+      }
     } else if (warp == kWarpV) {
       uint32_t f = 0, T = 0, partial_tiles = 0;
       while (true) {
@@ -413,8 +406,6 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
           bool bad = false;                                        // (reported by the K loader)
           if constexpr (kPaged) page = tile_page(p, pc, pc.tile0, &bad);
           const int zone0 = max(pc.seen0, pc.tile0 * kBN), zone1 = min(pc.seen, pc.tile1 * kBN);
-          if (lane == 0) s_scrub[f % kRing] = 0;
-          __syncwarp();
 #pragma unroll 1
           for (int t = pc.tile0; t < pc.tile1; ++t, ++T) {
             int next = 0;
@@ -426,7 +417,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
             const int r0 = max(zone0 - t * kBN, 0), r1 = min(zone1 - t * kBN, kBN);
             const bool look = r0 < r1;
             if (!clear && !look) {
-              load_tile<kD, kPaged>(p, &tmV, pc, t, dst, bar(V_FULL + st), page);
+              load_tile<kD, kPaged>(p, &tmV, pc, t, dst, bar(GO + st), page);
             } else {
               load_tile<kD, kPaged>(p, &tmV, pc, t, dst, bar(V_TMA), page);
               wait(V_TMA, partial_tiles++);
@@ -440,7 +431,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
                 }
               }
               if (look && any_nonfinite<kD>(dst, r0, r1)) {
-                if (lane == 0) s_scrub[f % kRing] = 1;
+                if (lane == 0) s_scrub[f % 4] = f + 1;   // (this warp is at most three pieces ahead of the epilogues)
 #pragma unroll 1
                 for (int i = lane; i < (r1 - r0) * (kD / 2); i += 32) {
                   const int r = r0 + i / (kD / 2), w = i % (kD / 2);
@@ -454,7 +445,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
               }
               fence_proxy_async();
               __syncwarp();
-              if (lane == 0) mbar_arrive(bar(V_FULL + st));
+              if (lane == 0) mbar_arrive(bar(GO + st));
               __syncwarp();
             }
             page = next;
@@ -462,8 +453,9 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         }
         ++f;
       }
-        for (uint32_t i = 0; i < kVStages; ++i)
-          if (T > i) drain_bar(bar(V_FULL + (T - 1 - i) % kVStages), ((T - 1 - i) / kVStages) & 1u);
+#pragma unroll 1
+      for (uint32_t i = 0; i < kVStages; ++i)
+        if (T > i) drain_bar(bar(GO + (T - 1 - i) % kVStages), ((T - 1 - i) / kVStages) & 1u);
     }
   } else {
     // ================= softmax =================
@@ -489,11 +481,10 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
       sq.first = pc.first; sq.n = pc.n; sq.base = pc.base;
       // rows without a token follow the last one: their results are dropped
       const int vis = visible(p.seqs, sq, min(t_seq, min((pc.r + 1) * p.cfg.tokens, pc.n) - 1));
-      float* ref_row = ref_max + row;
-      float* l_row = x_l + (f & 1u) * 256 + row;         // [0]: of the tile before the last, [128]: of the one before that
+      float* ref_row = ref_max + (f % kGroups) * 128 + row;
+      float* l_row = x_l + row;                           // [0]: of the tile before the last, [128]: of the one before that
       float m = -INFINITY, l = 0.f;
-      float m_other = -INFINITY;                         // what the other groups' denominators refer to
-      bool poison = false;
+      bool poison = false, ref_known = false;
 #pragma unroll 1
       for (int t = pc.tile0 + (int)((kGroups + g - T % kGroups) % kGroups); t < pc.tile1; t += kGroups) {
         const uint32_t Tt = T + (uint32_t)(t - pc.tile0);
@@ -527,26 +518,27 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         }
         const float cand = max3_nan(max3_nan(mx0, mx1, mx2), mx3, mx3) * sl2;
         poison |= !(cand < INFINITY);                    // NaN or +infinity among the row's scores
-        // the reference maximum, handed on from tile to tile
-        if (Tt > 0) wait(TURN + g, (Tt - 1) / kGroups);
+        // The piece's first tile sets the row's reference; the others use it as it stands.  Whether a tile before this one
+        // has moved it meanwhile is looked at when the probabilities are done.
         const bool first = t == pc.tile0;
-        const float ref = first ? -INFINITY : *ref_row;
-        const bool grow = cand - ref > kGrow || (ref == -INFINITY && cand > -INFINITY);
-        const float ref_new = grow ? cand : ref;
-        if (grow || first) *ref_row = ref_new;
-        m_other = ref;
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(TURN + (g + 1) % kGroups));
-        if (m != ref_new) {                              // (also when the other group moved it)
-          l = l > 0.f ? l * fast_exp2(m - ref_new) : l;
-          m = ref_new;
-        }
-        if (!first && __any_sync(0xffffffffu, grow)) {
-          wait(PV_DONE + (g + kGroups - 1) % kGroups, (Tt - 1) / kGroups);   // O holds everything before this tile, at the old reference
+        if (!first && !ref_known) wait(REF + f % kGroups, f / kGroups);
+        ref_known = true;
+        float ref = first ? cand : *ref_row;
+        bool settled = first;
+        if (first) {
+          *ref_row = ref;
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(REF + f % kGroups));
+        } else if (__any_sync(0xffffffffu, cand - ref > kGrow || (ref == -INFINITY && cand > -INFINITY))) {
+          // some row needs a larger reference: O has to follow, so everything before this tile is finished first
+          wait(TURN + (Tt - 1) % kGroups, (Tt - 1) / kGroups);
+          wait(PV_DONE + (Tt - 1) % kGroups, (Tt - 1) / kGroups);
           tc_fence_after();
-          const float corr = grow ? fast_exp2(ref - ref_new) : 1.0f;
-          // (a denominator that was handed over already and whose reader would not notice this step)
-          if (t + 2 == pc.tile1 && t > pc.tile0 && l_row[128] > 0.f) l_row[128] *= corr;
+          ref = *ref_row;
+          const bool grow = cand - ref > kGrow || (ref == -INFINITY && cand > -INFINITY);
+          const float corr = grow ? fast_exp2(ref - cand) : 1.0f;
+          if (grow) *ref_row = cand;
+          if (grow) ref = cand;
 #pragma unroll 1
           for (int c0 = 0; c0 < kD; c0 += 32) {
             float o[32];
@@ -555,6 +547,14 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
             for (int i = 0; i < 32; ++i) o[i] *= corr;
             tmem_st32(tO + c0, o);
           }
+          // denominators that other groups have handed over already follow too
+          if (t + 2 >= pc.tile1 && pc.tile1 - pc.tile0 > 2 && l_row[128] > 0.f) l_row[128] *= corr;
+          if (t + 1 == pc.tile1 && l_row[0] > 0.f) l_row[0] *= corr;
+          settled = true;
+        }
+        if (m != ref) {
+          l = l > 0.f ? l * fast_exp2(m - ref) : l;
+          m = ref;
         }
         const float mu = m == -INFINITY ? 0.f : m;
         // second pass: probabilities, 32 columns at a time, the next ones under way meanwhile.  (No row sees slots behind
@@ -575,8 +575,8 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
             sum1 += x[i + 1];
             sum2 += x[i + 2];
             sum3 += x[i + 3];
-            pk[i / 2] = round_pair(x[i], x[i + 1]);
-            pk[i / 2 + 1] = round_pair(x[i + 2], x[i + 3]);
+            pk[i / 2] = pack_bf16(x[i], x[i + 1]);
+            pk[i / 2 + 1] = pack_bf16(x[i + 2], x[i + 3]);
           }
           tmem_st16(tS + (c0 >> 1), pk);
         };
@@ -595,27 +595,55 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
           exponentials(xb, c0 + 32);
         }
         l += (sum0 + sum1) + (sum2 + sum3);
-        if (t + 2 == pc.tile1) l_row[0] = poison ? __int_as_float(0x7fffffff) : l;
-        if (t + 3 == pc.tile1) l_row[128] = poison ? __int_as_float(0x7fffffff) : l;
+        if (Tt > 0 && !settled) {
+          wait(TURN + (Tt - 1) % kGroups, (Tt - 1) / kGroups);
+          const float now = *ref_row;
+          if (__any_sync(0xffffffffu, now != m)) {       // moved by a tile before this one: follow
+            tmem_wait_st();
+            const float corr = now != m ? fast_exp2(m - now) : 1.0f;
+#pragma unroll 1
+            for (int c0 = 0; c0 < kBN; c0 += 32) {
+              float q[16];
+              tmem_ld16(tS + (c0 >> 1), q);
+              uint32_t pk[16];
+#pragma unroll
+              for (int i = 0; i < 16; ++i)
+                pk[i] = pack_bf16(bf16_lo(__float_as_uint(q[i])) * corr, bf16_hi(__float_as_uint(q[i])) * corr);
+              tmem_st16(tS + (c0 >> 1), pk);
+            }
+            if (now != m) {
+              l = l > 0.f ? l * corr : l;
+              m = now;
+            }
+          }
+        } else if (Tt > 0 && first) {
+          wait(TURN + (Tt - 1) % kGroups, (Tt - 1) / kGroups);
+        }
+        if (t + 2 == pc.tile1 || t + 3 == pc.tile1) {    // this group's last tile of the piece, but not the piece's last
+          if (f > 0) wait(O_FREE, f - 1);                // (the piece before has read its own)
+          l_row[t + 2 == pc.tile1 ? 0 : 128] = poison ? __int_as_float(0x7fffffff) : l;
+        }
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(bar(P_READY + g));
+        if (lane == 0) {
+          mbar_arrive(bar(TURN + g));
+          mbar_arrive(bar(GO + g));
+        }
       }
       T = Tend;
       if (finishes) {
         // ---- the piece's result ----
         if (poison) l = __int_as_float(0x7fffffff);
-        const float mu = m == -INFINITY ? 0.f : m;       // the last tile's group holds the final reference
         wait(PV_DONE + g, (T - 1) / kGroups);
         tc_fence_after();
 #pragma unroll
         for (int k = 0; k < kGroups - 1; ++k) {          // (their products come before this tile's)
           const float l_other = pc.tile1 - pc.tile0 > k + 1 ? l_row[k * 128] : 0.f;
-          if (l_other != 0.f) l += l_other * fast_exp2(m_other - mu);
+          if (l_other != 0.f) l += l_other;              // (at the last tile's reference)
         }
         const bool store = valid && *s_fail == 0;
-        const bool scrubbed = s_scrub[f % kRing] != 0;
+        const bool scrubbed = s_scrub[f % 4] == f + 1;
         const int tok = pc.first + t_seq, hq = pc.h * G + member;
         const uint32_t sO = base + L::kQ + (f % kQStages) * L::kTile;       // over the piece's Q tile: no product reads it now
         // 32 columns of the row at a time: a whole item is normalised into shared memory, a piece of a cut item goes to the
@@ -736,7 +764,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
   __syncthreads();
   pdl_launch_dependents();
   if (tid == 0 && *s_fail) atomicMax(p.d_status, (int)CHECK_WAIT_TIMEOUT);
-  if (warp == kWarpMma) {
+  if (warp == kWarpS) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
   }
