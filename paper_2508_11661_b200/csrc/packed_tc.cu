@@ -112,6 +112,14 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, float* v) {
                  "+f"(v[i + 6]), "+f"(v[i + 7]));
 }
 
+// Scores at and behind `limit` become -infinity.
+template <int kN>
+__device__ __forceinline__ void mask_row(float* v, int limit) {
+#pragma unroll
+  for (int i = 0; i < kN; ++i)
+    if (i >= limit) v[i] = -INFINITY;
+}
+
 // Pins registers that tcgen05.ld filled behind the wait for it.
 template <int kN>
 __device__ __forceinline__ void settle(float* v) {
@@ -127,6 +135,7 @@ struct Params {
   Pages pages;                 // table, width, n_pages, shift; paged calls
   Rows Q, K, V, O;             // K, V: packed rows, or the pools' data pointers
   int paged, box;              // slots per TMA box
+  int store_tokens;            // tokens of a warp's 32 rows, 0: rows are not whole tokens
   float scale;
   float* lse;
   float4* part_o;              // [slot][d/4][128]
@@ -144,19 +153,21 @@ __device__ __forceinline__ const __nv_bfloat16* kv_row(const Params& p, const Ro
   return base + (size_t)(pc.first + j) * rows.ts + (size_t)pc.h * rows.hs;
 }
 
-// 32 normalised columns of a row into a 128-byte-swizzled tile, from 16-byte piece `piece` on.
-__device__ __forceinline__ void stage_row(const float* o, float inv, bool empty, uint32_t tile, int row, int piece) {
+// 2 kN packed columns of a row into a 128-byte-swizzled tile, from 16-byte piece `piece` on.
+template <int kN>
+__device__ __forceinline__ void stage_row(const uint32_t* v, uint32_t tile, int row, int piece) {
 #pragma unroll
-  for (int i = 0; i < 32; i += 8) {
-    uint4 v;
-    v.x = pack_bf16(o[i] * inv, o[i + 1] * inv);
-    v.y = pack_bf16(o[i + 2] * inv, o[i + 3] * inv);
-    v.z = pack_bf16(o[i + 4] * inv, o[i + 5] * inv);
-    v.w = pack_bf16(o[i + 6] * inv, o[i + 7] * inv);
-    if (empty) v = make_uint4(0, 0, 0, 0);
-    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(tile + blk_off(row, piece + (i >> 3))), "r"(v.x), "r"(v.y),
-                 "r"(v.z), "r"(v.w) : "memory");
-  }
+  for (int i = 0; i < kN; i += 4)
+    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(tile + blk_off(row, piece + (i >> 2))), "r"(v[i]), "r"(v[i + 1]),
+                 "r"(v[i + 2]), "r"(v[i + 3]) : "memory");
+}
+__device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, int x, int y, int z, uint32_t src) {
+  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(map), "r"(x), "r"(y),
+               "r"(z), "r"(src) : "memory");
+}
+__device__ __forceinline__ void bulk_commit_and_wait_read() {
+  asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+  asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
 }
 
 // Loads the boxes of one key or value tile; `pages` holds this tile's page numbers in the lanes.
@@ -221,7 +232,8 @@ __device__ __forceinline__ bool any_nonfinite(uint32_t tile, int r0, int r1) {
 template <int kD, bool kPaged>
 __global__ void __launch_bounds__(ptc::kThreads, 1)
 packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
-                 const __grid_constant__ CUtensorMap tmV, const __grid_constant__ ptc::Params p) {
+                 const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmO,
+                 const __grid_constant__ ptc::Params p) {
   using namespace ptc;
   using L = Smem<kD>;
   extern __shared__ __align__(1024) unsigned char smem_raw[];
@@ -490,26 +502,21 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         const uint32_t Tt = T + (uint32_t)(t - pc.tile0);
         wait(S_FULL + g, Tt / kGroups);
         tc_fence_after();
-        // first pass over the scores: their maximum (64 columns at a time; the loops stay rolled so that the whole
-        // softmax fits the instruction cache next to the other roles' code)
+        // first pass over the scores: their maximum.  (The loops stay rolled: the code of a tile has to fit the schedulers'
+        // instruction caches, straight-line code that does not runs at 3-5 cycles an instruction.)
         const int limit = vis - t * kBN;
         const int width = min(pc.seen - t * kBN, kBN);   // slots that some row sees
         const bool masked = __any_sync(0xffffffffu, limit < kBN);
         float mx0 = -INFINITY, mx1 = -INFINITY, mx2 = -INFINITY, mx3 = -INFINITY;
 #pragma unroll 1
-        for (int c0 = 0; c0 < kBN; c0 += 64) {
-          float sv[64];
+        for (int c0 = 0; c0 < kBN; c0 += 32) {
+          float sv[32];
           tmem_ld32_nowait(tS + c0, sv);
-          tmem_ld32_nowait(tS + c0 + 32, sv + 32);
           tmem_wait_ld();
-          settle<64>(sv);
-          if (masked) {
+          settle<32>(sv);
+          if (masked) mask_row<32>(sv, limit - c0);
 #pragma unroll
-            for (int i = 0; i < 64; ++i)
-              if (c0 + i >= limit) sv[i] = -INFINITY;
-          }
-#pragma unroll
-          for (int i = 0; i < 64; i += 8) {
+          for (int i = 0; i < 32; i += 8) {
             mx0 = max3_nan(mx0, sv[i], sv[i + 1]);
             mx1 = max3_nan(mx1, sv[i + 2], sv[i + 3]);
             mx2 = max3_nan(mx2, sv[i + 4], sv[i + 5]);
@@ -557,15 +564,15 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
           m = ref;
         }
         const float mu = m == -INFINITY ? 0.f : m;
-        // second pass: probabilities, 32 columns at a time, the next ones under way meanwhile.  (No row sees slots behind
-        // `width`: the value product skips them.)
+        // second pass: probabilities, 32 columns at a time.  (No row sees slots behind `width`: the value product skips them.)
         float sum0 = 0.f, sum1 = 0.f, sum2 = 0.f, sum3 = 0.f;
-        auto exponentials = [&](float* x, int c0) {
-          if (masked) {
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-              if (c0 + i >= limit) x[i] = -INFINITY;
-          }
+#pragma unroll 1
+        for (int c0 = 0; c0 < max(width, 1); c0 += 32) {
+          float x[32];
+          tmem_ld32_nowait(tS + c0, x);
+          tmem_wait_ld();
+          settle<32>(x);
+          if (masked) mask_row<32>(x, limit - c0);
           uint32_t pk[16];
 #pragma unroll
           for (int i = 0; i < 32; i += 4) {
@@ -579,20 +586,6 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
             pk[i / 2 + 1] = pack_bf16(x[i + 2], x[i + 3]);
           }
           tmem_st16(tS + (c0 >> 1), pk);
-        };
-        float xa[32], xb[32];
-        tmem_ld32_nowait(tS, xa);
-#pragma unroll 1
-        for (int c0 = 0; c0 < max(width, 1); c0 += 64) {
-          tmem_wait_ld();
-          settle<32>(xa);
-          if (c0 + 32 < width) tmem_ld32_nowait(tS + c0 + 32, xb);
-          exponentials(xa, c0);
-          if (c0 + 32 >= width) break;
-          tmem_wait_ld();
-          settle<32>(xb);
-          if (c0 + 64 < width) tmem_ld32_nowait(tS + c0 + 64, xa);
-          exponentials(xb, c0 + 32);
         }
         l += (sum0 + sum1) + (sum2 + sum3);
         if (Tt > 0 && !settled) {
@@ -646,33 +639,33 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         const bool scrubbed = s_scrub[f % 4] == f + 1;
         const int tok = pc.first + t_seq, hq = pc.h * G + member;
         const uint32_t sO = base + L::kQ + (f % kQStages) * L::kTile;       // over the piece's Q tile: no product reads it now
-        // 32 columns of the row at a time: a whole item is normalised into shared memory, a piece of a cut item goes to the
-        // workspace as it is
+        // a whole item is normalised into shared memory, a piece of a cut item goes to the workspace as it is
         const float inv = l == 0.f ? 0.f : 1.0f / l;
 #pragma unroll 1
-        for (int c0 = 0; c0 < kD; c0 += 32) {
-          float o[32];
-          tmem_ld32_nowait(tO + c0, o);
-          tmem_wait_ld();
-          settle<32>(o);
+        for (int c0 = 0; c0 < kD; c0 += 16) {
+          float o[16];
+          tmem_ld16(tO + c0, o);
           if (scrubbed && store) {
             // infinities and NaN that were cleared from the value tile: back into the rows that see them
 #pragma unroll 1
             for (int j = max(pc.seen0, pc.tile0 * kBN); j < min(vis, pc.tile1 * kBN); ++j) {
               const __nv_bfloat16* v = kv_row(p, p.V, pc, j, kD) + c0;
 #pragma unroll
-              for (int i = 0; i < 32; ++i) {
+              for (int i = 0; i < 16; ++i) {
                 const float y = __bfloat162float(v[i]);
                 if (!(fabsf(y) < INFINITY)) o[i] += y;
               }
             }
           }
           if (pc.slot < 0) {
-            stage_row(o, inv, l == 0.f, sO + (c0 >> 6) * (kBM * 128), row, (c0 & 63) >> 3);
+            uint32_t pk[8];
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) pk[i / 2] = l == 0.f ? 0u : pack_bf16(o[i] * inv, o[i + 1] * inv);
+            stage_row<8>(pk, sO + (c0 >> 6) * (kBM * 128), row, (c0 & 63) >> 3);
           } else {
             float4* po = p.part_o + ((size_t)pc.slot * (kD / 4) + c0 / 4) * 128 + row;
 #pragma unroll
-            for (int i = 0; i < 32; i += 4) po[(i >> 2) * 128] = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+            for (int i = 0; i < 16; i += 4) po[(i >> 2) * 128] = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
           }
         }
         tc_fence_before();
@@ -731,26 +724,39 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
                   }
                 }
               }
-              stage_row(o, inv_all, l == 0.f, sO + (c0 >> 6) * (kBM * 128), row, (c0 & 63) >> 3);
+              uint32_t pk[16];
+#pragma unroll
+              for (int i = 0; i < 32; i += 2) pk[i / 2] = l == 0.f ? 0u : pack_bf16(o[i] * inv_all, o[i + 1] * inv_all);
+              stage_row<16>(pk, sO + (c0 >> 6) * (kBM * 128), row, (c0 & 63) >> 3);
             }
           }
         }
         if (write) {
-          // the rows leave shared memory in whole lines
           if (store && p.lse != nullptr) p.lse[(size_t)tok * p.Hq + hq] = l == 0.f ? -INFINITY : m_out * kLn2 + logf(l);
+          fence_proxy_async();
           __syncwarp();
-          constexpr int kLanes = kD / 8;                 // lanes per row
           const unsigned rows_ok = __ballot_sync(0xffffffffu, store);
-          const long long row_off = (long long)tok * p.O.ts + (long long)hq * p.O.hs;
           const int row0 = (warp & 3) * 32;
-#pragma unroll 4
-          for (int i = 0; i < 32; i += 32 / kLanes) {
-            const int r = i + lane / kLanes, c = lane % kLanes;
-            const long long off = __shfl_sync(0xffffffffu, row_off, r);
-            uint4 v;
-            asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
-                         : "r"(sO + (c >> 3) * (kBM * 128) + blk_off(row0 + r, c & 7)) : "memory");
-            if (rows_ok >> r & 1u) *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.O.data) + off + c * 8) = v;
+          if (p.store_tokens > 0 && rows_ok == 0xffffffffu) {
+            // the warp's 32 rows are whole tokens: out by TMA, straight from the staged tile
+            if (lane == 0) {
+#pragma unroll
+              for (int x = 0; x < kD; x += 64)
+                tma_store_3d(&tmO, x, pc.h * G, tok, sO + (x >> 6) * (kBM * 128) + row0 * 128);
+              bulk_commit_and_wait_read();
+            }
+          } else {
+            constexpr int kLanes = kD / 8;               // lanes per row
+            const long long row_off = (long long)tok * p.O.ts + (long long)hq * p.O.hs;
+#pragma unroll 1
+            for (int i = 0; i < 32; i += 32 / kLanes) {
+              const int r = i + lane / kLanes, c = lane % kLanes;
+              const long long off = __shfl_sync(0xffffffffu, row_off, r);
+              uint4 v;
+              asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                           : "r"(sO + (c >> 3) * (kBM * 128) + blk_off(row0 + r, c & 7)) : "memory");
+              if (rows_ok >> r & 1u) *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.O.data) + off + c * 8) = v;
+            }
           }
           fence_proxy_async();
         }
@@ -786,9 +792,11 @@ inline bool make_map(CUtensorMap* map, const void* data, int d, long long n1, lo
 
 template <int kD, bool kPaged>
 static cudaError_t launch(const Params& p, int ctas, cudaStream_t stream) {
-  CUtensorMap q, k, v;
+  CUtensorMap q, k, v, o;
   const int G = p.cfg.G, Hkv = p.cfg.Hkv;
   if (!make_map(&q, p.Q.data, kD, p.Hq, p.seqs.n_tokens, p.Q.hs, p.Q.ts, G, p.cfg.tokens)) return cudaErrorInvalidValue;
+  if (!make_map(&o, p.O.data, kD, p.Hq, p.seqs.n_tokens, p.O.hs, p.O.ts, G, p.store_tokens > 0 ? p.store_tokens : 1))
+    return cudaErrorInvalidValue;
   if (kPaged) {
     const long long rows = ((long long)p.pages.n_pages * Hkv) << p.pages.shift;
     if (!make_map(&k, p.K.data, kD, rows, 1, kD, rows * kD, p.box, 1) ||
@@ -812,7 +820,7 @@ static cudaError_t launch(const Params& p, int ctas, cudaStream_t stream) {
   attr.val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kern, q, k, v, p);
+  return cudaLaunchKernelEx(&cfg, kern, q, k, v, o, p);
 }
 }  // namespace ptc
 
@@ -829,6 +837,7 @@ cudaError_t launch_packed_tc(const samkv_packed_t& d, const Seqs& seqs, const Kv
   p.cfg.tile = ptc::kBN;
   p.cfg.fixed = 2 * ptc::kBN;
   p.cfg.min_chunk = 6 * ptc::kBN;
+  p.store_tokens = 32 % G == 0 ? 32 / G : 0;
   p.pages = kv.pages;
   p.paged = kv.paged;
   p.Q = Q;
