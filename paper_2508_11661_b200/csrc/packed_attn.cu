@@ -80,12 +80,23 @@ size_t packed_tc_scratch_bytes(int d);
 cudaError_t launch_packed_tc(const samkv_packed_t& d, const Seqs& seqs, const KvSource& kv, const Rows& Q, float scale,
                              const Rows& O, float* lse, const samkv_ctx_impl& h, cudaStream_t stream);
 
+size_t packed_decode_scratch_bytes(int d);
+cudaError_t launch_packed_decode(const samkv_packed_t& d, const Seqs& seqs, const KvSource& kv, const Rows& Q, float scale,
+                                 const Rows& O, float* lse, const samkv_ctx_impl& h, cudaStream_t stream);
+
+// (the decode kernel's pieces are an eighth of the other's)
 size_t packed_scratch_bytes(const samkv_packed_t& p) { return p.dtype == SAMKV_BF16 ? packed_tc_scratch_bytes(p.head_dim) : 0; }
 
 cudaError_t launch_packed_attn(const samkv_packed_t& p, const Seqs& seqs, const KvSource& kv, const Rows& Q, float scale,
                                const Rows& O, float* lse, const samkv_ctx_impl& h, cudaStream_t stream) {
   if (scale <= 0.f) scale = 1.0f / sqrtf((float)p.head_dim);
-  if (p.dtype == SAMKV_BF16) return launch_packed_tc(p, seqs, kv, Q, scale, O, lse, h, stream);
+  if (p.dtype == SAMKV_BF16) {
+    // Up to 16 packed rows per KV head: the decode kernel.  Without a hint, one token per sequence is taken for decode.
+    const int longest = p.max_seq_tokens > 0 ? p.max_seq_tokens : (p.n_tokens <= p.n_seq ? 1 : p.n_tokens);
+    if (kv.paged && (long long)longest * (p.n_q_heads / p.n_kv_heads) <= 16)
+      return launch_packed_decode(p, seqs, kv, Q, scale, O, lse, h, stream);
+    return launch_packed_tc(p, seqs, kv, Q, scale, O, lse, h, stream);
+  }
   const long long blocks = ((long long)p.n_tokens * p.n_q_heads + 3) / 4;
   if (blocks > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
 #define SAMKV_SIMPLE(T, D) \

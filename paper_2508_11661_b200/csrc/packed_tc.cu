@@ -777,34 +777,21 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
 }
 
 namespace ptc {
-inline bool make_map(CUtensorMap* map, const void* data, int d, long long n1, long long n2, long long stride1,
-                     long long stride2, int box1, int box2) {
-  EncodeTiledFn fn = encode_tiled_fn();
-  if (fn == nullptr) return false;
-  const cuuint64_t dims[3] = {(cuuint64_t)d, (cuuint64_t)n1, (cuuint64_t)n2};
-  const cuuint64_t strides[2] = {(cuuint64_t)stride1 * 2, (cuuint64_t)stride2 * 2};
-  const cuuint32_t box[3] = {64, (cuuint32_t)box1, (cuuint32_t)box2};
-  const cuuint32_t estr[3] = {1, 1, 1};
-  return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(data), dims, strides, box, estr,
-            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 template <int kD, bool kPaged>
 static cudaError_t launch(const Params& p, int ctas, cudaStream_t stream) {
   CUtensorMap q, k, v, o;
   const int G = p.cfg.G, Hkv = p.cfg.Hkv;
-  if (!make_map(&q, p.Q.data, kD, p.Hq, p.seqs.n_tokens, p.Q.hs, p.Q.ts, G, p.cfg.tokens)) return cudaErrorInvalidValue;
-  if (!make_map(&o, p.O.data, kD, p.Hq, p.seqs.n_tokens, p.O.hs, p.O.ts, G, p.store_tokens > 0 ? p.store_tokens : 1))
+  if (!make_rows_map(&q, p.Q.data, kD, p.Hq, p.seqs.n_tokens, p.Q.hs, p.Q.ts, G, p.cfg.tokens)) return cudaErrorInvalidValue;
+  if (!make_rows_map(&o, p.O.data, kD, p.Hq, p.seqs.n_tokens, p.O.hs, p.O.ts, G, p.store_tokens > 0 ? p.store_tokens : 1))
     return cudaErrorInvalidValue;
   if (kPaged) {
     const long long rows = ((long long)p.pages.n_pages * Hkv) << p.pages.shift;
-    if (!make_map(&k, p.K.data, kD, rows, 1, kD, rows * kD, p.box, 1) ||
-        !make_map(&v, p.V.data, kD, rows, 1, kD, rows * kD, p.box, 1))
+    if (!make_rows_map(&k, p.K.data, kD, rows, 1, kD, rows * kD, p.box, 1) ||
+        !make_rows_map(&v, p.V.data, kD, rows, 1, kD, rows * kD, p.box, 1))
       return cudaErrorInvalidValue;
   } else {
-    if (!make_map(&k, p.K.data, kD, p.seqs.n_tokens, Hkv, p.K.ts, p.K.hs, kBN, 1) ||
-        !make_map(&v, p.V.data, kD, p.seqs.n_tokens, Hkv, p.V.ts, p.V.hs, kBN, 1))
+    if (!make_rows_map(&k, p.K.data, kD, p.seqs.n_tokens, Hkv, p.K.ts, p.K.hs, kBN, 1) ||
+        !make_rows_map(&v, p.V.data, kD, p.seqs.n_tokens, Hkv, p.V.ts, p.V.hs, kBN, 1))
       return cudaErrorInvalidValue;
   }
   auto kern = packed_tc_kernel<kD, kPaged>;

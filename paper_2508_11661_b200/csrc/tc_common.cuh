@@ -214,5 +214,20 @@ inline bool make_kv_map(CUtensorMap* map, const void* slab, int capacity, int n_
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// bf16 tensor [n2][n1][d] with any strides (in elements) along its outer axes, read or written in boxes of 64 columns x
+// box1 x box2.
+inline bool make_rows_map(CUtensorMap* map, const void* data, int d, long long n1, long long n2, long long stride1,
+                          long long stride2, int box1, int box2) {
+  EncodeTiledFn fn = encode_tiled_fn();
+  if (fn == nullptr) return false;
+  const cuuint64_t dims[3] = {(cuuint64_t)d, (cuuint64_t)n1, (cuuint64_t)n2};
+  const cuuint64_t strides[2] = {(cuuint64_t)stride1 * 2, (cuuint64_t)stride2 * 2};
+  const cuuint32_t box[3] = {64, (cuuint32_t)box1, (cuuint32_t)box2};
+  const cuuint32_t estr[3] = {1, 1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(data), dims, strides, box, estr,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 }  // namespace tc
 }  // namespace samkv
