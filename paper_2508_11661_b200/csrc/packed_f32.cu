@@ -1,0 +1,348 @@
+// Attention of packed sequences over packed rows or over a paged cache, fp32 throughout (tensor cores would round the
+// operands to tf32).
+//
+// Persistent, one CTA of 256 threads per SM, work divided by packed_plan.cuh.  Row tiles of 64 packed rows (16 when every
+// sequence has at most 16 per KV head, so that decode is not spent on rows that do not exist), key tiles of 64 slots,
+// double-buffered with cp.async.  A thread owns kRows/16 rows x 4 slots of the scores and the same rows x d/16 columns of
+// the result: per 64 multiply-adds of the score product it reads 4 + 4 vectors of 16 bytes, so the FMA pipe and shared
+// memory are about level.  The 16 threads of a row agree on maxima and sums by shuffles.
+#include <math.h>
+
+#include "packed_plan.cuh"
+
+namespace samkv {
+namespace pf32 {
+
+constexpr int kBN = 64, kThreads = 256;
+
+template <int kD, int kRows>
+struct Smem {
+  static constexpr int kLd = kD + 4;                     // row stride in floats: rows 16 bytes apart in their banks
+  static constexpr int kPLd = kBN + 4;
+  static constexpr int kTile = kBN * kLd * 4;
+  static constexpr int kQ = 0;
+  static constexpr int kKv = kRows * kLd * 4;            // [2][K, V]; P takes K's place once the scores are done
+  static constexpr int kPiece = kKv + 4 * kTile;
+  static constexpr int kBytes = kPiece + 128;
+};
+
+struct Params {
+  Seqs seqs;
+  SplitCfg cfg;
+  Pages pages;
+  Rows Q, K, V, O;                                       // K, V: packed rows, or the pools
+  float scale;
+  float* lse;
+  float* part_o;                                         // [slot][kRows][kD]
+  float2* part_ml;                                       // [slot][kRows]
+  int* d_status;
+  int Hq;
+};
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool valid) {
+  const int sz = valid ? 16 : 0;                         // 0: the 16 bytes are zero-filled
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(sz) : "memory");
+}
+__device__ __forceinline__ float4 lds4(const float* p) { return *reinterpret_cast<const float4*>(p); }
+}  // namespace pf32
+
+template <int kD, int kRows, bool kPaged>
+__global__ void __launch_bounds__(pf32::kThreads, 1)
+packed_f32_kernel(const __grid_constant__ pf32::Params p) {
+  using namespace pf32;
+  using L = Smem<kD, kRows>;
+  constexpr int kR = kRows / 16;                         // rows per thread
+  constexpr int kC = kD / 64;                            // result columns per thread: kC vectors of 4
+  constexpr int kLd = L::kLd, kPLd = L::kPLd;
+  extern __shared__ __align__(16) unsigned char smem_raw[];
+  float* sQ = reinterpret_cast<float*>(smem_raw + L::kQ);
+  auto sK = [&](int st) { return reinterpret_cast<float*>(smem_raw + L::kKv + st * 2 * L::kTile); };
+  auto sV = [&](int st) { return reinterpret_cast<float*>(smem_raw + L::kKv + st * 2 * L::kTile + L::kTile); };
+  Piece* s_piece = reinterpret_cast<Piece*>(smem_raw + L::kPiece);
+  volatile int* s_flag = reinterpret_cast<volatile int*>(smem_raw + L::kPiece + 96);
+  PlanShared& plan = *reinterpret_cast<PlanShared*>(smem_raw + L::kKv);
+  const int tid = threadIdx.x, warp = tid >> 5;
+  const int ty = tid >> 4, tx = tid & 15;                // rows ty * kR + i, slots tx + 16 j, columns tx * 4 + 64 c
+  const int G = p.cfg.G;
+  pdl_wait();
+  long long chunk = 0;
+  plan_block<kThreads>(p.seqs, p.cfg, &plan, &chunk, p.d_status);
+  Walker w;
+  w.more = false;
+  if (warp == 0) w.init(p.seqs, p.cfg, &plan, chunk);
+  bool bad = false;
+
+  while (true) {
+    __syncthreads();                                     // everybody is done with the previous piece (and the plan)
+    if (warp == 0) {
+      Piece next;
+      const bool have = w.next(p.seqs, p.cfg, &next);
+      if (!have) next.tile0 = -1;
+      if (tid == 0) *s_piece = next;
+    }
+    __syncthreads();
+    const Piece pc = *s_piece;
+    if (pc.tile0 < 0) break;
+    const int n_rows = min(p.cfg.tokens, pc.n - pc.r * p.cfg.tokens) * G;
+    const int tok0 = pc.first + pc.r * p.cfg.tokens;
+    const uint32_t smem = (uint32_t)__cvta_generic_to_shared(smem_raw);
+    auto load_kv = [&](int t, int st) {
+      const int j0 = t * kBN;
+      const uint32_t dk = smem + L::kKv + st * 2 * L::kTile, dv = dk + L::kTile;
+#pragma unroll 4
+      for (int i = tid; i < kBN * (kD / 4); i += kThreads) {
+        const int r = i / (kD / 4), c = i % (kD / 4);
+        const bool ok = j0 + r < pc.seen;                // slots that no row sees read as zero
+        size_t ko = 0, vo = 0;
+        if (ok) {
+          if constexpr (kPaged) {
+            ko = vo = page_offset(p.pages, pc.s, j0 + r, pc.h, p.cfg.Hkv, kD, &bad) + c * 4;
+          } else {
+            ko = (size_t)(pc.first + j0 + r) * p.K.ts + (size_t)pc.h * p.K.hs + c * 4;
+            vo = (size_t)(pc.first + j0 + r) * p.V.ts + (size_t)pc.h * p.V.hs + c * 4;
+          }
+        }
+        cp_async16(dk + (r * kLd + c * 4) * 4, static_cast<const float*>(p.K.data) + ko, ok);
+        cp_async16(dv + (r * kLd + c * 4) * 4, static_cast<const float*>(p.V.data) + vo, ok);
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+#pragma unroll 2
+    for (int i = tid; i < kRows * (kD / 4); i += kThreads) {
+      const int r = i / (kD / 4), c = i % (kD / 4);
+      const bool ok = r < n_rows;
+      const size_t off = ok ? (size_t)(tok0 + r / G) * p.Q.ts + (size_t)(pc.h * G + r % G) * p.Q.hs + c * 4 : 0;
+      cp_async16(smem + L::kQ + (r * kLd + c * 4) * 4, static_cast<const float*>(p.Q.data) + off, ok);
+    }
+    load_kv(pc.tile0, 0);
+    Seq sq;
+    sq.first = pc.first; sq.n = pc.n; sq.base = pc.base;
+    const int last_tok = min((pc.r + 1) * p.cfg.tokens, pc.n) - 1;
+    int vis[kR];
+    float m[kR], l[kR], o[kR][kC * 4];
+#pragma unroll
+    for (int i = 0; i < kR; ++i) {
+      vis[i] = visible(p.seqs, sq, min(pc.r * p.cfg.tokens + (ty * kR + i) / G, last_tok));
+      m[i] = -INFINITY;
+      l[i] = 0.f;
+#pragma unroll
+      for (int c = 0; c < kC * 4; ++c) o[i][c] = 0.f;
+    }
+#pragma unroll 1
+    for (int t = pc.tile0; t < pc.tile1; ++t) {
+      const int st = (t - pc.tile0) & 1, j0 = t * kBN;
+      asm volatile("cp.async.wait_group 0;" ::: "memory");
+      __syncthreads();                                   // tile t is there, and tile t - 1 is used up
+      if (t + 1 < pc.tile1) load_kv(t + 1, st ^ 1);
+      // ---- scores ----
+      float s[kR][4];
+#pragma unroll
+      for (int i = 0; i < kR; ++i) s[i][0] = s[i][1] = s[i][2] = s[i][3] = 0.f;
+      const float *k = sK(st) + tx * kLd, *q = sQ + ty * kR * kLd;
+#pragma unroll 4
+      for (int e = 0; e < kD; e += 4) {
+        float4 kv[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) kv[j] = lds4(k + j * 16 * kLd + e);
+#pragma unroll
+        for (int i = 0; i < kR; ++i) {
+          const float4 a = lds4(q + i * kLd + e);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            s[i][j] = fmaf(a.x, kv[j].x, s[i][j]);
+            s[i][j] = fmaf(a.y, kv[j].y, s[i][j]);
+            s[i][j] = fmaf(a.z, kv[j].z, s[i][j]);
+            s[i][j] = fmaf(a.w, kv[j].w, s[i][j]);
+          }
+        }
+      }
+      // ---- online softmax ----
+#pragma unroll
+      for (int i = 0; i < kR; ++i) {
+        float mx = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          s[i][j] = j0 + tx + 16 * j < vis[i] ? s[i][j] * p.scale : -INFINITY;
+          mx = fmaxf(mx, s[i][j]);
+        }
+#pragma unroll
+        for (int x = 8; x > 0; x >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, x));
+        const float mn = fmaxf(m[i], mx), mu = mn == -INFINITY ? 0.f : mn;
+        const float corr = m[i] == mn ? 1.f : expf(m[i] - mu);
+        m[i] = mn;
+        l[i] *= corr;
+#pragma unroll
+        for (int c = 0; c < kC * 4; ++c) o[i][c] *= corr;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          s[i][j] = expf(s[i][j] - mu);
+          l[i] += s[i][j];                               // (this thread's slots; joined at the end)
+        }
+      }
+      __syncthreads();                                   // K is used up
+      float* sP = sK(st);
+#pragma unroll
+      for (int i = 0; i < kR; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sP[(ty * kR + i) * kPLd + tx + 16 * j] = s[i][j];
+      __syncthreads();
+      // ---- result ----
+      const float *v = sV(st) + tx * 4, *pr = sP + ty * kR * kPLd;
+      const bool edge = j0 + kBN > pc.seen0;             // some row does not see some slot: zero weights times what it holds
+#pragma unroll 2
+      for (int j = 0; j < kBN; j += 4) {
+        float4 a[kR];
+#pragma unroll
+        for (int i = 0; i < kR; ++i) a[i] = lds4(pr + i * kPLd + j);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          float4 b[kC];
+#pragma unroll
+          for (int c = 0; c < kC; ++c) b[c] = lds4(v + (j + u) * kLd + c * 64);
+#pragma unroll
+          for (int i = 0; i < kR; ++i) {
+            const float w = u == 0 ? a[i].x : u == 1 ? a[i].y : u == 2 ? a[i].z : a[i].w;
+            if (!edge || j0 + j + u < vis[i]) {
+#pragma unroll
+              for (int c = 0; c < kC; ++c) {
+                o[i][c * 4] = fmaf(w, b[c].x, o[i][c * 4]);
+                o[i][c * 4 + 1] = fmaf(w, b[c].y, o[i][c * 4 + 1]);
+                o[i][c * 4 + 2] = fmaf(w, b[c].z, o[i][c * 4 + 2]);
+                o[i][c * 4 + 3] = fmaf(w, b[c].w, o[i][c * 4 + 3]);
+              }
+            }
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kR; ++i)
+#pragma unroll
+      for (int x = 8; x > 0; x >>= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], x);
+    auto write_row = [&](int i, const float* acc, float M, float Ls) {
+      const int row = ty * kR + i;
+      if (row >= n_rows) return;
+      const int tok = tok0 + row / G, hq = pc.h * G + row % G;
+      const float inv = 1.0f / Ls;
+      float* op = static_cast<float*>(p.O.data) + (size_t)tok * p.O.ts + (size_t)hq * p.O.hs + tx * 4;
+#pragma unroll
+      for (int c = 0; c < kC; ++c)
+        *reinterpret_cast<float4*>(op + c * 64) =
+            Ls == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f)
+                      : make_float4(acc[c * 4] * inv, acc[c * 4 + 1] * inv, acc[c * 4 + 2] * inv, acc[c * 4 + 3] * inv);
+      if (tx == 0 && p.lse != nullptr) p.lse[(size_t)tok * p.Hq + hq] = Ls == 0.f ? -INFINITY : M + logf(Ls);
+    };
+    if (pc.slot < 0) {
+#pragma unroll
+      for (int i = 0; i < kR; ++i) write_row(i, o[i], m[i], l[i]);
+      continue;
+    }
+    // a piece of a cut item leaves (m, l, O); whoever takes the last ticket merges them in order of the pieces
+#pragma unroll
+    for (int i = 0; i < kR; ++i) {
+      const size_t row = (size_t)pc.slot * kRows + ty * kR + i;
+#pragma unroll
+      for (int c = 0; c < kC; ++c)
+        *reinterpret_cast<float4*>(p.part_o + row * kD + c * 64 + tx * 4) =
+            make_float4(o[i][c * 4], o[i][c * 4 + 1], o[i][c * 4 + 2], o[i][c * 4 + 3]);
+      if (tx == 0) p.part_ml[row] = make_float2(m[i], l[i]);
+    }
+    __threadfence();
+    __syncthreads();
+    if (tid == 0) *s_flag = last_piece(p.d_status, pc.ticket, pc.n_pieces);
+    __syncthreads();
+    if (*s_flag) {
+      __threadfence();
+#pragma unroll 1
+      for (int i = 0; i < kR; ++i) {
+        const int row = ty * kR + i;
+        if (row >= n_rows) continue;
+        float M = -INFINITY, Ls = 0.f, acc[kC * 4];
+#pragma unroll
+        for (int c = 0; c < kC * 4; ++c) acc[c] = 0.f;
+#pragma unroll 4
+        for (int n = 0; n < pc.n_pieces; ++n) {
+          const float2 x = __ldcg(p.part_ml + piece_slot(pc.ticket, n) * kRows + row);
+          if (x.y != 0.f) M = fmaxf(M, x.x);
+        }
+#pragma unroll 4
+        for (int n = 0; n < pc.n_pieces; ++n) {
+          const size_t at = (size_t)piece_slot(pc.ticket, n) * kRows + row;
+          const float2 x = __ldcg(p.part_ml + at);
+          const float wgt = x.y == 0.f ? 0.f : expf(x.x - M);
+#pragma unroll
+          for (int c = 0; c < kC; ++c) {
+            const float4 v4 = __ldcg(reinterpret_cast<const float4*>(p.part_o + at * kD + c * 64 + tx * 4));
+            if (x.y != 0.f) {
+              acc[c * 4] = fmaf(v4.x, wgt, acc[c * 4]);
+              acc[c * 4 + 1] = fmaf(v4.y, wgt, acc[c * 4 + 1]);
+              acc[c * 4 + 2] = fmaf(v4.z, wgt, acc[c * 4 + 2]);
+              acc[c * 4 + 3] = fmaf(v4.w, wgt, acc[c * 4 + 3]);
+            }
+          }
+          if (x.y != 0.f) Ls += x.y * wgt;
+        }
+        write_row(i, acc, M, Ls);
+      }
+    }
+  }
+  if (bad) atomicMax(p.d_status, (int)CHECK_PAGE_RANGE);
+  pdl_launch_dependents();
+}
+
+size_t packed_f32_scratch_bytes(int d) { return (size_t)2 * kMaxPackedCtas * 64 * ((size_t)d * 4 + 8); }
+
+namespace pf32 {
+template <int kD, int kRows, bool kPaged>
+static cudaError_t launch(Params p, int ctas, char* ws, cudaStream_t stream) {
+  p.cfg.tokens = kRows / p.cfg.G;
+  p.part_o = reinterpret_cast<float*>(ws);
+  p.part_ml = reinterpret_cast<float2*>(ws + (size_t)2 * ctas * kRows * kD * 4);
+  auto kern = packed_f32_kernel<kD, kRows, kPaged>;
+  cudaError_t e = ensure_dynamic_smem<5000 + kD * 4 + kRows * 2 + kPaged>(kern, Smem<kD, kRows>::kBytes);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)ctas);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = Smem<kD, kRows>::kBytes;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kern, p);
+}
+}  // namespace pf32
+
+cudaError_t launch_packed_f32(const samkv_packed_t& d, const Seqs& seqs, const KvSource& kv, const Rows& Q, float scale,
+                              const Rows& O, float* lse, bool few_rows, const samkv_ctx_impl& h, cudaStream_t stream) {
+  pf32::Params p = {};
+  p.seqs = seqs;
+  p.cfg.G = d.n_q_heads / d.n_kv_heads;
+  p.cfg.Hkv = d.n_kv_heads;
+  p.cfg.tile = pf32::kBN;
+  p.cfg.fixed = 2 * pf32::kBN;
+  p.cfg.min_chunk = 4 * pf32::kBN;
+  p.pages = kv.pages;
+  p.Q = Q;
+  p.O = O;
+  p.K = kv.K;
+  p.V = kv.V;
+  if (kv.paged) {
+    p.K.data = kv.pages.K;
+    p.V.data = kv.pages.V;
+  }
+  p.scale = scale;
+  p.lse = lse;
+  p.d_status = h.d_status;
+  p.Hq = d.n_q_heads;
+  const int ctas = h.sm_count < kMaxPackedCtas ? h.sm_count : kMaxPackedCtas;
+  char* ws = h.workspace + kStatusBytes;
+#define SAMKV_F32_CASE(D, R) (kv.paged ? pf32::launch<D, R, true>(p, ctas, ws, stream) : pf32::launch<D, R, false>(p, ctas, ws, stream))
+  if (d.head_dim == 128) return few_rows ? SAMKV_F32_CASE(128, 16) : SAMKV_F32_CASE(128, 64);
+  return few_rows ? SAMKV_F32_CASE(64, 16) : SAMKV_F32_CASE(64, 64);
+#undef SAMKV_F32_CASE
+}
+
+}  // namespace samkv
