@@ -397,16 +397,21 @@ def samkv_attn_kernel_count(handle: Handle, shape: Shape, T_q: int, cache_capaci
 
 # ------------------------------------------------------------------ packed sequences and the paged cache
 _TORCH_DTYPES = {SAMKV_F32: torch.float32, SAMKV_BF16: torch.bfloat16}
+_current_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else torch.cuda.current_device
 
 
-def _device_ptr(t: Optional[torch.Tensor], what: str, dtype: torch.dtype, shape: Sequence[int]) -> Optional[int]:
-    """Pointer of a contiguous CUDA tensor of this dtype and shape on the current device (None stays None)."""
+def _raw_stream(device: int) -> int:
+    return torch._C._cuda_getCurrentRawStream(device)
+
+
+def _device_ptr(t: Optional[torch.Tensor], what: str, dtype: torch.dtype, shape: tuple, device: int) -> Optional[int]:
+    """Pointer of a contiguous tensor of this dtype and shape on this CUDA device (None stays None)."""
     if t is None:
         return None
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+    if t.get_device() != device:
         raise ValueError(f"{what}: expected a CUDA tensor on the current device")
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{what}: expected {dtype} of shape {tuple(shape)}, got {t.dtype} of shape {tuple(t.shape)}")
+    if t.dtype is not dtype or t.shape != shape:
+        raise ValueError(f"{what}: expected {dtype} of shape {shape}, got {t.dtype} of shape {tuple(t.shape)}")
     if not t.is_contiguous():
         raise ValueError(f"{what}: expected a contiguous tensor")
     return t.data_ptr()
@@ -426,28 +431,33 @@ class Packed:
         self.n_seq = seq_offsets.shape[0] - 1
         self.c = samkv_packed_t(n_q_heads, n_kv_heads, head_dim, code, self.n_seq, n_tokens, max_seq_tokens,
                                 seq_offsets.data_ptr())
+        self._device = seq_offsets.get_device()
+        self._dtype = _TORCH_DTYPES.get(code)
+        self._q, self._kv = (n_tokens, n_q_heads, head_dim), (n_tokens, n_kv_heads, head_dim)
+        self._lse, self._per_token, self._per_seq = (n_tokens, n_q_heads), (n_tokens,), (self.n_seq,)
 
     def ref(self):
         return ctypes.byref(self.c)
 
-    def checked(self):
-        """The description for a call: the offsets have to be on the current device."""
-        _device_ptr(self.seq_offsets, "seq_offsets", torch.int32, (self.n_seq + 1,))
-        return ctypes.byref(self.c)
+    def device(self) -> int:
+        """The current device, on which the offsets have to be."""
+        d = _current_device()
+        if d != self._device:
+            raise ValueError("seq_offsets: expected a CUDA tensor on the current device")
+        return d
 
-    def rows(self, t: Optional[torch.Tensor], heads: int, what: str):
+    def rows(self, t: Optional[torch.Tensor], want: tuple, what: str, device: int):
         """samkv_rows_t of a tensor [n_tokens, heads, head_dim] with any token and head strides."""
         if t is None:
             return None
-        if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        if t.get_device() != device:
             raise ValueError(f"{what}: expected a CUDA tensor on the current device")
-        want = (self.n_tokens, heads, self.head_dim)
-        if t.dtype != _TORCH_DTYPES.get(self.c.dtype) or tuple(t.shape) != want:
-            raise ValueError(f"{what}: expected {_TORCH_DTYPES.get(self.c.dtype)} of shape {want}, got {t.dtype} of shape "
-                             f"{tuple(t.shape)}")
-        if t.stride(2) != 1:
+        if t.dtype is not self._dtype or t.shape != want:
+            raise ValueError(f"{what}: expected {self._dtype} of shape {want}, got {t.dtype} of shape {tuple(t.shape)}")
+        strides = t.stride()
+        if strides[2] != 1:
             raise ValueError(f"{what}: the head dimension must be contiguous")
-        return ctypes.byref(samkv_rows_t(t.data_ptr(), t.stride(0), t.stride(1)))
+        return samkv_rows_t(t.data_ptr(), strides[0], strides[1])
 
 
 class Pages:
@@ -456,16 +466,25 @@ class Pages:
     def __init__(self, K: torch.Tensor, V: torch.Tensor, block_table: torch.Tensor):
         if K.dim() != 4 or block_table.dim() != 2:
             raise ValueError("pages: expected pools of four dimensions and a table of two")
+        if V.shape != K.shape or V.dtype != K.dtype or block_table.dtype != torch.int32:
+            raise ValueError("pages: expected two pools of one shape and type and an int32 table")
+        if not (K.is_contiguous() and V.is_contiguous() and block_table.is_contiguous()):
+            raise ValueError("pages: expected contiguous tensors")
+        if len({K.get_device(), V.get_device(), block_table.get_device()}) != 1:
+            raise ValueError("pages: expected tensors on one device")
         self.K, self.V, self.block_table = K, V, block_table
+        self.c = samkv_pages_t(K.data_ptr(), V.data_ptr(), block_table.data_ptr(), K.shape[2], K.shape[0], block_table.shape[1])
 
     def checked(self, packed: Packed):
-        n_pages, _, page_size, _ = self.K.shape
-        pool = (n_pages, packed.n_kv_heads, page_size, packed.head_dim)
-        dt = _TORCH_DTYPES.get(packed.c.dtype)
-        width = self.block_table.shape[1]
-        return ctypes.byref(samkv_pages_t(_device_ptr(self.K, "K pages", dt, pool), _device_ptr(self.V, "V pages", dt, pool),
-                                          _device_ptr(self.block_table, "block_table", torch.int32, (packed.n_seq, width)),
-                                          page_size, n_pages, width))
+        """The description for a call with these sequences."""
+        if self.K.get_device() != packed._device:
+            raise ValueError("pages: expected CUDA tensors on the current device")
+        shape = self.K.shape
+        if shape[1] != packed.n_kv_heads or shape[3] != packed.head_dim or self.K.dtype is not packed._dtype:
+            raise ValueError(f"pages: expected {packed._dtype} pools with {packed.n_kv_heads} heads of {packed.head_dim}")
+        if self.block_table.shape[0] != packed.n_seq:
+            raise ValueError(f"block_table: expected {packed.n_seq} rows")
+        return self.c
 
 
 class Rope:
@@ -488,29 +507,33 @@ def samkv_packed_workspace_bytes(packed: Packed) -> int:
 
 
 def samkv_prefill(handle: Handle, packed: Packed, Q, K, V, scale: float, O, lse=None):
-    _check(lib().samkv_prefill(handle.h, packed.checked(), packed.rows(Q, packed.n_q_heads, "Q"),
-                               packed.rows(K, packed.n_kv_heads, "K"), packed.rows(V, packed.n_kv_heads, "V"),
-                               float(scale), packed.rows(O, packed.n_q_heads, "O"),
-                               _device_ptr(lse, "lse", torch.float32, (packed.n_tokens, packed.n_q_heads)), _stream()),
-           "samkv_prefill")
+    dev, q, kv = packed.device(), packed._q, packed._kv
+    status = lib().samkv_prefill(handle._h, packed.c, packed.rows(Q, q, "Q", dev), packed.rows(K, kv, "K", dev),
+                                 packed.rows(V, kv, "V", dev), scale, packed.rows(O, q, "O", dev),
+                                 _device_ptr(lse, "lse", torch.float32, packed._lse, dev), _raw_stream(dev))
+    if status:
+        raise SamkvError(status, "samkv_prefill")
 
 
 def samkv_append(handle: Handle, packed: Packed, K, V, pages: Optional[Pages] = None, cache_len=None,
                  rope: Optional[Rope] = None, positions=None, Q=None, Q_out=None, K_out=None, V_out=None):
-    _check(lib().samkv_append(handle.h, packed.checked(), packed.rows(K, packed.n_kv_heads, "K"),
-                              packed.rows(V, packed.n_kv_heads, "V"), None if pages is None else pages.checked(packed),
-                              _device_ptr(cache_len, "cache_len", torch.int32, (packed.n_seq,)),
-                              None if rope is None else rope.ref(),
-                              _device_ptr(positions, "positions", torch.int32, (packed.n_tokens,)),
-                              packed.rows(Q, packed.n_q_heads, "Q"), packed.rows(Q_out, packed.n_q_heads, "Q_out"),
-                              packed.rows(K_out, packed.n_kv_heads, "K_out"),
-                              packed.rows(V_out, packed.n_kv_heads, "V_out"), _stream()), "samkv_append")
+    dev, q, kv = packed.device(), packed._q, packed._kv
+    status = lib().samkv_append(handle._h, packed.c, packed.rows(K, kv, "K", dev), packed.rows(V, kv, "V", dev),
+                                None if pages is None else pages.checked(packed),
+                                _device_ptr(cache_len, "cache_len", torch.int32, packed._per_seq, dev),
+                                None if rope is None else rope.c,
+                                _device_ptr(positions, "positions", torch.int32, packed._per_token, dev),
+                                packed.rows(Q, q, "Q", dev), packed.rows(Q_out, q, "Q_out", dev),
+                                packed.rows(K_out, kv, "K_out", dev), packed.rows(V_out, kv, "V_out", dev), _raw_stream(dev))
+    if status:
+        raise SamkvError(status, "samkv_append")
 
 
 def samkv_paged_attn(handle: Handle, packed: Packed, pages: Pages, cache_len, Q, scale: float, causal: bool, O, lse=None):
-    _check(lib().samkv_paged_attn(handle.h, packed.checked(), pages.checked(packed),
-                                  _device_ptr(cache_len, "cache_len", torch.int32, (packed.n_seq,)),
-                                  packed.rows(Q, packed.n_q_heads, "Q"), float(scale), int(bool(causal)),
-                                  packed.rows(O, packed.n_q_heads, "O"),
-                                  _device_ptr(lse, "lse", torch.float32, (packed.n_tokens, packed.n_q_heads)), _stream()),
-           "samkv_paged_attn")
+    dev, q = packed.device(), packed._q
+    status = lib().samkv_paged_attn(handle._h, packed.c, pages.checked(packed),
+                                    _device_ptr(cache_len, "cache_len", torch.int32, packed._per_seq, dev),
+                                    packed.rows(Q, q, "Q", dev), scale, bool(causal), packed.rows(O, q, "O", dev),
+                                    _device_ptr(lse, "lse", torch.float32, packed._lse, dev), _raw_stream(dev))
+    if status:
+        raise SamkvError(status, "samkv_paged_attn")

@@ -214,7 +214,9 @@ def test_binding_checks_devices_types_and_shapes():
     p = B.Packed(8, 2, 128, off, 3)
     assert p.n_seq == 1 and B.samkv_packed_workspace_bytes(p) >= 256
     with pytest.raises(ValueError):
-        p.rows(torch.zeros(3, 8, 128, dtype=torch.bfloat16), 8, "Q")          # host memory
+        p.rows(torch.zeros(3, 8, 128, dtype=torch.bfloat16), (3, 8, 128), "Q", 0)          # host memory
+    with pytest.raises(ValueError):
+        B.Pages(torch.zeros(4, 2, 16, 128), torch.zeros(4, 2, 16, 64), off[None])
     with pytest.raises(ValueError):
         B.Pages(torch.zeros(4, 2, 16), torch.zeros(4, 2, 16, 128), off[None])
     with pytest.raises(ValueError):

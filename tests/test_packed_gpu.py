@@ -540,7 +540,8 @@ def test_workspace_and_handle_refusals():
         raw = ctypes.c_void_p()
         assert B.lib().samkv_create(ctypes.byref(raw), 0, small.data_ptr(), need - 256) == 0
         assert B.lib().samkv_paged_attn(raw, p.ref(), B.Pages(c.Kp, c.Vp, c.table).checked(p), c.cache_len.data_ptr(),
-                                        p.rows(c.Q, 8, "Q"), 0.0, 1, p.rows(O, 8, "O"), None, None) == 3
+                                        p.rows(c.Q, (c.T, 8, 128), "Q", 0), 0.0, 1, p.rows(O, (c.T, 8, 128), "O", 0), None,
+                                        None) == 3
         torch.cuda.synchronize()
         B.lib().samkv_destroy(raw)
     # nothing to do
