@@ -8,8 +8,8 @@
 
 namespace samkv {
 
-constexpr int kAppendThreads = 256;
-constexpr int kMaxAppendTokens = 8;            // tokens per CTA
+constexpr int kAppendThreads = 128;
+constexpr int kMaxAppendTokens = 2;            // tokens per CTA
 
 struct AppendArgs {
   Seqs seqs;

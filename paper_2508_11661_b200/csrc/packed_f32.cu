@@ -316,7 +316,7 @@ static cudaError_t launch(Params p, int ctas, char* ws, cudaStream_t stream) {
 }  // namespace pf32
 
 cudaError_t launch_packed_f32(const samkv_packed_t& d, const Seqs& seqs, const KvSource& kv, const Rows& Q, float scale,
-                              const Rows& O, float* lse, bool few_rows, const samkv_ctx_impl& h, cudaStream_t stream) {
+                              const Rows& O, float* lse, int rows, const samkv_ctx_impl& h, cudaStream_t stream) {
   pf32::Params p = {};
   p.seqs = seqs;
   p.cfg.G = d.n_q_heads / d.n_kv_heads;
@@ -340,8 +340,9 @@ cudaError_t launch_packed_f32(const samkv_packed_t& d, const Seqs& seqs, const K
   const int ctas = h.sm_count < kMaxPackedCtas ? h.sm_count : kMaxPackedCtas;
   char* ws = h.workspace + kStatusBytes;
 #define SAMKV_F32_CASE(D, R) (kv.paged ? pf32::launch<D, R, true>(p, ctas, ws, stream) : pf32::launch<D, R, false>(p, ctas, ws, stream))
-  if (d.head_dim == 128) return few_rows ? SAMKV_F32_CASE(128, 16) : SAMKV_F32_CASE(128, 64);
-  return few_rows ? SAMKV_F32_CASE(64, 16) : SAMKV_F32_CASE(64, 64);
+  if (d.head_dim == 128)
+    return rows == 16 ? SAMKV_F32_CASE(128, 16) : rows == 32 ? SAMKV_F32_CASE(128, 32) : SAMKV_F32_CASE(128, 64);
+  return rows == 16 ? SAMKV_F32_CASE(64, 16) : rows == 32 ? SAMKV_F32_CASE(64, 32) : SAMKV_F32_CASE(64, 64);
 #undef SAMKV_F32_CASE
 }
 
