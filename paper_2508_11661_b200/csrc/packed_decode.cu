@@ -427,12 +427,12 @@ packed_decode_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
             float M = -INFINITY, Ls = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
             for (int k = 0; k < pc.n_pieces; ++k) {
-              const float2 x = __ldcg(p.part_ml + piece_slot(pc.ticket, k) * kRows + row);
+              const float2 x = __ldcg(p.part_ml + piece_slot(pc, k) * kRows + row);
               if (x.y != 0.f) M = fmaxf(M, x.x);
             }
 #pragma unroll 4
             for (int k = 0; k < pc.n_pieces; ++k) {
-              const int slot = piece_slot(pc.ticket, k);
+              const int slot = piece_slot(pc, k);
               const float2 x = __ldcg(p.part_ml + slot * kRows + row);
               const float4 v = __ldcg(reinterpret_cast<const float4*>(p.part_o + ((size_t)slot * kRows + row) * kD + c4 * 4));
               if (x.y == 0.f) continue;

@@ -262,12 +262,12 @@ packed_f32_kernel(const __grid_constant__ pf32::Params p) {
         for (int c = 0; c < kC * 4; ++c) acc[c] = 0.f;
 #pragma unroll 4
         for (int n = 0; n < pc.n_pieces; ++n) {
-          const float2 x = __ldcg(p.part_ml + piece_slot(pc.ticket, n) * kRows + row);
+          const float2 x = __ldcg(p.part_ml + piece_slot(pc, n) * kRows + row);
           if (x.y != 0.f) M = fmaxf(M, x.x);
         }
 #pragma unroll 4
         for (int n = 0; n < pc.n_pieces; ++n) {
-          const size_t at = (size_t)piece_slot(pc.ticket, n) * kRows + row;
+          const size_t at = (size_t)piece_slot(pc, n) * kRows + row;
           const float2 x = __ldcg(p.part_ml + at);
           const float wgt = x.y == 0.f ? 0.f : expf(x.x - M);
 #pragma unroll

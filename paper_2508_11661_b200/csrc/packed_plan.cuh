@@ -12,13 +12,21 @@
 // and the one it ends with (slot 2c + 1).  The CTA that finishes an item's last piece merges them in order of the axis,
 // so results do not depend on timing.  Tickets are bytes of the workspace's status block, one per first border of an
 // item, and return to zero.
+//
+// That order walks each row tile of a sequence through all of its keys before the next one.  Where several row tiles
+// share keys that the L2 cache cannot hold, every one of them would fetch them from HBM again; such calls are laid out in
+// waves instead: keys are cut into blocks of one length, a unit is a row tile times a block, units run block by block
+// with the row tiles next to one another, and CTA c takes units c, c + grid, ...: the row tiles of a block run at the same
+// time and share its keys through L2 (128 tokens over 102400, 8 row tiles per KV head: see packed_tc.cu).
 #pragma once
 
 #include "packed.cuh"
 
 namespace samkv {
 
-constexpr int kMaxPackedCtas = 160;            // tickets: bytes of status words 1..31 and 33..41 (0 and 32 have other uses)
+constexpr int kMaxPackedCtas = 160;
+constexpr int kMaxTickets = 240;               // bytes of status words 1..31 and 33..61 (0 and 32 have other uses)
+constexpr int kMaxUnits = 896;                 // workspace slots of a call in waves
 
 struct SplitCfg {
   int G, Hkv;
@@ -26,6 +34,7 @@ struct SplitCfg {
   int tile;                    // slots per key tile
   int fixed;                   // slots that an item's fixed cost amounts to (>= 2 * tile)
   int min_chunk;               // least slots (fixed cost included) worth a CTA of its own (>= 2 * tile)
+  long long wave_slots;        // lay out in waves where the distinct key slots of a call exceed this; 0: never
 };
 
 struct Piece {
@@ -34,9 +43,15 @@ struct Piece {
   int seen0, seen;             // slots that the row tile's first and last token see
   int tile0, tile1;            // key tiles of this piece
   int slot;                    // workspace slot of the partial result, -1: the piece is the whole item
-  int ticket;                  // first border inside the item
+  int slot0, slot_step;        // slots of the item's pieces, see piece_slot()
+  int ticket;
   int n_pieces;
 };
+// Workspace slot of an item's piece k.  In waves the pieces are slot_step apart; else (slot_step 0) the first is the last
+// piece of the CTA before the first border, the others are the first ones of the CTAs that start at the borders.
+__device__ __forceinline__ int piece_slot(const Piece& p, int k) {
+  return p.slot_step > 0 ? p.slot0 + k * p.slot_step : p.slot0 + 2 * k - (k > 0 ? 1 : 0);
+}
 
 __device__ __forceinline__ int row_tiles(const SplitCfg& c, int n) { return (n + c.tokens - 1) / c.tokens; }
 // length of the first x items of one (sequence, head)
@@ -46,6 +61,7 @@ __device__ __forceinline__ long long items_length(const SplitCfg& c, int causal,
   return len;
 }
 
+constexpr int kWaveTries = 12;
 struct PlanShared {
   long long warp_len[32];
   int warp_items[32];
@@ -53,6 +69,10 @@ struct PlanShared {
   int s;
   long long total;             // length of the axis
   int items;
+  unsigned long long distinct; // key slots of the call, each counted once
+  int longest;                 // most tiles of an item
+  int wave_tiles;              // tiles per block of a call in waves, 0: contiguous stretches
+  unsigned units[kWaveTries];  // units for each length tried
 };
 
 // Block-wide: finds the sequence that holds this CTA's first position.  All kThreads threads call it; afterwards
@@ -63,6 +83,12 @@ __device__ __forceinline__ void plan_block(const Seqs& q, const SplitCfg& c, Pla
   constexpr int kWarps = kThreads / 32;
   const int per = (q.n_seq + kThreads - 1) / kThreads;
   const int s0 = min(tid * per, q.n_seq), s1 = min(s0 + per, q.n_seq);
+  if (tid == 0) {
+    sh->distinct = 0;
+    sh->longest = 0;
+    sh->wave_tiles = 0;
+  }
+  if (tid < kWaveTries) sh->units[tid] = 0;
   long long len = 0;
   int items = 0;
   bool clamped = false;
@@ -103,6 +129,55 @@ __device__ __forceinline__ void plan_block(const Seqs& q, const SplitCfg& c, Pla
   }
   __syncthreads();
   const long long total = sh->total;
+  if (c.wave_slots > 0 && total > 2 * c.wave_slots && sh->items <= kMaxTickets) {
+    // candidates for waves: a second look at the lengths
+    unsigned long long distinct = 0;
+    int longest = 0;
+#pragma unroll 1
+    for (int s = s0; s < s1; ++s) {
+      const Seq sq = load_seq(q, s);
+      if (sq.n == 0) continue;
+      const int seen = visible(q, sq, sq.n - 1);
+      distinct += (unsigned long long)c.Hkv * seen;
+      longest = max(longest, (seen + c.tile - 1) / c.tile);
+    }
+    if (distinct > 0) {
+      atomicAdd(&sh->distinct, distinct);
+      atomicMax(&sh->longest, longest);
+    }
+    __syncthreads();
+    if ((long long)sh->distinct > c.wave_slots && total > 2 * (long long)sh->distinct) {
+      const int most = sh->longest;
+#pragma unroll 1
+      for (int s = s0; s < s1; ++s) {
+        const Seq sq = load_seq(q, s);
+        if (sq.n == 0) continue;
+        const int nt = (visible(q, sq, sq.n - 1) + c.tile - 1) / c.tile;
+#pragma unroll 1
+        for (int k = 0; k < kWaveTries; ++k) {
+          const int bt = (most + k) / (k + 1);
+          atomicAdd(&sh->units[k], (unsigned)(c.Hkv * row_tiles(c, sq.n) * ((nt + bt - 1) / bt)));
+        }
+      }
+      __syncthreads();
+      if (tid == 0) {
+        long long best = -1;
+        for (int k = 0; k < kWaveTries; ++k) {
+          const int bt = (most + k) / (k + 1);
+          if (sh->units[k] > kMaxUnits || bt < 8) continue;
+          const long long cost = (long long)((sh->units[k] + gridDim.x - 1) / gridDim.x) * (bt * c.tile + c.fixed);
+          if (best < 0 || cost < best) {
+            best = cost;
+            sh->wave_tiles = bt;
+          }
+        }
+        // (an uneven mix of lengths leaves holes in the waves; the keys are fetched again instead)
+        if (best > total / (long long)gridDim.x * 3 / 2) sh->wave_tiles = 0;
+      }
+      __syncthreads();
+      if (sh->wave_tiles > 0) return;
+    }
+  }
   long long ctas = total / c.min_chunk;
   if (ctas < sh->items) ctas = sh->items;
   if (ctas > (long long)gridDim.x) ctas = gridDim.x;
@@ -134,6 +209,7 @@ struct Walker {
   int s, h, r, R;
   int w_first, w_n, w_base, w_s0;          // lane i: sequence w_s0 + i
   Seq cur;
+  int wave_tiles, unit, unit0, item0, nb;  // calls in waves: next unit, units and items before the current sequence
   int first_piece_tile;                    // tile the first piece starts with, -1 once taken
   bool more;
 
@@ -172,11 +248,20 @@ struct Walker {
     const long long p0 = ch * blockIdx.x;
     total_len = sh->total;
     chunk = ch;
+    wave_tiles = sh->wave_tiles;
+    w_s0 = -64;
+    if (wave_tiles > 0) {
+      unit = blockIdx.x;
+      unit0 = item0 = 0;
+      s = -1;
+      R = nb = 0;
+      more = true;
+      return;
+    }
     more = p0 < total_len;
     if (!more) return;
     p1 = min(p0 + ch, total_len);
     s = sh->s;
-    w_s0 = -64;
     fetch(q, s);
     R = row_tiles(c, cur.n);
     const long long per_head = items_length(c, q.causal, cur.base, R);
@@ -193,8 +278,53 @@ struct Walker {
     item_start = sh->start + h * per_head + items_length(c, q.causal, cur.base, r);
     first_piece_tile = border(c, p0, tiles(q, c));
   }
+  // Next unit of a call in waves.
+  __device__ __forceinline__ bool next_unit(const Seqs& q, const SplitCfg& c, Piece* out) {
+#pragma unroll 1
+    while (true) {
+      while (s < 0 || unit >= unit0 + c.Hkv * R * nb) {     // the sequence that holds it
+        if (s >= 0) {
+          unit0 += c.Hkv * R * nb;
+          item0 += c.Hkv * R;
+        }
+        if (++s >= q.n_seq) return false;
+        fetch(q, s);
+        R = row_tiles(c, cur.n);
+        nb = R == 0 ? 0 : (visible(q, cur, cur.n - 1) + c.tile * wave_tiles - 1) / (c.tile * wave_tiles);
+      }
+      int rest = unit - unit0;
+      r = rest % R;
+      rest /= R;
+      const int b = rest % nb;
+      h = rest / nb;
+      const int nt = tiles(q, c);
+      const int u = unit;
+      unit += gridDim.x;
+      if (b * wave_tiles >= nt) continue;
+      out->tile0 = b * wave_tiles;
+      out->tile1 = min(out->tile0 + wave_tiles, nt);
+      describe(q, c, out);
+      out->n_pieces = (nt + wave_tiles - 1) / wave_tiles;
+      out->ticket = item0 + h * R + r;
+      out->slot0 = u - b * R;
+      out->slot_step = R;
+      out->slot = out->n_pieces > 1 ? u : -1;
+      return true;
+    }
+  }
+  __device__ __forceinline__ void describe(const Seqs& q, const SplitCfg& c, Piece* out) const {
+    out->s = s;
+    out->h = h;
+    out->r = r;
+    out->first = cur.first;
+    out->n = cur.n;
+    out->base = cur.base;
+    out->seen0 = visible(q, cur, r * c.tokens);
+    out->seen = visible(q, cur, min((r + 1) * c.tokens, cur.n) - 1);
+  }
   // Next piece; false when the CTA's stretch is done.
   __device__ __forceinline__ bool next(const Seqs& q, const SplitCfg& c, Piece* out) {
+    if (wave_tiles > 0) return next_unit(q, c, out);
 #pragma unroll 1
     while (more) {
       const int nt = tiles(q, c);
@@ -206,14 +336,7 @@ struct Walker {
       const bool ends_inside = t1 < nt;
       const bool emit = t0 < t1;
       if (emit) {
-        out->s = s;
-        out->h = h;
-        out->r = r;
-        out->first = cur.first;
-        out->n = cur.n;
-        out->base = cur.base;
-        out->seen0 = visible(q, cur, r * c.tokens);
-        out->seen = visible(q, cur, min((r + 1) * c.tokens, cur.n) - 1);
+        describe(q, c, out);
         out->tile0 = t0;
         out->tile1 = t1;
         out->slot = -1;
@@ -229,6 +352,8 @@ struct Walker {
           out->slot = 2 * (int)blockIdx.x + (starts_inside ? 0 : 1);
           out->ticket = (int)ca;
           out->n_pieces = (int)(cb - ca) + 2;
+          out->slot0 = 2 * ((int)ca - 1) + 1;
+          out->slot_step = 0;
         }
       }
       // move on
@@ -255,10 +380,6 @@ struct Walker {
     return false;
   }
 };
-
-// Workspace slot of an item's piece k (0 = the one at the item's start): the first is the last piece of the CTA before
-// the first border, the others are the first pieces of the CTAs that start at the borders.
-__device__ __forceinline__ int piece_slot(int ticket, int k) { return k == 0 ? 2 * (ticket - 1) + 1 : 2 * (ticket + k - 1); }
 
 // Takes a ticket of a cut item; true for the CTA that comes last, which also clears the ticket.  One thread per piece,
 // after its CTA's partial results are written and fenced.

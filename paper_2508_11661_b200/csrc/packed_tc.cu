@@ -47,11 +47,11 @@ struct Smem {
   static constexpr int kRef = kV + kVStages * kTile;   // reference maxima, [kGroups (piece mod)][128] fp32
   static constexpr int kSum = kRef + kGroups * 512;    // denominators handed to the finishing group, [2][128] fp32
   static constexpr int kPieces = kSum + 1024;          // kRing descriptors
-  static constexpr int kBar = kPieces + 160;
+  static constexpr int kBar = kPieces + 184;
   static constexpr int kMisc = kBar + 288;             // tensor memory address, failure flag, "merge" and "scrub" flags
-  static constexpr int kBytes = kMisc + 64;
+  static constexpr int kBytes = kMisc + 40;
 };
-static_assert(kRing * sizeof(Piece) <= 160, "descriptors");
+static_assert(kRing * sizeof(Piece) <= 184, "descriptors");
 
 static_assert(Smem<128>::kBytes <= 232448, "shared memory of one CTA");
 
@@ -691,14 +691,14 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
             m_out = -INFINITY;
 #pragma unroll 1
             for (int k = 0; k < pc.n_pieces; ++k) {
-              const float2 x = __ldcg(p.part_ml + piece_slot(pc.ticket, k) * 128 + row);
+              const float2 x = __ldcg(p.part_ml + piece_slot(pc, k) * 128 + row);
               m_out = x.y == 0.f ? m_out : fmaxf(m_out, x.x);
             }
             const float Mu = m_out == -INFINITY ? 0.f : m_out;
             l = 0.f;
 #pragma unroll 1
             for (int k = 0; k < pc.n_pieces; ++k) {
-              const float2 x = __ldcg(p.part_ml + piece_slot(pc.ticket, k) * 128 + row);
+              const float2 x = __ldcg(p.part_ml + piece_slot(pc, k) * 128 + row);
               if (x.y != 0.f) l += x.y * fast_exp2(x.x - Mu);
             }
             const float inv_all = l == 0.f ? 0.f : 1.0f / l;
@@ -709,7 +709,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
               for (int i = 0; i < 32; ++i) o[i] = 0.f;
 #pragma unroll 2
               for (int k = 0; k < pc.n_pieces; ++k) {
-                const int slot = piece_slot(pc.ticket, k);
+                const int slot = piece_slot(pc, k);
                 const float2 x = __ldcg(p.part_ml + slot * 128 + row);
                 const float w = x.y == 0.f ? 0.f : fast_exp2(x.x - Mu);
                 const float4* src = p.part_o + ((size_t)slot * (kD / 4) + c0 / 4) * 128 + row;
@@ -811,7 +811,8 @@ static cudaError_t launch(const Params& p, int ctas, cudaStream_t stream) {
 }
 }  // namespace ptc
 
-size_t packed_tc_scratch_bytes(int d) { return (size_t)2 * kMaxPackedCtas * 128 * ((size_t)d * 4 + 8); }
+constexpr int kTcSlots = kMaxUnits > 2 * kMaxPackedCtas ? kMaxUnits : 2 * kMaxPackedCtas;
+size_t packed_tc_scratch_bytes(int d) { return (size_t)kTcSlots * 128 * ((size_t)d * 4 + 8); }
 
 cudaError_t launch_packed_tc(const samkv_packed_t& d, const Seqs& seqs, const KvSource& kv, const Rows& Q, float scale,
                              const Rows& O, float* lse, const samkv_ctx_impl& h, cudaStream_t stream) {
@@ -824,6 +825,7 @@ cudaError_t launch_packed_tc(const samkv_packed_t& d, const Seqs& seqs, const Kv
   p.cfg.tile = ptc::kBN;
   p.cfg.fixed = 2 * ptc::kBN;
   p.cfg.min_chunk = 6 * ptc::kBN;
+  p.cfg.wave_slots = (64LL << 20) / (d.head_dim * 4);        // K and V of half the L2 cache
   p.store_tokens = 32 % G == 0 ? 32 / G : 0;
   p.pages = kv.pages;
   p.paged = kv.paged;
@@ -841,7 +843,7 @@ cudaError_t launch_packed_tc(const samkv_packed_t& d, const Seqs& seqs, const Kv
   const int ctas = h.sm_count < kMaxPackedCtas ? h.sm_count : kMaxPackedCtas;
   char* ws = h.workspace + kStatusBytes;
   p.part_o = reinterpret_cast<float4*>(ws);
-  p.part_ml = reinterpret_cast<float2*>(ws + (size_t)2 * ctas * 128 * d.head_dim * 4);
+  p.part_ml = reinterpret_cast<float2*>(ws + (size_t)kTcSlots * 128 * d.head_dim * 4);
   p.d_status = h.d_status;
   p.Hq = d.n_q_heads;
   if (d.head_dim == 128)

@@ -556,3 +556,33 @@ def test_workspace_and_handle_refusals():
         B.samkv_paged_attn(h, p, B.Pages(c.Kp, c.Vp, c.table), c.cache_len, c.Q.float(), 0.0, True, O)
     with pytest.raises(ValueError):
         B.samkv_paged_attn(h, p, B.Pages(c.Kp, c.Vp, c.table), c.cache_len.long(), c.Q, 0.0, True, O)
+
+
+def test_chunks_over_keys_that_l2_cannot_hold():
+    """Several row tiles over more than 64 MB of keys run in waves of equal blocks; rows at the tiles' edges against the
+    64-bit form, the others against the contiguous layout of the same work (one KV head at a time), and twice bit for bit."""
+    for new, cached, Hq, Hkv in (([70, 1, 33], [60000, 300, 9000], 16, 2), ([300], [70001], 8, 2)):
+        c = PagedCase(new, cached, Hq, Hkv, 128, 64, "bf16", seed=63)
+        O, lse = run_paged(c)
+        O2, lse2 = run_paged(c)
+        assert torch.equal(O, O2) and torch.equal(lse, lse2)
+        q, o, l = f64(c.Q), f64(O), f64(lse)
+        at = 0
+        for s, n in enumerate(new):
+            length = cached[s] + n
+            rows = sorted({0, n // 2, n - 1, min(15, n - 1), min(16, n - 1)})
+            k, v = c.slots(c.Kp, s, length), c.slots(c.Vp, s, length)
+            ref = attend64(q[[at + r for r in rows]], k, v, cached[s] + np.array(rows) + 1, 128 ** -0.5)
+            check_rows(o[[at + r for r in rows]], l[[at + r for r in rows]], ref, "bf16", length, f"sequence {s}")
+            at += n
+        G = Hq // Hkv
+        one = PagedCase(new, cached, G, 1, 128, 64, "bf16", seed=63)
+        for h in range(Hkv):
+            one.Q = c.Q[:, h * G:(h + 1) * G].contiguous()
+            one.table = c.table
+            one.Kp, one.Vp = c.Kp[:, h:h + 1].contiguous(), c.Vp[:, h:h + 1].contiguous()
+            O1, lse1 = run_paged(one)
+            # both round the probabilities to 8 bits against other references: each is within its bound of the exact one
+            big = O1.abs().amax().float()
+            assert bool(((O1 - O[:, h * G:(h + 1) * G]).float().abs() <= 2.0 ** -6 * big).all())
+            assert bool((lse1 - lse[:, h * G:(h + 1) * G]).abs().le(1e-4).all())
