@@ -383,9 +383,9 @@ typedef struct {
 
 /* Bytes of workspace that samkv_prefill and samkv_paged_attn need in the handle they are called with (partial results
  * of key ranges that are split between CTAs; does not depend on the lengths).  0 on a bad description.  Such a handle is
- * made by samkv_create like any other; one workspace of the larger size serves both kinds of calls.  A captured graph
- * keeps using the workspace of the handle it was captured with: graphs that share a handle must not run at the same
- * time. */
+ * made by samkv_create like any other (whose memset of the workspace's first 256 bytes has to come before the first
+ * call in stream order); one workspace of the larger size serves both kinds of calls.  A captured graph keeps using the
+ * workspace of the handle it was captured with: graphs that share a handle must not run at the same time. */
 size_t samkv_packed_workspace_bytes(const samkv_packed_t* packed);
 
 /* Causal attention of whole prompts over themselves, e.g. of the documents whose caches the calls above take:

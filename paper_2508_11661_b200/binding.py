@@ -236,6 +236,8 @@ class Handle:
         self._h = ctypes.c_void_p()
         with torch.cuda.device(dev):
             _check(lib().samkv_create(ctypes.byref(self._h), dev, self.workspace.data_ptr(), nbytes), "samkv_create")
+            # the status block is cleared on the default stream: a first call on any other stream has to find it clear
+            torch.cuda.default_stream(dev).synchronize()
         return self
 
     def close(self):

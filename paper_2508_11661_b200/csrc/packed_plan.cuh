@@ -152,7 +152,7 @@ __device__ __forceinline__ void plan_block(const Seqs& q, const SplitCfg& c, Pla
       for (int s = s0; s < s1; ++s) {
         const Seq sq = load_seq(q, s);
         if (sq.n == 0) continue;
-        const int nt = (visible(q, sq, sq.n - 1) + c.tile - 1) / c.tile;
+        const int nt = max(1, (visible(q, sq, sq.n - 1) + c.tile - 1) / c.tile);
 #pragma unroll 1
         for (int k = 0; k < kWaveTries; ++k) {
           const int bt = (most + k) / (k + 1);
@@ -290,7 +290,8 @@ struct Walker {
         if (++s >= q.n_seq) return false;
         fetch(q, s);
         R = row_tiles(c, cur.n);
-        nb = R == 0 ? 0 : (visible(q, cur, cur.n - 1) + c.tile * wave_tiles - 1) / (c.tile * wave_tiles);
+        // (a sequence whose rows see nothing still gets its rows written)
+        nb = R == 0 ? 0 : max(1, (visible(q, cur, cur.n - 1) + c.tile * wave_tiles - 1) / (c.tile * wave_tiles));
       }
       int rest = unit - unit0;
       r = rest % R;

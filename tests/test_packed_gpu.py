@@ -586,3 +586,47 @@ def test_chunks_over_keys_that_l2_cannot_hold():
             big = O1.abs().amax().float()
             assert bool(((O1 - O[:, h * G:(h + 1) * G]).float().abs() <= 2.0 ** -6 * big).all())
             assert bool((lse1 - lse[:, h * G:(h + 1) * G]).abs().le(1e-4).all())
+
+
+def test_waves_with_a_sequence_that_sees_nothing():
+    """The layout in waves (see above) next to a sequence without cached tokens and no causal tail: its rows are empty."""
+    c = PagedCase([300, 5, 0], [70001, 0, 12], 8, 2, 128, 64, "bf16", seed=64)
+    O, lse = run_paged(c, causal=False)
+    assert bool((O[300:] == 0).all()) and bool((lse[300:] == -math.inf).all())
+    q, k, v = f64(c.Q)[:2], c.slots(c.Kp, 0, 70001), c.slots(c.Vp, 0, 70001)
+    check_rows(f64(O)[:2], f64(lse)[:2], attend64(q, k, v, [70001, 70001], 128 ** -0.5), "bf16", 70001)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_the_hint_never_changes_what_is_computed(dtype):
+    c = PagedCase([40, 1, 9], [100, 33, 5000], 8, 2, 128, 32, dtype, seed=65)
+    for hint in (0, 1, 3, 40, 1000):
+        O, lse = run_paged(c, max_seq=hint)
+        check_paged(c, O, lse)
+
+
+def test_first_call_of_a_fresh_handle_on_a_side_stream():
+    """Split work right after the handle was made, on a stream that the default stream does not order."""
+    c = PagedCase([1], [9001], 8, 1, 128, 64, "bf16", seed=66)
+    ref, _ = run_paged(c)
+    junk = [torch.full((8 << 20,), 255, dtype=torch.uint8, device=DEV) for _ in range(8)]
+    torch.cuda.synchronize()
+    del junk                                             # whatever the allocator hands out next is not zero
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        O, _ = run_paged(c)
+    torch.cuda.synchronize()
+    assert torch.equal(O, ref)
+
+
+def test_overlapping_offsets_and_foreign_rows_are_reported():
+    """Offsets that run backwards are clamped and reported; rows before the first sequence are not touched."""
+    c = PagedCase([10, 20], [64, 64], 4, 2, 64, 16, "bf16", seed=67)
+    p = B.Packed(4, 2, 64, torch.tensor([6, 10, 8], dtype=torch.int32, device=DEV), c.T)
+    h = B.Handle.for_packed(p)
+    O = torch.full_like(c.Q, 7.0)
+    B.samkv_paged_attn(h, p, B.Pages(c.Kp, c.Vp, c.table), c.cache_len, c.Q, 0.0, True, O)
+    assert B.samkv_poll_status(h) == 7
+    assert bool((O[:6] == 7.0).all()) and bool((O[10:] == 7.0).all()) and not bool((O[6:10] == 7.0).any())
+    B.samkv_paged_attn(h, p, B.Pages(c.Kp, c.Vp, c.table), c.cache_len, c.Q, 0.0, True, O)
+    assert B.samkv_poll_status(h) == 7 and B.samkv_poll_status(h) == 0
