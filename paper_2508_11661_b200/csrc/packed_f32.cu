@@ -22,7 +22,8 @@ struct Smem {
   static constexpr int kTile = kBN * kLd * 4;
   static constexpr int kQ = 0;
   static constexpr int kKv = kRows * kLd * 4;            // [2][K, V]; P takes K's place once the scores are done
-  static constexpr int kPiece = kKv + 4 * kTile;
+  static constexpr int kP = kKv + 4 * kTile;             // 16-row tiles: scores and weights, rescaling factors
+  static constexpr int kPiece = kP + (kRows == 16 ? 16 * kPLd * 4 + 64 : 0);
   static constexpr int kBytes = kPiece + 128;
 };
 
@@ -89,9 +90,11 @@ packed_f32_kernel(const __grid_constant__ pf32::Params p) {
     auto load_kv = [&](int t, int st) {
       const int j0 = t * kBN;
       const uint32_t dk = smem + L::kKv + st * 2 * L::kTile, dv = dk + L::kTile;
+      // a thread keeps its 16-byte column and steps through the rows
+      constexpr int kLanes = kD / 4, kStep = kThreads / kLanes;
+      const int c = tid % kLanes, r0 = tid / kLanes;
 #pragma unroll 4
-      for (int i = tid; i < kBN * (kD / 4); i += kThreads) {
-        const int r = i / (kD / 4), c = i % (kD / 4);
+      for (int r = r0; r < kBN; r += kStep) {
         const bool ok = j0 + r < pc.seen;                // slots that no row sees read as zero
         size_t ko = 0, vo = 0;
         if (ok) {
@@ -128,6 +131,148 @@ packed_f32_kernel(const __grid_constant__ pf32::Params p) {
 #pragma unroll
       for (int c = 0; c < kC * 4; ++c) o[i][c] = 0.f;
     }
+    if constexpr (kRows == 16) {
+      // Few rows: a thread owns 4 rows x 4 slots over a quarter of the head dimension, then 4 rows x 4 columns over half
+      // (d = 128) or a quarter (d = 64) of the slots, so that it still has 64 multiply-adds for 8 vectors read; the scores
+      // pass through shared memory in between.
+      const int lane = tid & 31, rg = (warp & 3) * 4;
+      const int ds = lane & 3, kg = (warp >> 2) * 8 + (lane >> 2);
+      constexpr int kColLanes = kD / 4, kSplits = 256 / (4 * kColLanes);
+      const int c4 = (lane & (kColLanes - 1)) * 4, split = (warp >> 2) * (32 / kColLanes) + lane / kColLanes;
+      float* sP = reinterpret_cast<float*>(smem_raw + L::kP);
+      float* sCorr = sP + 16 * kPLd;
+      const int my_vis = visible(p.seqs, sq, min(pc.r * p.cfg.tokens + (rg + ds) / G, last_tok));
+      int row_vis[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) row_vis[i] = visible(p.seqs, sq, min(pc.r * p.cfg.tokens + (rg + i) / G, last_tok));
+      float acc[4][4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
+#pragma unroll 1
+      for (int t = pc.tile0; t < pc.tile1; ++t) {
+        const int st = (t - pc.tile0) & 1, j0 = t * kBN;
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        __syncthreads();                                 // tile t is there, and tile t - 1 is used up
+        if (t + 1 < pc.tile1) load_kv(t + 1, st ^ 1);
+        // ---- scores ----
+        float s[4][4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[i][0] = s[i][1] = s[i][2] = s[i][3] = 0.f;
+        const float *k = sK(st) + kg * kLd + ds * 4, *q = sQ + rg * kLd + ds * 4;
+#pragma unroll 2
+        for (int e = 0; e < kD; e += 16) {
+          float4 kv[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) kv[j] = lds4(k + j * 16 * kLd + e);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float4 a = lds4(q + i * kLd + e);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              s[i][j] = fmaf(a.x, kv[j].x, s[i][j]);
+              s[i][j] = fmaf(a.y, kv[j].y, s[i][j]);
+              s[i][j] = fmaf(a.z, kv[j].z, s[i][j]);
+              s[i][j] = fmaf(a.w, kv[j].w, s[i][j]);
+            }
+          }
+        }
+        // the quarters are added up; lane ds keeps row rg + ds
+        const bool hi = ds & 2, lo = ds & 1;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float a = (hi ? s[2][j] : s[0][j]) + __shfl_xor_sync(0xffffffffu, hi ? s[0][j] : s[2][j], 2);
+          const float b = (hi ? s[3][j] : s[1][j]) + __shfl_xor_sync(0xffffffffu, hi ? s[1][j] : s[3][j], 2);
+          const float x = (lo ? b : a) + __shfl_xor_sync(0xffffffffu, lo ? a : b, 1);
+          sP[(rg + ds) * kPLd + kg + 16 * j] = j0 + kg + 16 * j < my_vis ? x * p.scale : -INFINITY;
+        }
+        __syncthreads();
+        // ---- online softmax: 16 threads per row ----
+        {
+          float x[4], mx = -INFINITY;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            x[j] = sP[ty * kPLd + tx + 16 * j];
+            mx = fmaxf(mx, x[j]);
+          }
+#pragma unroll
+          for (int o2 = 8; o2 > 0; o2 >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o2));
+          const float mn = fmaxf(m[0], mx), mu = mn == -INFINITY ? 0.f : mn;
+          const float corr = m[0] == mn ? 1.f : expf(m[0] - mu);
+          m[0] = mn;
+          l[0] *= corr;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            x[j] = expf(x[j] - mu);
+            l[0] += x[j];                                // (this thread's slots; joined at the end)
+            sP[ty * kPLd + tx + 16 * j] = x[j];
+          }
+          if (tx == 0) sCorr[ty] = corr;
+        }
+        __syncthreads();
+        // ---- result ----
+        const bool edge = j0 + kBN > pc.seen0;           // some row does not see some slot: zero weights times what it holds
+        constexpr int kSlots = kBN / kSplits;
+        const float *v = sV(st) + split * kSlots * kLd + c4, *pr = sP + rg * kPLd + split * kSlots;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float corr = sCorr[rg + i];
+#pragma unroll
+          for (int c = 0; c < 4; ++c) acc[i][c] *= corr;
+        }
+        if (!edge) {
+#pragma unroll 2
+          for (int j = 0; j < kSlots; j += 4) {
+            float4 a[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) a[i] = lds4(pr + i * kPLd + j);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+              const float4 b = lds4(v + (j + u) * kLd);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const float w2 = u == 0 ? a[i].x : u == 1 ? a[i].y : u == 2 ? a[i].z : a[i].w;
+                acc[i][0] = fmaf(w2, b.x, acc[i][0]);
+                acc[i][1] = fmaf(w2, b.y, acc[i][1]);
+                acc[i][2] = fmaf(w2, b.z, acc[i][2]);
+                acc[i][3] = fmaf(w2, b.w, acc[i][3]);
+              }
+            }
+          }
+        } else {
+#pragma unroll 1
+          for (int j = 0; j < kSlots; ++j) {
+            const float4 b = lds4(v + j * kLd);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float w2 = pr[i * kPLd + j];
+              if (j0 + split * kSlots + j < row_vis[i]) {
+                acc[i][0] = fmaf(w2, b.x, acc[i][0]);
+                acc[i][1] = fmaf(w2, b.y, acc[i][1]);
+                acc[i][2] = fmaf(w2, b.z, acc[i][2]);
+                acc[i][3] = fmaf(w2, b.w, acc[i][3]);
+              }
+            }
+          }
+        }
+      }
+      // the splits' parts through shared memory into the layout below
+      __syncthreads();
+      float* part = sK(0);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<float4*>(part + (split * 16 + rg + i) * kD + c4) = make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
+      __syncthreads();
+#pragma unroll
+      for (int c = 0; c < kC; ++c)
+#pragma unroll
+        for (int x = 0; x < kSplits; ++x) {
+          const float4 y = lds4(part + (x * 16 + ty) * kD + c * 64 + tx * 4);
+          o[0][c * 4] += y.x;
+          o[0][c * 4 + 1] += y.y;
+          o[0][c * 4 + 2] += y.z;
+          o[0][c * 4 + 3] += y.w;
+        }
+    } else {
 #pragma unroll 1
     for (int t = pc.tile0; t < pc.tile1; ++t) {
       const int st = (t - pc.tile0) & 1, j0 = t * kBN;
@@ -214,6 +359,7 @@ packed_f32_kernel(const __grid_constant__ pf32::Params p) {
           }
         }
       }
+    }
     }
 #pragma unroll
     for (int i = 0; i < kR; ++i)
