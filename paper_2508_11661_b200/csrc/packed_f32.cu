@@ -3,7 +3,7 @@
 //
 // Persistent, one CTA of 256 threads per SM, work divided by packed_plan.cuh.  Row tiles of 64 packed rows (16 when every
 // sequence has at most 16 per KV head, so that decode is not spent on rows that do not exist), key tiles of 64 slots,
-// double-buffered with cp.async.  A thread owns kRows/16 rows x 4 slots of the scores and the same rows x d/16 columns of
+// two to four of them in shared memory with cp.async.  A thread owns kRows/16 rows x 4 slots of the scores and the same rows x d/16 columns of
 // the result: per 64 multiply-adds of the score product it reads 4 + 4 vectors of 16 bytes, so the FMA pipe and shared
 // memory are about level.  The 16 threads of a row agree on maxima and sums by shuffles.
 #include <math.h>
@@ -21,8 +21,10 @@ struct Smem {
   static constexpr int kPLd = kBN + 4;
   static constexpr int kTile = kBN * kLd * 4;
   static constexpr int kQ = 0;
-  static constexpr int kKv = kRows * kLd * 4;            // [2][K, V]; P takes K's place once the scores are done
-  static constexpr int kP = kKv + 4 * kTile;             // 16-row tiles: scores and weights, rescaling factors
+  static constexpr int kKv = kRows * kLd * 4;            // [kStages][K, V]; P takes K's place once the scores are done
+  // tiles in shared memory: as many as fit, since a short tile is done before the next one has come
+  static constexpr int kStages = kD == 64 ? 4 : kRows == 64 ? 2 : 3;
+  static constexpr int kP = kKv + kStages * 2 * kTile;             // 16-row tiles: scores and weights, rescaling factors
   static constexpr int kPiece = kP + (kRows == 16 ? 16 * kPLd * 4 + 64 : 0);
   static constexpr int kBytes = kPiece + 128;
 };
@@ -108,7 +110,6 @@ packed_f32_kernel(const __grid_constant__ pf32::Params p) {
         cp_async16(dk + (r * kLd + c * 4) * 4, static_cast<const float*>(p.K.data) + ko, ok);
         cp_async16(dv + (r * kLd + c * 4) * 4, static_cast<const float*>(p.V.data) + vo, ok);
       }
-      asm volatile("cp.async.commit_group;" ::: "memory");
     };
 #pragma unroll 2
     for (int i = tid; i < kRows * (kD / 4); i += kThreads) {
@@ -117,7 +118,12 @@ packed_f32_kernel(const __grid_constant__ pf32::Params p) {
       const size_t off = ok ? (size_t)(tok0 + r / G) * p.Q.ts + (size_t)(pc.h * G + r % G) * p.Q.hs + c * 4 : 0;
       cp_async16(smem + L::kQ + (r * kLd + c * 4) * 4, static_cast<const float*>(p.Q.data) + off, ok);
     }
-    load_kv(pc.tile0, 0);
+    // (the last stage is filled from the loop on)
+#pragma unroll 1
+    for (int i = 0; i < L::kStages - 1; ++i) {
+      if (pc.tile0 + i < pc.tile1) load_kv(pc.tile0 + i, i);
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    }
     Seq sq;
     sq.first = pc.first; sq.n = pc.n; sq.base = pc.base;
     const int last_tok = min((pc.r + 1) * p.cfg.tokens, pc.n) - 1;
@@ -150,10 +156,11 @@ packed_f32_kernel(const __grid_constant__ pf32::Params p) {
       for (int i = 0; i < 4; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
 #pragma unroll 1
       for (int t = pc.tile0; t < pc.tile1; ++t) {
-        const int st = (t - pc.tile0) & 1, j0 = t * kBN;
-        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        const int st = (t - pc.tile0) % L::kStages, j0 = t * kBN;
+        asm volatile("cp.async.wait_group %0;" ::"n"(L::kStages - 2) : "memory");
         __syncthreads();                                 // tile t is there, and tile t - 1 is used up
-        if (t + 1 < pc.tile1) load_kv(t + 1, st ^ 1);
+        if (t + L::kStages - 1 < pc.tile1) load_kv(t + L::kStages - 1, (t - pc.tile0 + L::kStages - 1) % L::kStages);
+        asm volatile("cp.async.commit_group;" ::: "memory");
         // ---- scores ----
         float s[4][4];
 #pragma unroll
@@ -275,10 +282,11 @@ packed_f32_kernel(const __grid_constant__ pf32::Params p) {
     } else {
 #pragma unroll 1
     for (int t = pc.tile0; t < pc.tile1; ++t) {
-      const int st = (t - pc.tile0) & 1, j0 = t * kBN;
-      asm volatile("cp.async.wait_group 0;" ::: "memory");
+      const int st = (t - pc.tile0) % L::kStages, j0 = t * kBN;
+      asm volatile("cp.async.wait_group %0;" ::"n"(L::kStages - 2) : "memory");
       __syncthreads();                                   // tile t is there, and tile t - 1 is used up
-      if (t + 1 < pc.tile1) load_kv(t + 1, st ^ 1);
+      if (t + L::kStages - 1 < pc.tile1) load_kv(t + L::kStages - 1, (t - pc.tile0 + L::kStages - 1) % L::kStages);
+      asm volatile("cp.async.commit_group;" ::: "memory");
       // ---- scores ----
       float s[kR][4];
 #pragma unroll
