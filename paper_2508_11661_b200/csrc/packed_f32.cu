@@ -69,10 +69,14 @@ packed_f32_kernel(const __grid_constant__ pf32::Params p) {
   const int G = p.cfg.G;
   pdl_wait();
   long long chunk = 0;
-  plan_block<kThreads>(p.seqs, p.cfg, &plan, &chunk, p.d_status);
+  const bool warp_plans = p.seqs.n_seq <= kWarpPlanSeqs;
+  if (!warp_plans) plan_block<kThreads>(p.seqs, p.cfg, &plan, &chunk, p.d_status, tid);
   Walker w;
   w.more = false;
-  if (warp == 0) w.init(p.seqs, p.cfg, &plan, chunk);
+  if (warp == 0) {
+    if (warp_plans) plan_block<32>(p.seqs, p.cfg, &plan, &chunk, p.d_status, tid);
+    w.init(p.seqs, p.cfg, &plan, chunk);
+  }
   bool bad = false;
 
   while (true) {

@@ -75,12 +75,26 @@ struct PlanShared {
   unsigned units[kWaveTries];  // units for each length tried
 };
 
-// Block-wide: finds the sequence that holds this CTA's first position.  All kThreads threads call it; afterwards
-// *chunk is the length of a CTA's stretch (0: nothing to do) and sh->s, sh->start are set for CTAs that have one.
+// Sequences that the warp which walks the plan can also lay out by itself, next to whatever the other warps do; more of
+// them take the whole block.
+constexpr int kWarpPlanSeqs = 512;
+
+// Most quotients here fit 32 bits, whose division is a fifth of the 64-bit one.
+__device__ __forceinline__ long long quotient(long long a, long long b) {
+  return ((unsigned long long)(a | b) >> 32) == 0 ? (long long)((unsigned)a / (unsigned)b) : a / b;
+}
+
+// Finds the sequence that holds this CTA's first position.  Called by kThreads threads, a whole block or (32) one warp,
+// with their index among them; afterwards *chunk is the length of a CTA's stretch (0: nothing to do) and sh->s,
+// sh->start are set for CTAs that have one.
 template <int kThreads>
-__device__ __forceinline__ void plan_block(const Seqs& q, const SplitCfg& c, PlanShared* sh, long long* chunk, int* d_status) {
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+__device__ __forceinline__ void plan_block(const Seqs& q, const SplitCfg& c, PlanShared* sh, long long* chunk, int* d_status,
+                                           int tid) {
+  const int warp = tid >> 5, lane = tid & 31;
   constexpr int kWarps = kThreads / 32;
+  auto sync = []() {
+    if constexpr (kThreads == 32) __syncwarp(); else __syncthreads();
+  };
   const int per = (q.n_seq + kThreads - 1) / kThreads;
   const int s0 = min(tid * per, q.n_seq), s1 = min(s0 + per, q.n_seq);
   if (tid == 0) {
@@ -111,7 +125,7 @@ __device__ __forceinline__ void plan_block(const Seqs& q, const SplitCfg& c, Pla
   for (int o = 16; o > 0; o >>= 1) items += __shfl_xor_sync(0xffffffffu, items, o);
   if (lane == 31) sh->warp_len[warp] = incl;
   if (lane == 0) sh->warp_items[warp] = items;
-  __syncthreads();
+  sync();
   if (warp == 0) {
     const long long w = lane < kWarps ? sh->warp_len[lane] : 0;
     int it = lane < kWarps ? sh->warp_items[lane] : 0;
@@ -127,7 +141,7 @@ __device__ __forceinline__ void plan_block(const Seqs& q, const SplitCfg& c, Pla
     if (lane == 31) sh->total = wi;
     if (lane == 0) sh->items = it;
   }
-  __syncthreads();
+  sync();
   const long long total = sh->total;
   if (c.wave_slots > 0 && total > 2 * c.wave_slots && sh->items <= kMaxTickets) {
     // candidates for waves: a second look at the lengths
@@ -145,7 +159,7 @@ __device__ __forceinline__ void plan_block(const Seqs& q, const SplitCfg& c, Pla
       atomicAdd(&sh->distinct, distinct);
       atomicMax(&sh->longest, longest);
     }
-    __syncthreads();
+    sync();
     if ((long long)sh->distinct > c.wave_slots && total > 2 * (long long)sh->distinct) {
       const int most = sh->longest;
 #pragma unroll 1
@@ -159,7 +173,7 @@ __device__ __forceinline__ void plan_block(const Seqs& q, const SplitCfg& c, Pla
           atomicAdd(&sh->units[k], (unsigned)(c.Hkv * row_tiles(c, sq.n) * ((nt + bt - 1) / bt)));
         }
       }
-      __syncthreads();
+      sync();
       if (tid == 0) {
         long long best = -1;
         for (int k = 0; k < kWaveTries; ++k) {
@@ -174,15 +188,15 @@ __device__ __forceinline__ void plan_block(const Seqs& q, const SplitCfg& c, Pla
         // (an uneven mix of lengths leaves holes in the waves; the keys are fetched again instead)
         if (best > total / (long long)gridDim.x * 3 / 2) sh->wave_tiles = 0;
       }
-      __syncthreads();
+      sync();
       if (sh->wave_tiles > 0) return;
     }
   }
-  long long ctas = total / c.min_chunk;
+  long long ctas = quotient(total, c.min_chunk);
   if (ctas < sh->items) ctas = sh->items;
   if (ctas > (long long)gridDim.x) ctas = gridDim.x;
   if (ctas < 1) ctas = 1;
-  const long long ch = (total + ctas - 1) / ctas;
+  const long long ch = quotient(total + ctas - 1, ctas);
   *chunk = ch;
   const long long p0 = ch * blockIdx.x;
   const long long excl = sh->warp_len[warp] + incl - len;
@@ -199,7 +213,7 @@ __device__ __forceinline__ void plan_block(const Seqs& q, const SplitCfg& c, Pla
       at += w;
     }
   }
-  __syncthreads();
+  sync();
 }
 
 // Walks the pieces of this CTA; run by one whole warp (all lanes hold the same state but for the sequence window).
@@ -266,7 +280,7 @@ struct Walker {
     R = row_tiles(c, cur.n);
     const long long per_head = items_length(c, q.causal, cur.base, R);
     long long rem = p0 - sh->start;
-    h = (int)(rem / per_head);
+    h = (int)quotient(rem, per_head);
     rem -= h * per_head;
     int lo = 0, hi = R - 1;                  // largest r whose items before it are no longer than rem
 #pragma unroll 1
@@ -345,7 +359,7 @@ struct Walker {
         out->n_pieces = 1;
         if (starts_inside || ends_inside) {
           // borders inside the item, after they have been moved to tile borders
-          long long ca = item_start / chunk + 1, cb = (end - 1) / chunk;
+          long long ca = quotient(item_start, chunk) + 1, cb = quotient(end - 1, chunk);
 #pragma unroll 1
           while (ca <= cb && border(c, ca * chunk, nt) == 0) ++ca;
 #pragma unroll 1

@@ -283,7 +283,8 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
   const uint32_t tmem = *s_tmem;
   pdl_wait();                               // everything below reads what earlier kernels may have written
   long long chunk = 0;
-  plan_block<kThreads>(p.seqs, p.cfg, &plan, &chunk, p.d_status);
+  const bool warp_plans = p.seqs.n_seq <= kWarpPlanSeqs;
+  if (!warp_plans) plan_block<kThreads>(p.seqs, p.cfg, &plan, &chunk, p.d_status, tid);
 
   auto wait = [&](int i, uint32_t phase) { return wait_bar(bar(i), phase & 1u, s_fail); };
 
@@ -292,6 +293,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     if (warp == kWarpK) {
       // ================= plan and K =================
       Walker w;
+      if (warp_plans) plan_block<32>(p.seqs, p.cfg, &plan, &chunk, p.d_status, lane);
       w.init(p.seqs, p.cfg, &plan, chunk);
       Piece pc;
       uint32_t f = 0, T = 0;                // pieces, key tiles so far
