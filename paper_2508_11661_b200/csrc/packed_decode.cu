@@ -6,6 +6,9 @@
 // latency of HBM.  Eight consumer warps: tile T belongs to the four warps of parity T & 1, 16 slots each.  A warp runs
 // its own online softmax over its slots on mma.sync m16n8k16 (16 rows fill one instruction; tcgen05's 128 rows would
 // not), so warps exchange nothing until a piece ends; then the eight (m, l, O) are merged through shared memory.
+// 32 requests over 20480 slots, 32/8 heads of 128: 0.403 ms, 6.67 TB/s, the rate of a plain copy (1.03 of the measured
+// one); one request over 102400 slots, 64/8 heads: 76 us, 5.5 TB/s (start-up, the ring's first fill and the merge of 19
+// pieces per KV head are about 12 us of it).  The tensor-memory kernel takes 0.50 ms and 107 us for the same calls.
 // Every wait is bounded; a wait that runs out ends the others and is recorded as a device check.
 #include "packed_plan.cuh"
 #include "tc_common.cuh"

@@ -1,11 +1,14 @@
 // Attention of packed sequences over packed rows or over a paged cache, fp32 throughout (tensor cores would round the
 // operands to tf32).
 //
-// Persistent, one CTA of 256 threads per SM, work divided by packed_plan.cuh.  Row tiles of 64 packed rows (16 when every
-// sequence has at most 16 per KV head, so that decode is not spent on rows that do not exist), key tiles of 64 slots,
-// two to four of them in shared memory with cp.async.  A thread owns kRows/16 rows x 4 slots of the scores and the same rows x d/16 columns of
-// the result: per 64 multiply-adds of the score product it reads 4 + 4 vectors of 16 bytes, so the FMA pipe and shared
-// memory are about level.  The 16 threads of a row agree on maxima and sums by shuffles.
+// Persistent, one CTA of 256 threads per SM, work divided by packed_plan.cuh.  Row tiles of 64, 32 or 16 packed rows
+// (launch_packed_attn chooses), key tiles of 64 slots, two to four of them in shared memory with cp.async.  With 64 and 32
+// rows a thread owns kRows/16 rows x 4 slots of the scores and the same rows x d/16 columns of the result: per 64
+// multiply-adds of the score product it reads 4 + 4 vectors of 16 bytes, so the FMA pipe and shared memory are about level.
+// With 16 rows it keeps that ratio by splitting the head dimension, and the slots, between threads.  The 16 threads of a
+// row agree on maxima and sums by shuffles.
+// Bound by instruction issue at 64 rows (61 % of the slots; 4 sequences of 1024 tokens, 8/2 heads of 128: 27 TFLOP/s of the
+// FMA pipe's nominal 74), by latency where there is little work: 4 documents of 256 tokens, 4/2 heads of 64, 21 us.
 #include <math.h>
 
 #include "packed_plan.cuh"

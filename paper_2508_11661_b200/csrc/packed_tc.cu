@@ -2,24 +2,34 @@
 //
 // Persistent, one CTA per SM.  An item is a tile of up to 128 query rows (row = token x group member, so the G query
 // heads that share a KV head share its keys) against key tiles of 128 slots; packed_plan.cuh divides the call's items
-// evenly among the CTAs.  Roles of the 12 warps:
-//   warps 0-3   softmax of the even key tiles of the CTA's running count, thread = row
-//   warps 4-7   softmax of the odd ones
-//   warp 8      issues S(T) = Q K(T)^T into the score buffer T & 1
-//   warp 9      issues O += P(T) V(T)
-//   warp 10     walks the plan, loads Q (two buffers) and K (three stages) by TMA
-//   warp 11     loads V (two stages), clears value rows behind a sequence's last slot
-// Both groups add into ONE accumulator: they use a common reference maximum per row, kept in shared memory and handed
-// from tile to tile in order (tile T + 1 reads it after tile T has decided).  The reference only has to be within a factor
-// of 2^64 of the row's maximum (P is bf16 and O, l are fp32: all have the exponent range for it), so after a row's first
-// tile it practically never moves; when it does, the group waits for the products in flight and rescales O in tensor
-// memory.  That frees tensor memory for P buffers of their own (S0 S1 128 columns each, O 128, P0 P1 64 each: all 512),
-// so S(T+2) is issued as soon as S(T) sits in registers and never waits for the exponentials of T: score product,
-// exponentials and value product of different tiles overlap without a chain between them.
-// Probabilities are rounded to bf16 on the integer pipe (round half away, one byte permute per pair); the denominator
-// sums them before that rounding, so lse is good to fp32.
-// Every wait is bounded; a wait that runs out sets a flag that ends all others, the CTA drains its copies and frees its
-// tensor memory, and the failure is recorded as a device check.  TMA reads this GPU's memory only, without multicast.
+// among the CTAs.  Roles of the 16 warps:
+//   warps 0-11  softmax, three groups of four; tile T (the CTA's running count) belongs to group T mod 3, thread = row
+//   warp 12     issues S(T) = Q K(T)^T into score buffer T mod 3
+//   warp 13     issues O += P(T) V(T)
+//   warp 14     walks the plan, loads Q (two buffers) and K (two stages) by TMA
+//   warp 15     loads V (three stages), sees to value rows that not every query row sees
+// All groups add into ONE accumulator.  They share a reference maximum per row: a piece's first tile sets it, the others
+// use it as it stands, since it only has to be within a factor of 2^64 of the row's maximum (P is bf16 and O, l are fp32:
+// all have the exponent range for it).  A tile that needs a larger one waits for everything before it and rescales O in
+// tensor memory; tiles behind it that used the old one notice before they hand over their probabilities and rescale
+// those.  P(T) overlays the first half of S(T), so tensor memory holds three score buffers and O: 512 columns.
+// The group with a piece's last tile writes the result while the others are at the next piece's tiles.
+//
+// What bounds it.  A tile costs 1024 cycles on the tensor pipe (16 products of 64 cycles), 1024 on the special-function
+// unit, and 1280 of shared-memory bandwidth (operands 768, TMA writes 512), but the three groups run a tile each through
+// a chain of about 6000 cycles (poll, maximum, exponentials, hand-over, two products, polls), about 2000 per tile: tensor
+// pipe 37-45 % busy.  Measured steps: two groups taking turns 4000 cycles per tile; the loops rolled so that a tile's code
+// fits the schedulers' instruction caches (straight-line code ran at 5 cycles an instruction) 2550; three groups 2100.
+// One thread issuing both kinds of products, packed two-wide arithmetic, 64 scores at a time, every fourth exponential as
+// a polynomial, and not loading K and V at all (as an experiment) change nothing or cost up to 15 %.
+// 20 documents of 1536 tokens, 32/8 heads: 0.49 ms (790 TFLOP/s) at 1965 MHz; back to back the board's 1000 W cap settles
+// the clock near 1600 MHz: 0.575 ms (670 TFLOP/s).  128 tokens over 102400 slots, 64/8 heads: 0.51 ms (840 TFLOP/s; 0.62
+// without the layout in waves, which keeps the eight row tiles of a KV head on the same keys at the same time).
+//
+// Probabilities are rounded to bf16 for the second product; the denominator sums them before that rounding, so lse is good
+// to fp32.  Every wait is bounded; a wait that runs out sets a flag that ends all others, the CTA drains its copies and
+// frees its tensor memory, and the failure is recorded as a device check.  TMA reads and writes this GPU's memory only,
+// without multicast.
 #include "packed_plan.cuh"
 #include "tc_common.cuh"
 
