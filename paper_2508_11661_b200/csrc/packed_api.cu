@@ -64,15 +64,21 @@ samkv_status_t make_rope(const samkv_packed_t& p, const samkv_rope_t* r, RopeTab
   if (r->rot_dim < 16 || r->rot_dim > p.head_dim || r->rot_dim % 16 != 0) return SAMKV_ERR_INVALID_ARG;
   if (r->inv_freq == nullptr && !(r->base > 0.0 && isfinite(r->base))) return SAMKV_ERR_INVALID_ARG;
   const long double two_pi = 6.283185307179586476925286766559005768L;
-  // base^(-2i/rot_dim) as powers of one ratio: a call pays for one power, and 63 products in 64-bit mantissas lose 2^-58
-  const long double ratio = r->inv_freq != nullptr ? 0.0L : powl((long double)r->base, -2.0L / r->rot_dim);
-  long double power = 1.0L;
-  for (int i = 0; i < r->rot_dim / 2; ++i, power *= ratio) {
-    if (r->inv_freq != nullptr && !isfinite(r->inv_freq[i])) return SAMKV_ERR_INVALID_ARG;
-    long double turn = (r->inv_freq != nullptr ? (long double)r->inv_freq[i] : power) / two_pi;
-    turn -= floorl(turn);                                          // whole turns of a position change nothing
-    const long double scaled = roundl(ldexpl(turn, 64));
-    out->turn[i] = scaled >= 18446744073709551616.0L ? 0ull : (unsigned long long)scaled;
+  if (r->inv_freq == nullptr) {
+    // base^(-2i/rot_dim) as powers of one ratio: a call pays for one power, and 63 products in 64-bit mantissas lose 2^-58.
+    // A base below 1 turns faster than once in 2 pi; its turns are reduced like given ones.
+    const long double ratio = powl((long double)r->base, -2.0L / r->rot_dim), unit = 18446744073709551616.0L / two_pi;
+    long double power = unit;
+    for (int i = 0; i < r->rot_dim / 2; ++i, power *= ratio)
+      out->turn[i] = (unsigned long long)((power < 18446744073709551616.0L ? power : fmodl(power, 18446744073709551616.0L)) + 0.5L);
+  } else {
+    for (int i = 0; i < r->rot_dim / 2; ++i) {
+      if (!isfinite(r->inv_freq[i])) return SAMKV_ERR_INVALID_ARG;
+      long double turn = (long double)r->inv_freq[i] / two_pi;
+      turn -= floorl(turn);                                        // whole turns of a position change nothing
+      const long double scaled = roundl(ldexpl(turn, 64));
+      out->turn[i] = scaled >= 18446744073709551616.0L ? 0ull : (unsigned long long)scaled;
+    }
   }
   out->rot_dim = r->rot_dim;
   out->interleaved = r->interleaved != 0;
