@@ -1,14 +1,20 @@
 // Attention of packed sequences over packed rows or over a paged cache, fp32 throughout (tensor cores would round the
 // operands to tf32).
 //
-// Persistent, one CTA of 256 threads per SM, work divided by packed_plan.cuh.  Row tiles of 64, 32 or 16 packed rows
-// (launch_packed_attn chooses), key tiles of 64 slots, two to four of them in shared memory with cp.async.  With 64 and 32
-// rows a thread owns kRows/16 rows x 4 slots of the scores and the same rows x d/16 columns of the result: per 64
-// multiply-adds of the score product it reads 4 + 4 vectors of 16 bytes, so the FMA pipe and shared memory are about level.
-// With 16 rows it keeps that ratio by splitting the head dimension, and the slots, between threads.  The 16 threads of a
-// row agree on maxima and sums by shuffles.
-// Bound by instruction issue at 64 rows (61 % of the slots; 4 sequences of 1024 tokens, 8/2 heads of 128: 27 TFLOP/s of the
-// FMA pipe's nominal 74), by latency where there is little work: 4 documents of 256 tokens, 4/2 heads of 64, 21 us.
+// Persistent, one CTA of 256 threads per SM, work divided by packed_plan.cuh, key tiles of 64 slots, two to four of them in
+// shared memory with cp.async.  Multiply-adds are issued two at a time (fma.rn.f32x2: the same roundings, half the issue
+// slots).  Row tiles of 64, 32 or 8 packed rows; launch_packed_attn chooses.
+//   64 and 32 rows: a thread owns kRows/16 rows x 4 slots of the scores and the same rows x d/16 columns of the result.
+//     The 16 threads of a row agree on maxima and sums by shuffles.
+//   8 rows: each warp takes 8 slots of every tile, loads them itself and runs its own online softmax, so that nothing in
+//     the loop waits for another warp; the eight results are joined when a piece ends.  A thread keeps 8 rows x 8 elements
+//     of Q in registers, reads a slot's key once, and the d / 8 threads of a slot are added up by shuffles that leave each
+//     with a row of its own; for the result it owns 8 rows x 4 columns.
+// Measured: prompts of 1024 and 700 tokens, 32/8 heads of 128, 64 rows: 538 us, 30 TFLOP/s of the FMA pipe's nominal 74 (two
+// warps per scheduler issue 0.45 instructions a cycle: dependent chains and shared memory).  Decode, 32 requests x 1000
+// slots, 32/8 heads of 128, 8 rows: 55 us, 4.9 TB/s (138 us when the CTA shared tiles of 16 rows).  Little work is latency:
+// an item costs about 2.5 us besides its tiles; 6 sequences of 1 to 64 tokens, 4/2 heads of 64: 17 us (22 us with 16 rows).
+// Starting the next item's loads before the results leave made every shape 4 to 8 % slower (the code grew), so it is not done.
 #include <math.h>
 
 #include "packed_plan.cuh"
@@ -20,16 +26,21 @@ constexpr int kBN = 64, kThreads = 256;
 
 template <int kD, int kRows>
 struct Smem {
-  static constexpr int kLd = kD + 4;                     // row stride in floats: rows 16 bytes apart in their banks
-  static constexpr int kPLd = kBN + 4;
+  static constexpr bool kFew = kRows == 8;
+  static constexpr int kLd = kFew ? kD : kD + 4;         // row stride in floats: 16 bytes on in the banks, or rows read whole
+  static constexpr int kPLd = kFew ? 12 : kBN + 4;
   static constexpr int kTile = kBN * kLd * 4;
-  static constexpr int kQ = 0;
-  static constexpr int kKv = kRows * kLd * 4;            // [kStages][K, V]; P takes K's place once the scores are done
+  static constexpr int kQ = 0;                           // (8 rows: Q is in registers)
+  // [kStages][K, V]; P takes K's place once the scores are done (8 rows: has its own); a piece's results leave by the first
+  static constexpr int kKv = kFew ? 0 : kRows * kLd * 4;
   // tiles in shared memory: as many as fit, since a short tile is done before the next one has come
   static constexpr int kStages = kD == 64 ? 4 : kRows == 64 ? 2 : 3;
-  static constexpr int kP = kKv + kStages * 2 * kTile;             // 16-row tiles: scores and weights, rescaling factors
-  static constexpr int kPiece = kP + (kRows == 16 ? 16 * kPLd * 4 + 64 : 0);
-  static constexpr int kBytes = kPiece + 128;
+  static constexpr int kP = kKv + kStages * 2 * kTile;             // 8 rows: [warp][slot][row] weights
+  static constexpr int kCorr = kP + (kFew ? 8 * 8 * kPLd * 4 : 0);  // 8 rows: [warp][row] rescaling factors
+  static constexpr int kMl = kCorr + (kFew ? 8 * 8 * 4 : 0);       // [warp, or one][row] maximum and sum
+  static constexpr int kPiece = kMl + (kFew ? 8 : 1) * kRows * 8;  // [2]
+  static constexpr int kBytes = kPiece + 256;
+  static_assert(sizeof(Piece) <= 96 && kBytes <= 227 * 1024, "shared memory of a CTA");
 };
 
 struct Params {
@@ -50,6 +61,30 @@ __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool v
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(sz) : "memory");
 }
 __device__ __forceinline__ float4 lds4(const float* p) { return *reinterpret_cast<const float4*>(p); }
+// Two fp32 values in one 64-bit register, for the two-wide instructions: half the issue slots, the same arithmetic.
+typedef unsigned long long f2;
+__device__ __forceinline__ ulonglong2 lds4x2(const float* p) { return *reinterpret_cast<const ulonglong2*>(p); }
+__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) {
+  f2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ f2 mul2(f2 a, f2 b) {
+  f2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f2 join2(float a, float b) {
+  f2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ f2 both(float a) { return join2(a, a); }
+__device__ __forceinline__ float2 split2(f2 v) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
+}
 }  // namespace pf32
 
 template <int kD, int kRows, bool kPaged>
@@ -57,18 +92,17 @@ __global__ void __launch_bounds__(pf32::kThreads, 1)
 packed_f32_kernel(const __grid_constant__ pf32::Params p) {
   using namespace pf32;
   using L = Smem<kD, kRows>;
-  constexpr int kR = kRows / 16;                         // rows per thread
-  constexpr int kC = kD / 64;                            // result columns per thread: kC vectors of 4
+  constexpr bool kFew = L::kFew;
   constexpr int kLd = L::kLd, kPLd = L::kPLd;
   extern __shared__ __align__(16) unsigned char smem_raw[];
   float* sQ = reinterpret_cast<float*>(smem_raw + L::kQ);
   auto sK = [&](int st) { return reinterpret_cast<float*>(smem_raw + L::kKv + st * 2 * L::kTile); };
   auto sV = [&](int st) { return reinterpret_cast<float*>(smem_raw + L::kKv + st * 2 * L::kTile + L::kTile); };
+  float2* sMl = reinterpret_cast<float2*>(smem_raw + L::kMl);
   Piece* s_piece = reinterpret_cast<Piece*>(smem_raw + L::kPiece);
-  volatile int* s_flag = reinterpret_cast<volatile int*>(smem_raw + L::kPiece + 96);
+  volatile int* s_flag = reinterpret_cast<volatile int*>(smem_raw + L::kPiece + 200);
   PlanShared& plan = *reinterpret_cast<PlanShared*>(smem_raw + L::kKv);
-  const int tid = threadIdx.x, warp = tid >> 5;
-  const int ty = tid >> 4, tx = tid & 15;                // rows ty * kR + i, slots tx + 16 j, columns tx * 4 + 64 c
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int G = p.cfg.G;
   pdl_wait();
   long long chunk = 0;
@@ -81,333 +115,418 @@ packed_f32_kernel(const __grid_constant__ pf32::Params p) {
     w.init(p.seqs, p.cfg, &plan, chunk);
   }
   bool bad = false;
+  auto next_piece = [&](int at) {
+    Piece next;
+    if (!w.next(p.seqs, p.cfg, &next)) next.tile0 = -1;
+    if (lane == 0) s_piece[at] = next;
+  };
+  if (warp == 0) next_piece(0);
 
-  while (true) {
+#pragma unroll 1
+  for (int k = 0;; ++k) {
     __syncthreads();                                     // everybody is done with the previous piece (and the plan)
-    if (warp == 0) {
-      Piece next;
-      const bool have = w.next(p.seqs, p.cfg, &next);
-      if (!have) next.tile0 = -1;
-      if (tid == 0) *s_piece = next;
-    }
-    __syncthreads();
-    const Piece pc = *s_piece;
+    const Piece pc = s_piece[k & 1];
     if (pc.tile0 < 0) break;
     const int n_rows = min(p.cfg.tokens, pc.n - pc.r * p.cfg.tokens) * G;
     const int tok0 = pc.first + pc.r * p.cfg.tokens;
     const uint32_t smem = (uint32_t)__cvta_generic_to_shared(smem_raw);
-    auto load_kv = [&](int t, int st) {
-      const int j0 = t * kBN;
-      const uint32_t dk = smem + L::kKv + st * 2 * L::kTile, dv = dk + L::kTile;
-      // a thread keeps its 16-byte column and steps through the rows
-      constexpr int kLanes = kD / 4, kStep = kThreads / kLanes;
-      const int c = tid % kLanes, r0 = tid / kLanes;
-#pragma unroll 4
-      for (int r = r0; r < kBN; r += kStep) {
-        const bool ok = j0 + r < pc.seen;                // slots that no row sees read as zero
-        size_t ko = 0, vo = 0;
-        if (ok) {
-          if constexpr (kPaged) {
-            ko = vo = page_offset(p.pages, pc.s, j0 + r, pc.h, p.cfg.Hkv, kD, &bad) + c * 4;
-          } else {
-            ko = (size_t)(pc.first + j0 + r) * p.K.ts + (size_t)pc.h * p.K.hs + c * 4;
-            vo = (size_t)(pc.first + j0 + r) * p.V.ts + (size_t)pc.h * p.V.hs + c * 4;
-          }
-        }
-        cp_async16(dk + (r * kLd + c * 4) * 4, static_cast<const float*>(p.K.data) + ko, ok);
-        cp_async16(dv + (r * kLd + c * 4) * 4, static_cast<const float*>(p.V.data) + vo, ok);
-      }
-    };
-#pragma unroll 2
-    for (int i = tid; i < kRows * (kD / 4); i += kThreads) {
-      const int r = i / (kD / 4), c = i % (kD / 4);
-      const bool ok = r < n_rows;
-      const size_t off = ok ? (size_t)(tok0 + r / G) * p.Q.ts + (size_t)(pc.h * G + r % G) * p.Q.hs + c * 4 : 0;
-      cp_async16(smem + L::kQ + (r * kLd + c * 4) * 4, static_cast<const float*>(p.Q.data) + off, ok);
-    }
-    // (the last stage is filled from the loop on)
-#pragma unroll 1
-    for (int i = 0; i < L::kStages - 1; ++i) {
-      if (pc.tile0 + i < pc.tile1) load_kv(pc.tile0 + i, i);
-      asm volatile("cp.async.commit_group;" ::: "memory");
-    }
     Seq sq;
     sq.first = pc.first; sq.n = pc.n; sq.base = pc.base;
     const int last_tok = min((pc.r + 1) * p.cfg.tokens, pc.n) - 1;
-    int vis[kR];
-    float m[kR], l[kR], o[kR][kC * 4];
+    float* part = sK(0);                                 // [warp, or one][row][column]: results on their way out
+    if constexpr (kFew) {
+      // ================= 8 rows: the warps on their own =================
+      constexpr int kDs = kD / 8, kKeys = 32 / kDs, kIter = 8 / kKeys;     // lanes of a slot, slots at a time
+      const int ds = lane % kDs, sub = lane / kDs;
+      const int row = kDs == 16 ? ds >> 1 : ds;                            // whose score the lane is left with
+      const bool b0 = ds & (kDs / 2), b1 = ds & (kDs / 4), b2 = ds & (kDs / 8);
+      constexpr int kLanes = kD / 4, kStep = 32 / kLanes;                  // lanes of a row of K or V
+      const int c4 = lane % kLanes * 4, half = lane / kLanes;              // (d = 64: even and odd slots of the result)
+      float* sP = reinterpret_cast<float*>(smem_raw + L::kP) + warp * 8 * kPLd;
+      float* sCorr = reinterpret_cast<float*>(smem_raw + L::kCorr) + warp * 8;
+      // where slot (lane & 7) of this warp's share of a tile lies; looked up a tile before it is needed
+      auto locate = [&](int t) -> long long {
+        const int slot = t * kBN + warp * 8 + (lane & 7);
+        if (t >= pc.tile1 || slot >= pc.seen) return -1;
+        if constexpr (kPaged) return (long long)page_offset(p.pages, pc.s, slot, pc.h, p.cfg.Hkv, kD, &bad);
+        return pc.first + slot;
+      };
+      auto load_kv = [&](int st, long long where) {
+        const uint32_t dk = smem + L::kKv + st * 2 * L::kTile + (warp * 8 + half) * kD * 4 + c4 * 4, dv = dk + L::kTile;
 #pragma unroll
-    for (int i = 0; i < kR; ++i) {
-      vis[i] = visible(p.seqs, sq, min(pc.r * p.cfg.tokens + (ty * kR + i) / G, last_tok));
-      m[i] = -INFINITY;
-      l[i] = 0.f;
+        for (int r = 0; r < 8; r += kStep) {
+          const long long x = __shfl_sync(0xffffffffu, where, r + half);
+          const bool ok = x >= 0;                        // slots that no row sees read as zero
+          size_t ko = ok ? x + c4 : 0, vo = ko;
+          if constexpr (!kPaged) {
+            ko = ok ? (size_t)x * p.K.ts + (size_t)pc.h * p.K.hs + c4 : 0;
+            vo = ok ? (size_t)x * p.V.ts + (size_t)pc.h * p.V.hs + c4 : 0;
+          }
+          cp_async16(dk + r * kD * 4, static_cast<const float*>(p.K.data) + ko, ok);
+          cp_async16(dv + r * kD * 4, static_cast<const float*>(p.V.data) + vo, ok);
+        }
+      };
+      long long where = locate(pc.tile0);
+      f2 q[8][4];
+      const float* qp = static_cast<const float*>(p.Q.data) + (size_t)tok0 * p.Q.ts + (size_t)pc.h * G * p.Q.hs + ds * 4;
+      int member = 0;                                    // row i: token i / G, group member i % G
 #pragma unroll
-      for (int c = 0; c < kC * 4; ++c) o[i][c] = 0.f;
-    }
-    if constexpr (kRows == 16) {
-      // Few rows: a thread owns 4 rows x 4 slots over a quarter of the head dimension, then 4 rows x 4 columns over half
-      // (d = 128) or a quarter (d = 64) of the slots, so that it still has 64 multiply-adds for 8 vectors read; the scores
-      // pass through shared memory in between.
-      const int lane = tid & 31, rg = (warp & 3) * 4;
-      const int ds = lane & 3, kg = (warp >> 2) * 8 + (lane >> 2);
-      constexpr int kColLanes = kD / 4, kSplits = 256 / (4 * kColLanes);
-      const int c4 = (lane & (kColLanes - 1)) * 4, split = (warp >> 2) * (32 / kColLanes) + lane / kColLanes;
-      float* sP = reinterpret_cast<float*>(smem_raw + L::kP);
-      float* sCorr = sP + 16 * kPLd;
-      const int my_vis = visible(p.seqs, sq, min(pc.r * p.cfg.tokens + (rg + ds) / G, last_tok));
-      int row_vis[4];
+      for (int i = 0; i < 8; ++i) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) row_vis[i] = visible(p.seqs, sq, min(pc.r * p.cfg.tokens + (rg + i) / G, last_tok));
-      float acc[4][4];
+        for (int e = 0; e < 2; ++e) {
+          const ulonglong2 x = i < n_rows ? *reinterpret_cast<const ulonglong2*>(qp + e * (kD / 2)) : make_ulonglong2(0ull, 0ull);
+          q[i][e * 2] = x.x;
+          q[i][e * 2 + 1] = x.y;
+        }
+        qp += p.Q.hs;
+        if (++member == G) {
+          member = 0;
+          qp += (ptrdiff_t)p.Q.ts - (ptrdiff_t)G * p.Q.hs;
+        }
+      }
+#pragma unroll 1
+      for (int i = 0; i < L::kStages - 1; ++i) {
+        const long long now = where;
+        where = locate(pc.tile0 + i + 1);
+        if (pc.tile0 + i < pc.tile1) load_kv(i, now);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+      }
+      if (warp == 0) next_piece((k + 1) & 1);
+      const int vis = visible(p.seqs, sq, min(pc.r * p.cfg.tokens + row / G, last_tok));
+      float m = -INFINITY, l = 0.f;
+      f2 acc[4][4];                                      // [pair of rows][column]
 #pragma unroll
-      for (int i = 0; i < 4; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
+      for (int i = 0; i < 4; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0ull;
+#pragma unroll 1
+      for (int t = pc.tile0; t < pc.tile1; ++t) {
+        const int st = (t - pc.tile0) % L::kStages, j0 = t * kBN + warp * 8;
+        asm volatile("cp.async.wait_group %0;" ::"n"(L::kStages - 2) : "memory");
+        __syncwarp();                                    // the warp's share of tile t is there, that of tile t - 1 used up
+        const long long now = where;
+        where = locate(t + L::kStages);
+        if (t + L::kStages - 1 < pc.tile1) load_kv((t - pc.tile0 + L::kStages - 1) % L::kStages, now);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        if (j0 >= pc.seen) break;                        // (only in the last tile)
+        // ---- scores ----
+        float x[kIter], mx = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < kIter; ++i) {
+          const float* kp = sK(st) + (warp * 8 + i * kKeys + sub) * kD + ds * 4;
+          const ulonglong2 a = lds4x2(kp), b = lds4x2(kp + kD / 2);
+          float v[8];
+#pragma unroll
+          for (int r = 0; r < 8; ++r) {
+            const float2 z = split2(fma2(q[r][3], b.y, fma2(q[r][2], b.x, fma2(q[r][1], a.y, mul2(q[r][0], a.x)))));
+            v[r] = z.x + z.y;
+          }
+          // every exchange halves the rows that a lane still adds up
+#pragma unroll
+          for (int r = 0; r < 4; ++r) v[r] = (b0 ? v[r + 4] : v[r]) + __shfl_xor_sync(0xffffffffu, b0 ? v[r] : v[r + 4], kDs / 2);
+#pragma unroll
+          for (int r = 0; r < 2; ++r) v[r] = (b1 ? v[r + 2] : v[r]) + __shfl_xor_sync(0xffffffffu, b1 ? v[r] : v[r + 2], kDs / 4);
+          v[0] = (b2 ? v[1] : v[0]) + __shfl_xor_sync(0xffffffffu, b2 ? v[0] : v[1], kDs / 8);
+          if constexpr (kDs == 16) v[0] += __shfl_xor_sync(0xffffffffu, v[0], 1);
+          x[i] = j0 + i * kKeys + sub < vis ? v[0] * p.scale : -INFINITY;
+          mx = fmaxf(mx, x[i]);
+        }
+        // ---- online softmax ----
+#pragma unroll
+        for (int o = kDs; o < 32; o <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+        const float mn = fmaxf(m, mx), mu = mn == -INFINITY ? 0.f : mn;
+        const float corr = m == mn ? 1.f : expf(m - mu);
+        m = mn;
+        l *= corr;
+        const bool mine = kDs == 8 || (ds & 1) == 0;
+#pragma unroll
+        for (int i = 0; i < kIter; ++i) {
+          x[i] = expf(x[i] - mu);
+          l += x[i];                                     // (this lane's slots; joined at the end)
+          if (mine) sP[(i * kKeys + sub) * kPLd + row] = x[i];
+        }
+        if (mine && sub == 0) sCorr[row] = corr;
+        __syncwarp();
+        // ---- result ----
+        const float* v = sV(st) + warp * 8 * kD + c4;
+        const ulonglong2 corr01 = lds4x2(sCorr), corr23 = lds4x2(sCorr + 4);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          acc[0][c] = mul2(acc[0][c], corr01.x);
+          acc[1][c] = mul2(acc[1][c], corr01.y);
+          acc[2][c] = mul2(acc[2][c], corr23.x);
+          acc[3][c] = mul2(acc[3][c], corr23.y);
+        }
+        if (j0 + 8 <= pc.seen0) {
+#pragma unroll
+          for (int j = 0; j < 8; j += kStep) {
+            const float4 b = lds4(v + (j + half) * kD);
+            const ulonglong2 w01 = lds4x2(sP + (j + half) * kPLd), w23 = lds4x2(sP + (j + half) * kPLd + 4);
+            const f2 bb[4] = {both(b.x), both(b.y), both(b.z), both(b.w)};
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+              acc[0][c] = fma2(w01.x, bb[c], acc[0][c]);
+              acc[1][c] = fma2(w01.y, bb[c], acc[1][c]);
+              acc[2][c] = fma2(w23.x, bb[c], acc[2][c]);
+              acc[3][c] = fma2(w23.y, bb[c], acc[3][c]);
+            }
+          }
+        } else {
+          // some row does not see some slot: a weight of zero would still carry over infinities and NaN
+          const int n_any = min(8, pc.seen - j0);
+          int sees[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) sees[i] = __shfl_sync(0xffffffffu, vis, kDs == 16 ? i * 2 : i) - j0;
+#pragma unroll 1
+          for (int j = half; j < n_any; j += kStep) {
+            const float4 b = lds4(v + j * kD);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const f2 w2 = *reinterpret_cast<const f2*>(sP + j * kPLd + i * 2);
+              const bool s0 = j < sees[i * 2], s1 = j < sees[i * 2 + 1];
+              acc[i][0] = fma2(w2, join2(s0 ? b.x : 0.f, s1 ? b.x : 0.f), acc[i][0]);
+              acc[i][1] = fma2(w2, join2(s0 ? b.y : 0.f, s1 ? b.y : 0.f), acc[i][1]);
+              acc[i][2] = fma2(w2, join2(s0 ? b.z : 0.f, s1 ? b.z : 0.f), acc[i][2]);
+              acc[i][3] = fma2(w2, join2(s0 ? b.w : 0.f, s1 ? b.w : 0.f), acc[i][3]);
+            }
+          }
+        }
+      }
+#pragma unroll
+      for (int o = kDs; o < 32; o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+      if (sub == 0 && (kDs == 8 || (ds & 1) == 0)) sMl[warp * 8 + row] = make_float2(m, l);
+      if constexpr (kStep == 2) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            const float2 y = split2(acc[i][c]);
+            acc[i][c] = join2(y.x + __shfl_xor_sync(0xffffffffu, y.x, 16), y.y + __shfl_xor_sync(0xffffffffu, y.y, 16));
+          }
+      }
+      __syncthreads();                                   // the tiles are used up
+      static_assert(8 * 8 * kD * 4 <= 2 * L::kTile, "the warps' results take the first stage");
+      if (half == 0) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float2 a = split2(acc[i][0]), b = split2(acc[i][1]), c = split2(acc[i][2]), d = split2(acc[i][3]);
+          float* at = part + (warp * 8 + i * 2) * kD + c4;
+          *reinterpret_cast<float4*>(at) = make_float4(a.x, b.x, c.x, d.x);
+          *reinterpret_cast<float4*>(at + kD) = make_float4(a.y, b.y, c.y, d.y);
+        }
+      }
+    } else {
+      // ================= 64 and 32 rows: the CTA together =================
+      constexpr int kR = kRows / 16;                     // rows per thread
+      constexpr int kC = kD / 64;                        // result columns per thread: kC vectors of 4
+      const int ty = tid >> 4, tx = tid & 15;            // rows ty * kR + i, slots tx + 16 j, columns tx * 4 + 64 c
+      auto load_kv = [&](int t, int st) {
+        const int j0 = t * kBN;
+        const uint32_t dk = smem + L::kKv + st * 2 * L::kTile, dv = dk + L::kTile;
+        // a thread keeps its 16-byte column and steps through the rows
+        constexpr int kLanes = kD / 4, kStep = kThreads / kLanes;
+        const int c = tid % kLanes, r0 = tid / kLanes;
+#pragma unroll 4
+        for (int r = r0; r < kBN; r += kStep) {
+          const bool ok = j0 + r < pc.seen;                // slots that no row sees read as zero
+          size_t ko = 0, vo = 0;
+          if (ok) {
+            if constexpr (kPaged) {
+              ko = vo = page_offset(p.pages, pc.s, j0 + r, pc.h, p.cfg.Hkv, kD, &bad) + c * 4;
+            } else {
+              ko = (size_t)(pc.first + j0 + r) * p.K.ts + (size_t)pc.h * p.K.hs + c * 4;
+              vo = (size_t)(pc.first + j0 + r) * p.V.ts + (size_t)pc.h * p.V.hs + c * 4;
+            }
+          }
+          cp_async16(dk + (r * kLd + c * 4) * 4, static_cast<const float*>(p.K.data) + ko, ok);
+          cp_async16(dv + (r * kLd + c * 4) * 4, static_cast<const float*>(p.V.data) + vo, ok);
+        }
+      };
+#pragma unroll 2
+      for (int i = tid; i < kRows * (kD / 4); i += kThreads) {
+        const int r = i / (kD / 4), c = i % (kD / 4);
+        const bool ok = r < n_rows;
+        const size_t off = ok ? (size_t)(tok0 + r / G) * p.Q.ts + (size_t)(pc.h * G + r % G) * p.Q.hs + c * 4 : 0;
+        cp_async16(smem + L::kQ + (r * kLd + c * 4) * 4, static_cast<const float*>(p.Q.data) + off, ok);
+      }
+      // (the last stage is filled from the loop on)
+#pragma unroll 1
+      for (int i = 0; i < L::kStages - 1; ++i) {
+        if (pc.tile0 + i < pc.tile1) load_kv(pc.tile0 + i, i);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+      }
+      if (warp == 0) next_piece((k + 1) & 1);
+      int vis[kR];
+      float m[kR], l[kR];
+#pragma unroll
+      for (int i = 0; i < kR; ++i) {
+        vis[i] = visible(p.seqs, sq, min(pc.r * p.cfg.tokens + (ty * kR + i) / G, last_tok));
+        m[i] = -INFINITY;
+        l[i] = 0.f;
+      }
+      f2 o2[kR][kC * 2];
+#pragma unroll
+      for (int i = 0; i < kR; ++i)
+#pragma unroll
+        for (int c = 0; c < kC * 2; ++c) o2[i][c] = 0ull;
 #pragma unroll 1
       for (int t = pc.tile0; t < pc.tile1; ++t) {
         const int st = (t - pc.tile0) % L::kStages, j0 = t * kBN;
         asm volatile("cp.async.wait_group %0;" ::"n"(L::kStages - 2) : "memory");
-        __syncthreads();                                 // tile t is there, and tile t - 1 is used up
+        __syncthreads();                                   // tile t is there, and tile t - 1 is used up
         if (t + L::kStages - 1 < pc.tile1) load_kv(t + L::kStages - 1, (t - pc.tile0 + L::kStages - 1) % L::kStages);
         asm volatile("cp.async.commit_group;" ::: "memory");
         // ---- scores ----
-        float s[4][4];
+        f2 sum[kR][4];                                     // even and odd elements of the head dimension apart
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[i][0] = s[i][1] = s[i][2] = s[i][3] = 0.f;
-        const float *k = sK(st) + kg * kLd + ds * 4, *q = sQ + rg * kLd + ds * 4;
-#pragma unroll 2
-        for (int e = 0; e < kD; e += 16) {
-          float4 kv[4];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) kv[j] = lds4(k + j * 16 * kLd + e);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float4 a = lds4(q + i * kLd + e);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              s[i][j] = fmaf(a.x, kv[j].x, s[i][j]);
-              s[i][j] = fmaf(a.y, kv[j].y, s[i][j]);
-              s[i][j] = fmaf(a.z, kv[j].z, s[i][j]);
-              s[i][j] = fmaf(a.w, kv[j].w, s[i][j]);
-            }
-          }
-        }
-        // the quarters are added up; lane ds keeps row rg + ds
-        const bool hi = ds & 2, lo = ds & 1;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float a = (hi ? s[2][j] : s[0][j]) + __shfl_xor_sync(0xffffffffu, hi ? s[0][j] : s[2][j], 2);
-          const float b = (hi ? s[3][j] : s[1][j]) + __shfl_xor_sync(0xffffffffu, hi ? s[1][j] : s[3][j], 2);
-          const float x = (lo ? b : a) + __shfl_xor_sync(0xffffffffu, lo ? a : b, 1);
-          sP[(rg + ds) * kPLd + kg + 16 * j] = j0 + kg + 16 * j < my_vis ? x * p.scale : -INFINITY;
-        }
-        __syncthreads();
-        // ---- online softmax: 16 threads per row ----
-        {
-          float x[4], mx = -INFINITY;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            x[j] = sP[ty * kPLd + tx + 16 * j];
-            mx = fmaxf(mx, x[j]);
-          }
-#pragma unroll
-          for (int o2 = 8; o2 > 0; o2 >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o2));
-          const float mn = fmaxf(m[0], mx), mu = mn == -INFINITY ? 0.f : mn;
-          const float corr = m[0] == mn ? 1.f : expf(m[0] - mu);
-          m[0] = mn;
-          l[0] *= corr;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            x[j] = expf(x[j] - mu);
-            l[0] += x[j];                                // (this thread's slots; joined at the end)
-            sP[ty * kPLd + tx + 16 * j] = x[j];
-          }
-          if (tx == 0) sCorr[ty] = corr;
-        }
-        __syncthreads();
-        // ---- result ----
-        const bool edge = j0 + kBN > pc.seen0;           // some row does not see some slot: zero weights times what it holds
-        constexpr int kSlots = kBN / kSplits;
-        const float *v = sV(st) + split * kSlots * kLd + c4, *pr = sP + rg * kPLd + split * kSlots;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float corr = sCorr[rg + i];
-#pragma unroll
-          for (int c = 0; c < 4; ++c) acc[i][c] *= corr;
-        }
-        if (!edge) {
-#pragma unroll 2
-          for (int j = 0; j < kSlots; j += 4) {
-            float4 a[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) a[i] = lds4(pr + i * kPLd + j);
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-              const float4 b = lds4(v + (j + u) * kLd);
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const float w2 = u == 0 ? a[i].x : u == 1 ? a[i].y : u == 2 ? a[i].z : a[i].w;
-                acc[i][0] = fmaf(w2, b.x, acc[i][0]);
-                acc[i][1] = fmaf(w2, b.y, acc[i][1]);
-                acc[i][2] = fmaf(w2, b.z, acc[i][2]);
-                acc[i][3] = fmaf(w2, b.w, acc[i][3]);
-              }
-            }
-          }
-        } else {
-#pragma unroll 1
-          for (int j = 0; j < kSlots; ++j) {
-            const float4 b = lds4(v + j * kLd);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const float w2 = pr[i * kPLd + j];
-              if (j0 + split * kSlots + j < row_vis[i]) {
-                acc[i][0] = fmaf(w2, b.x, acc[i][0]);
-                acc[i][1] = fmaf(w2, b.y, acc[i][1]);
-                acc[i][2] = fmaf(w2, b.z, acc[i][2]);
-                acc[i][3] = fmaf(w2, b.w, acc[i][3]);
-              }
-            }
-          }
-        }
-      }
-      // the splits' parts through shared memory into the layout below
-      __syncthreads();
-      float* part = sK(0);
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        *reinterpret_cast<float4*>(part + (split * 16 + rg + i) * kD + c4) = make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
-      __syncthreads();
-#pragma unroll
-      for (int c = 0; c < kC; ++c)
-#pragma unroll
-        for (int x = 0; x < kSplits; ++x) {
-          const float4 y = lds4(part + (x * 16 + ty) * kD + c * 64 + tx * 4);
-          o[0][c * 4] += y.x;
-          o[0][c * 4 + 1] += y.y;
-          o[0][c * 4 + 2] += y.z;
-          o[0][c * 4 + 3] += y.w;
-        }
-    } else {
-#pragma unroll 1
-    for (int t = pc.tile0; t < pc.tile1; ++t) {
-      const int st = (t - pc.tile0) % L::kStages, j0 = t * kBN;
-      asm volatile("cp.async.wait_group %0;" ::"n"(L::kStages - 2) : "memory");
-      __syncthreads();                                   // tile t is there, and tile t - 1 is used up
-      if (t + L::kStages - 1 < pc.tile1) load_kv(t + L::kStages - 1, (t - pc.tile0 + L::kStages - 1) % L::kStages);
-      asm volatile("cp.async.commit_group;" ::: "memory");
-      // ---- scores ----
-      float s[kR][4];
-#pragma unroll
-      for (int i = 0; i < kR; ++i) s[i][0] = s[i][1] = s[i][2] = s[i][3] = 0.f;
-      const float *k = sK(st) + tx * kLd, *q = sQ + ty * kR * kLd;
+        for (int i = 0; i < kR; ++i) sum[i][0] = sum[i][1] = sum[i][2] = sum[i][3] = 0ull;
+        const float *k = sK(st) + tx * kLd, *q = sQ + ty * kR * kLd;
 #pragma unroll 4
-      for (int e = 0; e < kD; e += 4) {
-        float4 kv[4];
+        for (int e = 0; e < kD; e += 4) {
+          ulonglong2 kv[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) kv[j] = lds4(k + j * 16 * kLd + e);
+          for (int j = 0; j < 4; ++j) kv[j] = lds4x2(k + j * 16 * kLd + e);
+#pragma unroll
+          for (int i = 0; i < kR; ++i) {
+            const ulonglong2 a = lds4x2(q + i * kLd + e);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sum[i][j] = fma2(a.y, kv[j].y, fma2(a.x, kv[j].x, sum[i][j]));
+          }
+        }
+        float s[kR][4];
+#pragma unroll
+        for (int i = 0; i < kR; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float2 x = split2(sum[i][j]);
+            s[i][j] = x.x + x.y;
+          }
+        // ---- online softmax ----
 #pragma unroll
         for (int i = 0; i < kR; ++i) {
-          const float4 a = lds4(q + i * kLd + e);
+          float mx = -INFINITY;
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            s[i][j] = fmaf(a.x, kv[j].x, s[i][j]);
-            s[i][j] = fmaf(a.y, kv[j].y, s[i][j]);
-            s[i][j] = fmaf(a.z, kv[j].z, s[i][j]);
-            s[i][j] = fmaf(a.w, kv[j].w, s[i][j]);
+            s[i][j] = j0 + tx + 16 * j < vis[i] ? s[i][j] * p.scale : -INFINITY;
+            mx = fmaxf(mx, s[i][j]);
+          }
+#pragma unroll
+          for (int x = 8; x > 0; x >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, x));
+          const float mn = fmaxf(m[i], mx), mu = mn == -INFINITY ? 0.f : mn;
+          const float corr = m[i] == mn ? 1.f : expf(m[i] - mu);
+          m[i] = mn;
+          l[i] *= corr;
+          const f2 corr2 = both(corr);
+#pragma unroll
+          for (int c = 0; c < kC * 2; ++c) o2[i][c] = mul2(o2[i][c], corr2);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            s[i][j] = expf(s[i][j] - mu);
+            l[i] += s[i][j];                               // (this thread's slots; joined at the end)
+          }
+        }
+        __syncthreads();                                   // K is used up
+        float* sP = sK(st);
+#pragma unroll
+        for (int i = 0; i < kR; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) sP[(ty * kR + i) * kPLd + tx + 16 * j] = s[i][j];
+        __syncthreads();
+        // ---- result ----
+        const float *v = sV(st) + tx * 4, *pr = sP + ty * kR * kPLd;
+        const int n_all = min(max(pc.seen0 - j0, 0), kBN) & ~3, n_any = min(pc.seen - j0, kBN);
+#pragma unroll 2
+        for (int j = 0; j < n_all; j += 4) {
+          float4 a[kR];
+#pragma unroll
+          for (int i = 0; i < kR; ++i) a[i] = lds4(pr + i * kPLd + j);
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            ulonglong2 b[kC];
+#pragma unroll
+            for (int c = 0; c < kC; ++c) b[c] = lds4x2(v + (j + u) * kLd + c * 64);
+#pragma unroll
+            for (int i = 0; i < kR; ++i) {
+              const f2 w2 = both(u == 0 ? a[i].x : u == 1 ? a[i].y : u == 2 ? a[i].z : a[i].w);
+#pragma unroll
+              for (int c = 0; c < kC; ++c) {
+                o2[i][c * 2] = fma2(w2, b[c].x, o2[i][c * 2]);
+                o2[i][c * 2 + 1] = fma2(w2, b[c].y, o2[i][c * 2 + 1]);
+              }
+            }
+          }
+        }
+        // slots that some row does not see: a weight of zero would still carry over infinities and NaN
+#pragma unroll 1
+        for (int j = n_all; j < n_any; ++j) {
+          ulonglong2 b[kC];
+#pragma unroll
+          for (int c = 0; c < kC; ++c) b[c] = lds4x2(v + j * kLd + c * 64);
+#pragma unroll
+          for (int i = 0; i < kR; ++i) {
+            const f2 w2 = both(pr[i * kPLd + j]);
+            if (j0 + j < vis[i]) {
+#pragma unroll
+              for (int c = 0; c < kC; ++c) {
+                o2[i][c * 2] = fma2(w2, b[c].x, o2[i][c * 2]);
+                o2[i][c * 2 + 1] = fma2(w2, b[c].y, o2[i][c * 2 + 1]);
+              }
+            }
           }
         }
       }
-      // ---- online softmax ----
 #pragma unroll
       for (int i = 0; i < kR; ++i) {
-        float mx = -INFINITY;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          s[i][j] = j0 + tx + 16 * j < vis[i] ? s[i][j] * p.scale : -INFINITY;
-          mx = fmaxf(mx, s[i][j]);
-        }
-#pragma unroll
-        for (int x = 8; x > 0; x >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, x));
-        const float mn = fmaxf(m[i], mx), mu = mn == -INFINITY ? 0.f : mn;
-        const float corr = m[i] == mn ? 1.f : expf(m[i] - mu);
-        m[i] = mn;
-        l[i] *= corr;
-#pragma unroll
-        for (int c = 0; c < kC * 4; ++c) o[i][c] *= corr;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          s[i][j] = expf(s[i][j] - mu);
-          l[i] += s[i][j];                               // (this thread's slots; joined at the end)
-        }
+        for (int x = 8; x > 0; x >>= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], x);
+        if (tx == 0) sMl[ty * kR + i] = make_float2(m[i], l[i]);
       }
-      __syncthreads();                                   // K is used up
-      float* sP = sK(st);
+      __syncthreads();                                   // the tiles are used up
 #pragma unroll
       for (int i = 0; i < kR; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) sP[(ty * kR + i) * kPLd + tx + 16 * j] = s[i][j];
-      __syncthreads();
-      // ---- result ----
-      const float *v = sV(st) + tx * 4, *pr = sP + ty * kR * kPLd;
-      const bool edge = j0 + kBN > pc.seen0;             // some row does not see some slot: zero weights times what it holds
-#pragma unroll 2
-      for (int j = 0; j < kBN; j += 4) {
-        float4 a[kR];
+        for (int c = 0; c < kC; ++c)
+          *reinterpret_cast<ulonglong2*>(part + (ty * kR + i) * kD + c * 64 + tx * 4) = make_ulonglong2(o2[i][c * 2], o2[i][c * 2 + 1]);
+    }
+    __syncthreads();
+    // rows leave the CTA (or their parts do) as whole lines
+    auto write_row = [&](int r, int c, float4 x, float M, float Ls) {
+      const int tok = tok0 + r / G, hq = pc.h * G + r % G;
+      const float inv = 1.0f / Ls;
+      *reinterpret_cast<float4*>(static_cast<float*>(p.O.data) + (size_t)tok * p.O.ts + (size_t)hq * p.O.hs + c) =
+          Ls == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(x.x * inv, x.y * inv, x.z * inv, x.w * inv);
+      if (c == 0 && p.lse != nullptr) p.lse[(size_t)tok * p.Hq + hq] = Ls == 0.f ? -INFINITY : M + logf(Ls);
+    };
+    const int n_vec = n_rows * (kD / 4);
+#pragma unroll 1
+    for (int i = tid; i < n_vec; i += kThreads) {
+      const int r = i / (kD / 4), c = i % (kD / 4) * 4;
+      float2 ml = sMl[r];
+      float4 x = lds4(part + r * kD + c);
+      if constexpr (kFew) {
+        float M = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < kR; ++i) a[i] = lds4(pr + i * kPLd + j);
+        for (int y = 0; y < 8; ++y)
+          if (sMl[y * 8 + r].y != 0.f) M = fmaxf(M, sMl[y * 8 + r].x);
+        ml = make_float2(M, 0.f);
+        x = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          float4 b[kC];
-#pragma unroll
-          for (int c = 0; c < kC; ++c) b[c] = lds4(v + (j + u) * kLd + c * 64);
-#pragma unroll
-          for (int i = 0; i < kR; ++i) {
-            const float w = u == 0 ? a[i].x : u == 1 ? a[i].y : u == 2 ? a[i].z : a[i].w;
-            if (!edge || j0 + j + u < vis[i]) {
-#pragma unroll
-              for (int c = 0; c < kC; ++c) {
-                o[i][c * 4] = fmaf(w, b[c].x, o[i][c * 4]);
-                o[i][c * 4 + 1] = fmaf(w, b[c].y, o[i][c * 4 + 1]);
-                o[i][c * 4 + 2] = fmaf(w, b[c].z, o[i][c * 4 + 2]);
-                o[i][c * 4 + 3] = fmaf(w, b[c].w, o[i][c * 4 + 3]);
-              }
-            }
-          }
+        for (int y = 0; y < 8; ++y) {
+          const float2 a = sMl[y * 8 + r];
+          if (a.y == 0.f) continue;                      // the warp saw nothing for this row
+          const float wgt = expf(a.x - M);
+          const float4 z = lds4(part + (y * 8 + r) * kD + c);
+          x = make_float4(fmaf(z.x, wgt, x.x), fmaf(z.y, wgt, x.y), fmaf(z.z, wgt, x.z), fmaf(z.w, wgt, x.w));
+          ml.y += a.y * wgt;
         }
       }
+      if (pc.slot < 0) {
+        write_row(r, c, x, ml.x, ml.y);
+      } else {
+        *reinterpret_cast<float4*>(p.part_o + ((size_t)pc.slot * kRows + r) * kD + c) = x;
+        if (c == 0) p.part_ml[(size_t)pc.slot * kRows + r] = ml;
+      }
     }
-    }
-#pragma unroll
-    for (int i = 0; i < kR; ++i)
-#pragma unroll
-      for (int x = 8; x > 0; x >>= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], x);
-    auto write_row = [&](int i, const float* acc, float M, float Ls) {
-      const int row = ty * kR + i;
-      if (row >= n_rows) return;
-      const int tok = tok0 + row / G, hq = pc.h * G + row % G;
-      const float inv = 1.0f / Ls;
-      float* op = static_cast<float*>(p.O.data) + (size_t)tok * p.O.ts + (size_t)hq * p.O.hs + tx * 4;
-#pragma unroll
-      for (int c = 0; c < kC; ++c)
-        *reinterpret_cast<float4*>(op + c * 64) =
-            Ls == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f)
-                      : make_float4(acc[c * 4] * inv, acc[c * 4 + 1] * inv, acc[c * 4 + 2] * inv, acc[c * 4 + 3] * inv);
-      if (tx == 0 && p.lse != nullptr) p.lse[(size_t)tok * p.Hq + hq] = Ls == 0.f ? -INFINITY : M + logf(Ls);
-    };
-    if (pc.slot < 0) {
-#pragma unroll
-      for (int i = 0; i < kR; ++i) write_row(i, o[i], m[i], l[i]);
-      continue;
-    }
-    // a piece of a cut item leaves (m, l, O); whoever takes the last ticket merges them in order of the pieces
-#pragma unroll
-    for (int i = 0; i < kR; ++i) {
-      const size_t row = (size_t)pc.slot * kRows + ty * kR + i;
-#pragma unroll
-      for (int c = 0; c < kC; ++c)
-        *reinterpret_cast<float4*>(p.part_o + row * kD + c * 64 + tx * 4) =
-            make_float4(o[i][c * 4], o[i][c * 4 + 1], o[i][c * 4 + 2], o[i][c * 4 + 3]);
-      if (tx == 0) p.part_ml[row] = make_float2(m[i], l[i]);
-    }
+    if (pc.slot < 0) continue;
+    // a piece of a cut item left (m, l, O); whoever takes the last ticket merges them in order of the pieces
     __threadfence();
     __syncthreads();
     if (tid == 0) *s_flag = last_piece(p.d_status, pc.ticket, pc.n_pieces);
@@ -415,35 +534,26 @@ packed_f32_kernel(const __grid_constant__ pf32::Params p) {
     if (*s_flag) {
       __threadfence();
 #pragma unroll 1
-      for (int i = 0; i < kR; ++i) {
-        const int row = ty * kR + i;
-        if (row >= n_rows) continue;
-        float M = -INFINITY, Ls = 0.f, acc[kC * 4];
-#pragma unroll
-        for (int c = 0; c < kC * 4; ++c) acc[c] = 0.f;
+      for (int i = tid; i < n_vec; i += kThreads) {
+        const int r = i / (kD / 4), c = i % (kD / 4) * 4;
+        float M = -INFINITY, Ls = 0.f;
+        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
         for (int n = 0; n < pc.n_pieces; ++n) {
-          const float2 x = __ldcg(p.part_ml + piece_slot(pc, n) * kRows + row);
-          if (x.y != 0.f) M = fmaxf(M, x.x);
+          const float2 ml = __ldcg(p.part_ml + piece_slot(pc, n) * kRows + r);
+          if (ml.y != 0.f) M = fmaxf(M, ml.x);
         }
 #pragma unroll 4
         for (int n = 0; n < pc.n_pieces; ++n) {
-          const size_t at = (size_t)piece_slot(pc, n) * kRows + row;
-          const float2 x = __ldcg(p.part_ml + at);
-          const float wgt = x.y == 0.f ? 0.f : expf(x.x - M);
-#pragma unroll
-          for (int c = 0; c < kC; ++c) {
-            const float4 v4 = __ldcg(reinterpret_cast<const float4*>(p.part_o + at * kD + c * 64 + tx * 4));
-            if (x.y != 0.f) {
-              acc[c * 4] = fmaf(v4.x, wgt, acc[c * 4]);
-              acc[c * 4 + 1] = fmaf(v4.y, wgt, acc[c * 4 + 1]);
-              acc[c * 4 + 2] = fmaf(v4.z, wgt, acc[c * 4 + 2]);
-              acc[c * 4 + 3] = fmaf(v4.w, wgt, acc[c * 4 + 3]);
-            }
-          }
-          if (x.y != 0.f) Ls += x.y * wgt;
+          const size_t at = (size_t)piece_slot(pc, n) * kRows + r;
+          const float2 ml = __ldcg(p.part_ml + at);
+          const float4 z = __ldcg(reinterpret_cast<const float4*>(p.part_o + at * kD + c));
+          if (ml.y == 0.f) continue;
+          const float wgt = expf(ml.x - M);
+          x = make_float4(fmaf(z.x, wgt, x.x), fmaf(z.y, wgt, x.y), fmaf(z.z, wgt, x.z), fmaf(z.w, wgt, x.w));
+          Ls += ml.y * wgt;
         }
-        write_row(i, acc, M, Ls);
+        write_row(r, c, x, M, Ls);
       }
     }
   }
@@ -483,7 +593,7 @@ cudaError_t launch_packed_f32(const samkv_packed_t& d, const Seqs& seqs, const K
   p.cfg.G = d.n_q_heads / d.n_kv_heads;
   p.cfg.Hkv = d.n_kv_heads;
   p.cfg.tile = pf32::kBN;
-  p.cfg.fixed = 2 * pf32::kBN;
+  p.cfg.fixed = (rows == 8 ? 3 : 2) * pf32::kBN;
   p.cfg.min_chunk = 4 * pf32::kBN;
   p.pages = kv.pages;
   p.Q = Q;
@@ -502,8 +612,8 @@ cudaError_t launch_packed_f32(const samkv_packed_t& d, const Seqs& seqs, const K
   char* ws = h.workspace + kStatusBytes;
 #define SAMKV_F32_CASE(D, R) (kv.paged ? pf32::launch<D, R, true>(p, ctas, ws, stream) : pf32::launch<D, R, false>(p, ctas, ws, stream))
   if (d.head_dim == 128)
-    return rows == 16 ? SAMKV_F32_CASE(128, 16) : rows == 32 ? SAMKV_F32_CASE(128, 32) : SAMKV_F32_CASE(128, 64);
-  return rows == 16 ? SAMKV_F32_CASE(64, 16) : rows == 32 ? SAMKV_F32_CASE(64, 32) : SAMKV_F32_CASE(64, 64);
+    return rows == 8 ? SAMKV_F32_CASE(128, 8) : rows == 32 ? SAMKV_F32_CASE(128, 32) : SAMKV_F32_CASE(128, 64);
+  return rows == 8 ? SAMKV_F32_CASE(64, 8) : rows == 32 ? SAMKV_F32_CASE(64, 32) : SAMKV_F32_CASE(64, 64);
 #undef SAMKV_F32_CASE
 }
 

@@ -247,13 +247,13 @@ struct Walker {
   }
   __device__ __forceinline__ int tiles(const Seqs& q, const SplitCfg& c) const {
     const int t = min((r + 1) * c.tokens, cur.n) - 1;
-    return max(1, (visible(q, cur, t) + c.tile - 1) / c.tile);
+    return max(1, (visible(q, cur, t) + c.tile - 1) >> (31 - __clz(c.tile)));
   }
   // tile border nearest to position p of the current item; pieces shorter than two tiles are not worth their merge
   __device__ __forceinline__ int border(const SplitCfg& c, long long p, int nt) const {
     const long long y = p - item_start - c.fixed;
     if (y <= 0) return 0;
-    long long t = (y + c.tile / 2) / c.tile;
+    long long t = (y + c.tile / 2) >> (31 - __clz(c.tile));
     if (t < 2) return 0;
     if (t > nt - 2) return nt;
     return (int)t;

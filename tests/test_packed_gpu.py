@@ -630,3 +630,32 @@ def test_overlapping_offsets_and_foreign_rows_are_reported():
     assert bool((O[:6] == 7.0).all()) and bool((O[10:] == 7.0).all()) and not bool((O[6:10] == 7.0).any())
     B.samkv_paged_attn(h, p, B.Pages(c.Kp, c.Vp, c.table), c.cache_len, c.Q, 0.0, True, O)
     assert B.samkv_poll_status(h) == 7 and B.samkv_poll_status(h) == 0
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("lens", [[100, 50, 61, 90, 1], [40, 48, 33, 47], [700, 3, 515], [9, 4, 17, 2, 30], [640, 1000]])
+def test_fp32_row_tiles(d, lens):
+    """The fp32 kernel's heights of a row tile (8, 32, 64 rows, by the rows of the call and their lengths), and what a row does
+    not see: infinities and NaN behind it change no bit."""
+    T, Hq, Hkv = sum(lens) + 3, 8, 2
+    q, k, v = (randn(T, h, d, dtype="f32", seed=70 + i) for i, h in enumerate((Hq, Hkv, Hkv)))
+    O, lse = run_prefill(q, k, v, lens, "f32")
+    check_prefill(q, k, v, lens, "f32", O, lse)
+    at = lens[0] + lens[1] // 2 + 1                      # in the second sequence, seldom on a tile's border
+    for bad in (float("nan"), float("inf"), -float("inf")):
+        k2, v2 = k.clone(), v.clone()
+        k2[at:sum(lens[:2])], v2[at:sum(lens[:2])] = bad, bad
+        O2, lse2 = run_prefill(q, k2, v2, lens, "f32")
+        keep = torch.ones(T, dtype=torch.bool, device=DEV)
+        keep[at:sum(lens[:2])] = False
+        assert torch.equal(O[keep], O2[keep]) and torch.equal(lse[keep], lse2[keep])
+
+
+@pytest.mark.parametrize("Hq,Hkv,d", [(8, 2, 64), (8, 2, 128), (32, 1, 64), (11, 1, 128), (14, 2, 64)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_fp32_tall_row_tiles_over_pages(Hq, Hkv, d, causal):
+    c = PagedCase([700, 0, 3, 515], [0, 10, 300, 77], Hq, Hkv, d, 16, "f32", seed=73, pad=2, garbage=float("nan"))
+    O, lse = run_paged(c, causal)
+    check_paged(c, O, lse, causal)
+    O2, lse2 = run_paged(c, causal)
+    assert torch.equal(O, O2) and torch.equal(lse, lse2)
