@@ -411,7 +411,8 @@ samkv_status_t samkv_prefill(samkv_handle_t h, const samkv_packed_t* packed, con
  *   K_out,V_out packed destinations next to, or instead of, the pages (both or neither, NULL: none); e.g. the slabs
  *               samkv_prefill and samkv_score read
  *   Q, Q_out    optional (both or neither): Q rows, rotated by the same positions
- * Q_out, K_out, V_out may be the very same rows as Q, K, V; otherwise outputs must not overlap inputs.
+ * Q_out, K_out, V_out may be the very same rows as Q, K, V; otherwise outputs must not overlap inputs.  The pools must
+ * not overlap one another or any packed tensor.
  * A slot at or behind table_width * page_size, or one whose page is invalid, is skipped and recorded as a device check.
  * Rotation in fp32, one rounding to dtype; rows that are not rotated are copied bit-exactly.  No workspace. */
 samkv_status_t samkv_append(samkv_handle_t h, const samkv_packed_t* packed, const samkv_rows_t* K,
@@ -424,7 +425,7 @@ samkv_status_t samkv_append(samkv_handle_t h, const samkv_packed_t* packed, cons
  *   cache_len  int32 [n_seq] device: slots in the cache before this step, as given to samkv_append
  *   causal     != 0: the new tokens' own rows have been appended; token t sees slots < cache_len[s] + t + 1
  *              == 0: every token sees the slots < cache_len[s] (a row that sees none: O = 0, lse = -inf)
- *   Q, O       packed with n_q_heads; O must not overlap Q
+ *   Q, O       packed with n_q_heads; O must not overlap Q or the pools
  *   scale, lse as for samkv_prefill
  * Slots that no token sees are never used, whatever they hold.  A sequence whose slots would pass table_width *
  * page_size is cut off there and recorded as a device check. */

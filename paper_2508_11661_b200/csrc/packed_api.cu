@@ -69,8 +69,10 @@ samkv_status_t make_rope(const samkv_packed_t& p, const samkv_rope_t* r, RopeTab
     // A base below 1 turns faster than once in 2 pi; its turns are reduced like given ones.
     const long double ratio = powl((long double)r->base, -2.0L / r->rot_dim), unit = 18446744073709551616.0L / two_pi;
     long double power = unit;
-    for (int i = 0; i < r->rot_dim / 2; ++i, power *= ratio)
-      out->turn[i] = (unsigned long long)((power < 18446744073709551616.0L ? power : fmodl(power, 18446744073709551616.0L)) + 0.5L);
+    for (int i = 0; i < r->rot_dim / 2; ++i, power *= ratio) {
+      const long double x = (power < 18446744073709551616.0L ? power : fmodl(power, 18446744073709551616.0L)) + 0.5L;
+      out->turn[i] = x >= 18446744073709551616.0L ? 0ull : (unsigned long long)x;
+    }
   } else {
     for (int i = 0; i < r->rot_dim / 2; ++i) {
       if (!isfinite(r->inv_freq[i])) return SAMKV_ERR_INVALID_ARG;
@@ -104,6 +106,16 @@ bool rows_overlap(const samkv_packed_t& p, const Rows& a, int heads_a, const Row
     if (gap >= wa && gap + wb <= ts) return false;
   }
   return true;
+}
+
+// Does a packed tensor's address range meet one of the pools, or (r == nullptr) one pool the other?
+bool meets_pools(const samkv_packed_t& p, const Pages& g, const Rows* r, int heads) {
+  const long long e = p.dtype == SAMKV_BF16 ? 2 : 4, pool = (((long long)g.n_pages * p.n_kv_heads) << g.shift) * p.head_dim * e;
+  const char *k = (const char*)g.K, *v = (const char*)g.V;
+  if (r == nullptr) return k < v + pool && v < k + pool;
+  const char* a = (const char*)r->data;
+  const char* b = a + e * ((p.n_tokens - 1) * r->ts + (heads - 1) * r->hs + p.head_dim);
+  return (a < k + pool && k < b) || (a < v + pool && v < b);
 }
 
 samkv_status_t check_workspace(const samkv_ctx_impl* h, const samkv_packed_t& p) {
@@ -194,6 +206,13 @@ samkv_status_t samkv_append(samkv_handle_t handle, const samkv_packed_t* packed,
       if (outs[j].r != nullptr && rows_overlap(*packed, o, outs[i].heads, *outs[j].r, outs[j].heads))
         return SAMKV_ERR_INVALID_ARG;
   }
+  if (pages != nullptr) {
+    if (meets_pools(*packed, pg, nullptr, 0) || meets_pools(*packed, pg, &k, Hkv) || meets_pools(*packed, pg, &v, Hkv))
+      return SAMKV_ERR_INVALID_ARG;
+    if (Q != nullptr && (meets_pools(*packed, pg, &q, Hq) || meets_pools(*packed, pg, &qo, Hq))) return SAMKV_ERR_INVALID_ARG;
+    if (K_out != nullptr && (meets_pools(*packed, pg, &ko, Hkv) || meets_pools(*packed, pg, &vo, Hkv)))
+      return SAMKV_ERR_INVALID_ARG;
+  }
   if ((st = check_handle(h)) != SAMKV_OK) return st;
   const Seqs seqs = {packed->seq_offsets, cache_len, packed->n_seq, packed->n_tokens, INT_MAX, 0};
   return from_cuda(launch_append(*packed, seqs, k, v, pages != nullptr ? &pg : nullptr, table, positions,
@@ -219,6 +238,7 @@ samkv_status_t samkv_paged_attn(samkv_handle_t handle, const samkv_packed_t* pac
   if ((st = check_rows(*packed, O, packed->n_q_heads, true, &o)) != SAMKV_OK) return st;
   if ((st = check_pages(*packed, pages, &kv.pages)) != SAMKV_OK) return st;
   if (rows_overlap(*packed, o, packed->n_q_heads, q, packed->n_q_heads)) return SAMKV_ERR_INVALID_ARG;
+  if (meets_pools(*packed, kv.pages, &o, packed->n_q_heads)) return SAMKV_ERR_INVALID_ARG;
   if ((st = check_handle(h)) != SAMKV_OK) return st;
   if ((st = check_workspace(h, *packed)) != SAMKV_OK) return st;
   const Seqs seqs = {packed->seq_offsets, cache_len, packed->n_seq, packed->n_tokens,

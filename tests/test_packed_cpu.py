@@ -31,7 +31,7 @@ class Call:
         for name, heads in (("Q", Hq), ("K", Hkv), ("V", Hkv), ("O", Hq), ("K_out", Hkv), ("V_out", Hkv)):
             self.r[name] = B.samkv_rows_t(at, heads * d, d)
             at += T * heads * d * e
-        self.pages = B.samkv_pages_t(base, base, base, 16, 4, 3)
+        self.pages = B.samkv_pages_t(base + (1 << 18), base + (1 << 19), base, 16, 4, 3)      # pools of up to 64 KB
         self.rope = B.samkv_rope_t(d, 0, 10000.0, None)
         self.cache_len, self.positions, self.lse, self.scale = base, None, None, 0.0
 
@@ -162,6 +162,30 @@ def test_outputs_must_not_overlap():
     assert c.append() == CUDA and c.prefill() == INVALID
     c.r["O"] = B.samkv_rows_t(base + 2 * 10 * w, 8 * 128, 128)
     assert c.prefill() == CUDA
+
+
+@no_gpu
+def test_pools_must_not_overlap_what_a_call_reads_or_writes():
+    pool = 4 * 2 * 16 * 128 * 2
+    for which in ("K", "V"):
+        def moved(**kw):
+            c = Call()
+            start = getattr(c.pages, which)
+            for name, (back, rows_from_end) in kw.items():
+                heads = 8 if name in ("Q", "O") else 2
+                c.r[name] = B.samkv_rows_t(start + (pool if rows_from_end else -10 * heads * 128 * 2) + back, heads * 128, 128)
+            return c
+
+        for name in ("Q", "K", "V", "O", "K_out", "V_out"):
+            assert moved(**{name: (0, True)}).append() == CUDA and moved(**{name: (0, False)}).append() == CUDA
+            assert moved(**{name: (-16, True)}).append() == INVALID and moved(**{name: (16, False)}).append() == INVALID
+        assert moved(O=(0, True)).attn() == CUDA and moved(O=(-16, True)).attn() == INVALID
+        assert moved(Q=(-16, True)).attn() == CUDA            # both only read
+    c = Call()
+    c.pages.V = c.pages.K + pool - 16
+    assert c.append() == INVALID and c.attn() == CUDA
+    c.pages.V = c.pages.K + pool
+    assert c.append() == CUDA
 
 
 @no_gpu
