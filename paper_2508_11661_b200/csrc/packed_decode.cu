@@ -119,15 +119,13 @@ packed_decode_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
   __syncthreads();
   pdl_wait();
   long long chunk = 0;
-  const bool warp_plans = p.seqs.n_seq <= kWarpPlanSeqs;
-  if (!warp_plans) plan_block<kThreads>(p.seqs, p.cfg, &plan, &chunk, p.d_status, tid);
+  if (p.seqs.n_seq > kWarpPlanSeqs) plan_block<kThreads>(p.seqs, p.cfg, &plan, &chunk, p.d_status, tid);
   auto wait = [&](int i, uint32_t phase) { return wait_bar(bar(i), phase & 1u, s_fail); };
 
   if (warp == kConsumers) {
     // ================= producer: plan, Q, K and V =================
     Walker w;
-    if (warp_plans) plan_block<32>(p.seqs, p.cfg, &plan, &chunk, p.d_status, lane);
-    w.init(p.seqs, p.cfg, &plan, chunk);
+    w.begin(p.seqs, p.cfg, &plan, chunk, p.d_status);
     __syncwarp();
     Piece pc;
     uint32_t f = 0, T = 0;

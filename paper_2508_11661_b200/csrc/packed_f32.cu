@@ -106,14 +106,10 @@ packed_f32_kernel(const __grid_constant__ pf32::Params p) {
   const int G = p.cfg.G;
   pdl_wait();
   long long chunk = 0;
-  const bool warp_plans = p.seqs.n_seq <= kWarpPlanSeqs;
-  if (!warp_plans) plan_block<kThreads>(p.seqs, p.cfg, &plan, &chunk, p.d_status, tid);
+  if (p.seqs.n_seq > kWarpPlanSeqs) plan_block<kThreads>(p.seqs, p.cfg, &plan, &chunk, p.d_status, tid);
   Walker w;
   w.more = false;
-  if (warp == 0) {
-    if (warp_plans) plan_block<32>(p.seqs, p.cfg, &plan, &chunk, p.d_status, tid);
-    w.init(p.seqs, p.cfg, &plan, chunk);
-  }
+  if (warp == 0) w.begin(p.seqs, p.cfg, &plan, chunk, p.d_status);
   bool bad = false;
   auto next_piece = [&](int at) {
     Piece next;
@@ -144,20 +140,35 @@ packed_f32_kernel(const __grid_constant__ pf32::Params p) {
       const int c4 = lane % kLanes * 4, half = lane / kLanes;              // (d = 64: even and odd slots of the result)
       float* sP = reinterpret_cast<float*>(smem_raw + L::kP) + warp * 8 * kPLd;
       float* sCorr = reinterpret_cast<float*>(smem_raw + L::kCorr) + warp * 8;
-      // where slot (lane & 7) of this warp's share of a tile lies; looked up a tile before it is needed
-      auto locate = [&](int t) -> long long {
-        const int slot = t * kBN + warp * 8 + (lane & 7);
-        if (t >= pc.tile1 || slot >= pc.seen) return -1;
-        if constexpr (kPaged) return (long long)page_offset(p.pages, pc.s, slot, pc.h, p.cfg.Hkv, kD, &bad);
-        return pc.first + slot;
+      // The lanes hold the page numbers of four tiles, lane 8 i + j that of slot j of this warp's share of tile t4 + i.  The
+      // next four are asked for when the last of them is used, and first looked at a tile later.
+      int t4 = pc.tile0, page = 0;
+      auto slot_of_lane = [&]() { return (t4 + (lane >> 3)) * kBN + warp * 8 + (lane & 7); };
+      auto wanted = [&]() { return t4 + (lane >> 3) < pc.tile1 && slot_of_lane() < pc.seen; };
+      auto look_up = [&]() {
+        if (kPaged && wanted()) page = p.pages.table[(size_t)pc.s * p.pages.width + (slot_of_lane() >> p.pages.shift)];
       };
-      auto load_kv = [&](int st, long long where) {
+      look_up();
+      auto load_kv = [&](int t, int st) {
+        const int four = (t - t4) * 8;
+        long long where = -1;                            // row of K and V for the lane's slot
+        if (wanted()) {
+          where = pc.first + slot_of_lane();
+          if constexpr (kPaged) {
+            if ((unsigned)page >= (unsigned)p.pages.n_pages) {
+              bad = true;
+              page = 0;
+            }
+            const int shift = p.pages.shift;
+            where = (((long long)page * p.cfg.Hkv + pc.h) << shift) + (slot_of_lane() & ((1 << shift) - 1));
+          }
+        }
         const uint32_t dk = smem + L::kKv + st * 2 * L::kTile + (warp * 8 + half) * kD * 4 + c4 * 4, dv = dk + L::kTile;
 #pragma unroll
         for (int r = 0; r < 8; r += kStep) {
-          const long long x = __shfl_sync(0xffffffffu, where, r + half);
+          const long long x = __shfl_sync(0xffffffffu, where, four + r + half);
           const bool ok = x >= 0;                        // slots that no row sees read as zero
-          size_t ko = ok ? x + c4 : 0, vo = ko;
+          size_t ko = ok ? (size_t)x * kD + c4 : 0, vo = ko;
           if constexpr (!kPaged) {
             ko = ok ? (size_t)x * p.K.ts + (size_t)pc.h * p.K.hs + c4 : 0;
             vo = ok ? (size_t)x * p.V.ts + (size_t)pc.h * p.V.hs + c4 : 0;
@@ -165,8 +176,11 @@ packed_f32_kernel(const __grid_constant__ pf32::Params p) {
           cp_async16(dk + r * kD * 4, static_cast<const float*>(p.K.data) + ko, ok);
           cp_async16(dv + r * kD * 4, static_cast<const float*>(p.V.data) + vo, ok);
         }
+        if (four == 24) {
+          t4 += 4;
+          look_up();
+        }
       };
-      long long where = locate(pc.tile0);
       f2 q[8][4];
       const float* qp = static_cast<const float*>(p.Q.data) + (size_t)tok0 * p.Q.ts + (size_t)pc.h * G * p.Q.hs + ds * 4;
       int member = 0;                                    // row i: token i / G, group member i % G
@@ -186,9 +200,7 @@ packed_f32_kernel(const __grid_constant__ pf32::Params p) {
       }
 #pragma unroll 1
       for (int i = 0; i < L::kStages - 1; ++i) {
-        const long long now = where;
-        where = locate(pc.tile0 + i + 1);
-        if (pc.tile0 + i < pc.tile1) load_kv(i, now);
+        if (pc.tile0 + i < pc.tile1) load_kv(pc.tile0 + i, i);
         asm volatile("cp.async.commit_group;" ::: "memory");
       }
       if (warp == 0) next_piece((k + 1) & 1);
@@ -202,9 +214,7 @@ packed_f32_kernel(const __grid_constant__ pf32::Params p) {
         const int st = (t - pc.tile0) % L::kStages, j0 = t * kBN + warp * 8;
         asm volatile("cp.async.wait_group %0;" ::"n"(L::kStages - 2) : "memory");
         __syncwarp();                                    // the warp's share of tile t is there, that of tile t - 1 used up
-        const long long now = where;
-        where = locate(t + L::kStages);
-        if (t + L::kStages - 1 < pc.tile1) load_kv((t - pc.tile0 + L::kStages - 1) % L::kStages, now);
+        if (t + L::kStages - 1 < pc.tile1) load_kv(t + L::kStages - 1, (t - pc.tile0 + L::kStages - 1) % L::kStages);
         asm volatile("cp.async.commit_group;" ::: "memory");
         if (j0 >= pc.seen) break;                        // (only in the last tile)
         // ---- scores ----
@@ -505,16 +515,19 @@ packed_f32_kernel(const __grid_constant__ pf32::Params p) {
         float M = -INFINITY;
 #pragma unroll
         for (int y = 0; y < 8; ++y)
-          if (sMl[y * 8 + r].y != 0.f) M = fmaxf(M, sMl[y * 8 + r].x);
+          M = fmaxf(M, sMl[y * 8 + r].y != 0.f ? sMl[y * 8 + r].x : -INFINITY);
         ml = make_float2(M, 0.f);
         x = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
         for (int y = 0; y < 8; ++y) {
           const float2 a = sMl[y * 8 + r];
-          if (a.y == 0.f) continue;                      // the warp saw nothing for this row
-          const float wgt = expf(a.x - M);
+          const bool any = a.y != 0.f;                   // (no branch: the eight go on side by side)
+          const float wgt = any ? expf(a.x - M) : 0.f;
           const float4 z = lds4(part + (y * 8 + r) * kD + c);
-          x = make_float4(fmaf(z.x, wgt, x.x), fmaf(z.y, wgt, x.y), fmaf(z.z, wgt, x.z), fmaf(z.w, wgt, x.w));
+          x.x = any ? fmaf(z.x, wgt, x.x) : x.x;
+          x.y = any ? fmaf(z.y, wgt, x.y) : x.y;
+          x.z = any ? fmaf(z.z, wgt, x.z) : x.z;
+          x.w = any ? fmaf(z.w, wgt, x.w) : x.w;
           ml.y += a.y * wgt;
         }
       }
@@ -541,16 +554,19 @@ packed_f32_kernel(const __grid_constant__ pf32::Params p) {
 #pragma unroll 4
         for (int n = 0; n < pc.n_pieces; ++n) {
           const float2 ml = __ldcg(p.part_ml + piece_slot(pc, n) * kRows + r);
-          if (ml.y != 0.f) M = fmaxf(M, ml.x);
+          M = fmaxf(M, ml.y != 0.f ? ml.x : -INFINITY);
         }
 #pragma unroll 4
         for (int n = 0; n < pc.n_pieces; ++n) {
           const size_t at = (size_t)piece_slot(pc, n) * kRows + r;
           const float2 ml = __ldcg(p.part_ml + at);
           const float4 z = __ldcg(reinterpret_cast<const float4*>(p.part_o + at * kD + c));
-          if (ml.y == 0.f) continue;
-          const float wgt = expf(ml.x - M);
-          x = make_float4(fmaf(z.x, wgt, x.x), fmaf(z.y, wgt, x.y), fmaf(z.z, wgt, x.z), fmaf(z.w, wgt, x.w));
+          const bool any = ml.y != 0.f;                  // (no branch: four loads under way at a time)
+          const float wgt = any ? expf(ml.x - M) : 0.f;
+          x.x = any ? fmaf(z.x, wgt, x.x) : x.x;
+          x.y = any ? fmaf(z.y, wgt, x.y) : x.y;
+          x.z = any ? fmaf(z.z, wgt, x.z) : x.z;
+          x.w = any ? fmaf(z.w, wgt, x.w) : x.w;
           Ls += ml.y * wgt;
         }
         write_row(r, c, x, M, Ls);

@@ -84,6 +84,19 @@ __device__ __forceinline__ long long quotient(long long a, long long b) {
   return ((unsigned long long)(a | b) >> 32) == 0 ? (long long)((unsigned)a / (unsigned)b) : a / b;
 }
 
+// Length of a CTA's stretch of the axis.
+__device__ __forceinline__ long long stretch(const SplitCfg& c, long long total, int items) {
+  long long ctas = quotient(total, c.min_chunk);
+  if (ctas < items) ctas = items;
+  if (ctas > (long long)gridDim.x) ctas = gridDim.x;
+  if (ctas < 1) ctas = 1;
+  return quotient(total + ctas - 1, ctas);
+}
+// Calls of this size may be laid out in waves.
+__device__ __forceinline__ bool maybe_waves(const SplitCfg& c, long long total, int items) {
+  return c.wave_slots > 0 && total > 2 * c.wave_slots && items <= kMaxTickets;
+}
+
 // Finds the sequence that holds this CTA's first position.  Called by kThreads threads, a whole block or (32) one warp,
 // with their index among them; afterwards *chunk is the length of a CTA's stretch (0: nothing to do) and sh->s,
 // sh->start are set for CTAs that have one.
@@ -143,7 +156,7 @@ __device__ __forceinline__ void plan_block(const Seqs& q, const SplitCfg& c, Pla
   }
   sync();
   const long long total = sh->total;
-  if (c.wave_slots > 0 && total > 2 * c.wave_slots && sh->items <= kMaxTickets) {
+  if (maybe_waves(c, total, sh->items)) {
     // candidates for waves: a second look at the lengths
     unsigned long long distinct = 0;
     int longest = 0;
@@ -192,11 +205,7 @@ __device__ __forceinline__ void plan_block(const Seqs& q, const SplitCfg& c, Pla
       if (sh->wave_tiles > 0) return;
     }
   }
-  long long ctas = quotient(total, c.min_chunk);
-  if (ctas < sh->items) ctas = sh->items;
-  if (ctas > (long long)gridDim.x) ctas = gridDim.x;
-  if (ctas < 1) ctas = 1;
-  const long long ch = quotient(total + ctas - 1, ctas);
+  const long long ch = stretch(c, total, sh->items);
   *chunk = ch;
   const long long p0 = ch * blockIdx.x;
   const long long excl = sh->warp_len[warp] + incl - len;
@@ -258,12 +267,45 @@ struct Walker {
     if (t > nt - 2) return nt;
     return (int)t;
   }
-  __device__ __forceinline__ void init(const Seqs& q, const SplitCfg& c, const PlanShared* sh, long long ch) {
-    const long long p0 = ch * blockIdx.x;
+  // Lays the call out, unless the block has (ch is its result then), and finds this CTA's place.
+  __device__ __forceinline__ void begin(const Seqs& q, const SplitCfg& c, PlanShared* sh, long long ch, int* d_status) {
+    const int lane = threadIdx.x & 31;
+    wave_tiles = 0;
+    w_s0 = -64;
+    if (q.n_seq <= 32) {
+      // A sequence per lane, nothing through shared memory: 2.6 us of every call's latency with the general form below,
+      // most of it chains of loads and 64-bit arithmetic that only many sequences need.
+      Seq x = {0, 0, 0, false};
+      if (lane < q.n_seq) x = load_seq(q, lane);
+      const int tiles_x = row_tiles(c, x.n);
+      const long long len = c.Hkv * items_length(c, q.causal, x.base, tiles_x);
+      const int items = __reduce_add_sync(0xffffffffu, c.Hkv * tiles_x);
+      long long incl = len;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const long long v = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += v;
+      }
+      total_len = __shfl_sync(0xffffffffu, incl, 31);
+      if (!maybe_waves(c, total_len, items)) {
+        if (x.clamped && blockIdx.x == 0) atomicMax(d_status, (int)CHECK_SEQ_RANGE);
+        chunk = stretch(c, total_len, items);
+        const long long p0 = chunk * blockIdx.x;
+        more = p0 < total_len;
+        if (!more) return;
+        s = __ffs(__ballot_sync(0xffffffffu, p0 < incl)) - 1;
+        w_s0 = 0;
+        w_first = x.first;
+        w_n = x.n;
+        w_base = x.base;
+        place(q, c, p0, __shfl_sync(0xffffffffu, incl - len, s));
+        return;
+      }
+    }
+    if (q.n_seq <= kWarpPlanSeqs) plan_block<32>(q, c, sh, &ch, d_status, lane);
     total_len = sh->total;
     chunk = ch;
     wave_tiles = sh->wave_tiles;
-    w_s0 = -64;
     if (wave_tiles > 0) {
       unit = blockIdx.x;
       unit0 = item0 = 0;
@@ -272,24 +314,33 @@ struct Walker {
       more = true;
       return;
     }
-    more = p0 < total_len;
+    more = ch * blockIdx.x < total_len;
     if (!more) return;
-    p1 = min(p0 + ch, total_len);
     s = sh->s;
+    place(q, c, ch * blockIdx.x, sh->start);
+  }
+  // The item at position p0 of the axis, in sequence s, which starts at position `start`.
+  __device__ __forceinline__ void place(const Seqs& q, const SplitCfg& c, long long p0, long long start) {
+    p1 = min(p0 + chunk, total_len);
     fetch(q, s);
     R = row_tiles(c, cur.n);
     const long long per_head = items_length(c, q.causal, cur.base, R);
-    long long rem = p0 - sh->start;
+    long long rem = p0 - start;
     h = (int)quotient(rem, per_head);
     rem -= h * per_head;
-    int lo = 0, hi = R - 1;                  // largest r whose items before it are no longer than rem
+    // largest r whose items before it are no longer than rem: 32 candidates at a time
+    const int lane = threadIdx.x & 31;
+    int lo = 0, n = R;                       // it is one of lo .. lo + n - 1
 #pragma unroll 1
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (items_length(c, q.causal, cur.base, mid) <= rem) lo = mid; else hi = mid - 1;
+    while (n > 1) {
+      const int step = (n + 31) >> 5, at = lane * step;
+      const unsigned fits = __ballot_sync(0xffffffffu, at < n && items_length(c, q.causal, cur.base, lo + at) <= rem);
+      const int skip = (__popc(fits) - 1) * step;          // (lengths rise with r, and lane 0's fits)
+      lo += skip;
+      n = min(step, n - skip);
     }
     r = lo;
-    item_start = sh->start + h * per_head + items_length(c, q.causal, cur.base, r);
+    item_start = start + h * per_head + items_length(c, q.causal, cur.base, r);
     first_piece_tile = border(c, p0, tiles(q, c));
   }
   // Next unit of a call in waves.

@@ -293,8 +293,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
   const uint32_t tmem = *s_tmem;
   pdl_wait();                               // everything below reads what earlier kernels may have written
   long long chunk = 0;
-  const bool warp_plans = p.seqs.n_seq <= kWarpPlanSeqs;
-  if (!warp_plans) plan_block<kThreads>(p.seqs, p.cfg, &plan, &chunk, p.d_status, tid);
+  if (p.seqs.n_seq > kWarpPlanSeqs) plan_block<kThreads>(p.seqs, p.cfg, &plan, &chunk, p.d_status, tid);
 
   auto wait = [&](int i, uint32_t phase) { return wait_bar(bar(i), phase & 1u, s_fail); };
 
@@ -303,8 +302,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     if (warp == kWarpK) {
       // ================= plan and K =================
       Walker w;
-      if (warp_plans) plan_block<32>(p.seqs, p.cfg, &plan, &chunk, p.d_status, lane);
-      w.init(p.seqs, p.cfg, &plan, chunk);
+      w.begin(p.seqs, p.cfg, &plan, chunk, p.d_status);
       Piece pc;
       uint32_t f = 0, T = 0;                // pieces, key tiles so far
       bool bad = false;
