@@ -10,11 +10,12 @@
 //     the loop waits for another warp; the eight results are joined when a piece ends.  A thread keeps 8 rows x 8 elements
 //     of Q in registers, reads a slot's key once, and the d / 8 threads of a slot are added up by shuffles that leave each
 //     with a row of its own; for the result it owns 8 rows x 4 columns.
-// Measured: prompts of 1024 and 700 tokens, 32/8 heads of 128, 64 rows: 538 us, 30 TFLOP/s of the FMA pipe's nominal 74 (two
-// warps per scheduler issue 0.45 instructions a cycle: dependent chains and shared memory).  Decode, 32 requests x 1000
+// Measured: prompts of 1024 and 700 tokens, 32/8 heads of 128, 64 rows: 538 us, 30 TFLOP/s of the FMA pipe's nominal 74
+// (shared memory is busy 62 % of the cycles, and two warps per scheduler cover little of their chains).  Decode, 32 requests x 1000
 // slots, 32/8 heads of 128, 8 rows: 55 us, 4.9 TB/s (138 us when the CTA shared tiles of 16 rows).  Little work is latency:
-// an item costs about 2.5 us besides its tiles; 6 sequences of 1 to 64 tokens, 4/2 heads of 64: 17 us (22 us with 16 rows).
-// Starting the next item's loads before the results leave made every shape 4 to 8 % slower (the code grew), so it is not done.
+// an item costs about 2 us besides its tiles (a third until its first tile is there, 0.5 us to join the warps' results);
+// 6 sequences of 1 to 64 tokens, 4/2 heads of 64: 16 us (22 us with 16 rows).  Starting the next item's loads before the
+// results leave made every shape 4 to 8 % slower (the code grew), so it is not done.
 #include <math.h>
 
 #include "packed_plan.cuh"
@@ -181,7 +182,12 @@ packed_f32_kernel(const __grid_constant__ pf32::Params p) {
           look_up();
         }
       };
-      f2 q[8][4];
+#pragma unroll 1
+      for (int i = 0; i < L::kStages - 1; ++i) {
+        if (pc.tile0 + i < pc.tile1) load_kv(pc.tile0 + i, i);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+      }
+      f2 q[8][4];                                        // (after the copies of K and V are on their way: 1 to 5 % faster)
       const float* qp = static_cast<const float*>(p.Q.data) + (size_t)tok0 * p.Q.ts + (size_t)pc.h * G * p.Q.hs + ds * 4;
       int member = 0;                                    // row i: token i / G, group member i % G
 #pragma unroll
@@ -197,11 +203,6 @@ packed_f32_kernel(const __grid_constant__ pf32::Params p) {
           member = 0;
           qp += (ptrdiff_t)p.Q.ts - (ptrdiff_t)G * p.Q.hs;
         }
-      }
-#pragma unroll 1
-      for (int i = 0; i < L::kStages - 1; ++i) {
-        if (pc.tile0 + i < pc.tile1) load_kv(pc.tile0 + i, i);
-        asm volatile("cp.async.commit_group;" ::: "memory");
       }
       if (warp == 0) next_piece((k + 1) & 1);
       const int vis = visible(p.seqs, sq, min(pc.r * p.cfg.tokens + row / G, last_tok));

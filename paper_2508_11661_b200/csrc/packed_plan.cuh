@@ -273,8 +273,8 @@ struct Walker {
     wave_tiles = 0;
     w_s0 = -64;
     if (q.n_seq <= 32) {
-      // A sequence per lane, nothing through shared memory: 2.6 us of every call's latency with the general form below,
-      // most of it chains of loads and 64-bit arithmetic that only many sequences need.
+      // A sequence per lane, nothing through shared memory: 1.6 us of every call's latency, 2.6 us with the general form
+      // below (chains of loads and 64-bit arithmetic that only many sequences need).
       Seq x = {0, 0, 0, false};
       if (lane < q.n_seq) x = load_seq(q, lane);
       const int tiles_x = row_tiles(c, x.n);
