@@ -99,7 +99,8 @@ __device__ __forceinline__ bool maybe_waves(const SplitCfg& c, long long total, 
 
 // Finds the sequence that holds this CTA's first position.  Called by kThreads threads, a whole block or (32) one warp,
 // with their index among them; afterwards *chunk is the length of a CTA's stretch (0: nothing to do) and sh->s,
-// sh->start are set for CTAs that have one.
+// sh->start are set for CTAs that have one.  No thread looks at *sh behind the last barrier in here, so that the warp which
+// walks the plan may give the memory away once it has begun.
 template <int kThreads>
 __device__ __forceinline__ void plan_block(const Seqs& q, const SplitCfg& c, PlanShared* sh, long long* chunk, int* d_status,
                                            int tid) {
@@ -202,7 +203,9 @@ __device__ __forceinline__ void plan_block(const Seqs& q, const SplitCfg& c, Pla
         if (best > total / (long long)gridDim.x * 3 / 2) sh->wave_tiles = 0;
       }
       sync();
-      if (sh->wave_tiles > 0) return;
+      const bool waves = sh->wave_tiles > 0;
+      sync();                  // (the memory may be the destination of copies as soon as one warp goes on)
+      if (waves) return;
     }
   }
   const long long ch = stretch(c, total, sh->items);

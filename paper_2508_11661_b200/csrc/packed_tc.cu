@@ -303,6 +303,9 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
       // ================= plan and K =================
       Walker w;
       w.begin(p.seqs, p.cfg, &plan, chunk, p.d_status);
+      __syncwarp();
+      fence_proxy_async();                  // the plan's memory becomes the destination of copies
+      __syncwarp();
       Piece pc;
       uint32_t f = 0, T = 0;                // pieces, key tiles so far
       bool bad = false;
