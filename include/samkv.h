@@ -428,7 +428,7 @@ samkv_status_t samkv_append(samkv_handle_t h, const samkv_packed_t* packed, cons
  *   Q, O       packed with n_q_heads; O must not overlap Q or the pools
  *   scale, lse as for samkv_prefill
  * Slots that no token sees are never used, whatever they hold.  A sequence whose slots would pass table_width *
- * page_size is cut off there and recorded as a device check. */
+ * page_size is cut off there and recorded as a device check: its tokens see the slots that the table has. */
 samkv_status_t samkv_paged_attn(samkv_handle_t h, const samkv_packed_t* packed, const samkv_pages_t* pages,
                                 const int32_t* cache_len, const samkv_rows_t* Q, float scale, int32_t causal,
                                 const samkv_rows_t* O, float* lse, void* stream);

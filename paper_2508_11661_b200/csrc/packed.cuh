@@ -38,15 +38,15 @@ __device__ __forceinline__ Seq load_seq(const Seqs& q, int s) {
   const int a = q.off[s], b = q.off[s + 1], c = q.cache_len != nullptr ? q.cache_len[s] : 0;
   r.first = min(max(a, 0), q.n_tokens);
   r.n = min(max(b, r.first), q.n_tokens) - r.first;
-  const int most = q.causal ? max(q.limit - r.n, 0) : q.limit;
-  r.base = min(max(c, 0), most);
-  r.clamped = r.first != a || r.first + r.n != b || (r.n > 0 && (r.base != c || (q.causal && r.n > q.limit)));
+  r.base = min(max(c, 0), q.limit);
+  r.clamped = r.first != a || r.first + r.n != b || (r.n > 0 && (r.base != c || (q.causal && r.n > q.limit - r.base)));
   return r;
 }
 
-// Slots that token t of the sequence sees.
+// Slots that token t of the sequence sees: a table that ends sooner cuts them off there (base <= limit, so that nothing
+// here passes 32 bits).
 __device__ __forceinline__ int visible(const Seqs& q, const Seq& r, int t) {
-  return q.causal ? min(r.base + t + 1, q.limit) : r.base;
+  return q.causal ? (int)min((unsigned)r.base + (unsigned)t + 1u, (unsigned)q.limit) : r.base;
 }
 
 // Where the keys and values of an attention call live: pages, or packed rows (slot j of a sequence = row first + j).

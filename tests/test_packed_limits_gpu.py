@@ -1,0 +1,48 @@
+"""Packed and paged calls where their rounding, their bounds and their hand-overs are easiest to get wrong."""
+import numpy as np
+import pytest
+import torch
+
+from packed_testlib import DT, PagedCase, attend64, check_rows, f64
+from test_packed_gpu import DEV, run_paged
+
+pytestmark = pytest.mark.gpu
+
+
+class FullTables(PagedCase):
+    """Every sequence owns `width` pages, all of them filled; lengths are set by the test."""
+
+    def __init__(self, new, width, Hq, Hkv, d, page, dtype, seed=0, pad=0):
+        super().__init__(new, [0] * len(new), Hq, Hkv, d, page, dtype, seed=seed, pad=pad)
+        g = torch.Generator().manual_seed(seed + 1000)
+        self.width, self.n_pages = width, len(new) * width
+        self.table_cpu = torch.randperm(self.n_pages, generator=g).to(torch.int32).view(len(new), width).contiguous()
+        self.table = self.table_cpu.to(DEV)
+        self.Kp = torch.randn((self.n_pages, Hkv, page, d), generator=g).to(DT[dtype]).to(DEV)
+        self.Vp = torch.randn((self.n_pages, Hkv, page, d), generator=g).to(DT[dtype]).to(DEV)
+
+
+# ------------------------------------------------------------------------------------------------ tables that are too short
+@pytest.mark.parametrize("dtype,new,width,page,hint", [
+    ("bf16", [3, 2, 3, 1, 3], 4, 16, 3),                 # decode
+    ("bf16", [40, 7, 130, 300, 33], 3, 64, 0),           # tensor memory; 300 tokens pass a table of 192 slots by themselves
+    ("f32", [3, 2, 3, 1, 3], 4, 16, 3),                  # 8 rows
+    ("f32", [40, 7, 230, 300, 333], 3, 64, 0)])          # 64 rows
+@pytest.mark.parametrize("causal", [True, False])
+def test_sequences_that_pass_their_table_are_cut_off(dtype, new, width, page, hint, causal):
+    """Token t sees the slots < cache_len + t + 1 (or < cache_len) as far as the table goes: a token that fits keeps its own."""
+    limit = width * page
+    for lens in ([limit - 1, limit, limit - 2, limit + 7, 0], [2**31 - 1, limit - 5, 1, 0, limit - 1]):
+        c = FullTables(new, width, 8, 2, 128, page, dtype, seed=200, pad=3)
+        c.cache_len = torch.tensor(lens, dtype=torch.int32, device=DEV)
+        over = any(n > limit or (causal and n + k > limit) for n, k in zip(lens, new))
+        assert over
+        O, lse = run_paged(c, causal, max_seq=hint, poll=7)
+        q, o, l = f64(c.Q), f64(O), f64(lse)
+        at = 0
+        for s, n in enumerate(new):
+            vis = np.minimum(lens[s] + (np.arange(1, n + 1) if causal else np.zeros(n, dtype=np.int64)), limit)
+            ref = attend64(q[at:at + n], c.slots(c.Kp, s, limit), c.slots(c.Vp, s, limit), vis, 128 ** -0.5)
+            check_rows(o[at:at + n], l[at:at + n], ref, dtype, limit, f"sequence {s}: {n} over {lens[s]} of {limit}")
+            at += n
+        assert (o[at:] == 7.0).all()
