@@ -339,7 +339,9 @@ samkv_status_t samkv_align(samkv_handle_t h, const samkv_shape_t* shape, const i
  * Sequence s owns the rows seq_offsets[s] .. seq_offsets[s+1]-1 of every packed tensor (row = token).  Sequences may be
  * empty.  Rows of outputs behind the last sequence are left as they were; input rows there are not used.
  * Offsets and lengths are DEVICE data (a captured call may be replayed with others); the kernels clamp what they read to
- * the bounds below and record a device check (samkv_poll_status) where a value had to be clamped. */
+ * the bounds below and record a device check (samkv_poll_status) where a value had to be clamped.  Offsets that run
+ * backwards are recorded, too: for attention a sequence that ends before it starts and all behind it are empty, so that no
+ * row belongs to two sequences; samkv_append takes each row as one of at most one sequence. */
 #define SAMKV_MAX_SEQ 65536
 
 typedef struct {

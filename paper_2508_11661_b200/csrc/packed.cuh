@@ -31,6 +31,7 @@ struct Seq {
   int first, n;                // first packed row, new tokens
   int base;                    // slots seen by every new token
   bool clamped;
+  bool backwards;              // ends before it starts
 };
 
 __device__ __forceinline__ Seq load_seq(const Seqs& q, int s) {
@@ -38,6 +39,7 @@ __device__ __forceinline__ Seq load_seq(const Seqs& q, int s) {
   const int a = q.off[s], b = q.off[s + 1], c = q.cache_len != nullptr ? q.cache_len[s] : 0;
   r.first = min(max(a, 0), q.n_tokens);
   r.n = min(max(b, r.first), q.n_tokens) - r.first;
+  r.backwards = b < a;
   r.base = min(max(c, 0), q.limit);
   r.clamped = r.first != a || r.first + r.n != b || (r.n > 0 && (r.base != c || (q.causal && r.n > q.limit - r.base)));
   return r;

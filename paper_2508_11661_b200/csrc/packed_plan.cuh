@@ -18,6 +18,9 @@
 // waves instead: keys are cut into blocks of one length, a unit is a row tile times a block, units run block by block
 // with the row tiles next to one another, and CTA c takes units c, c + grid, ...: the row tiles of a block run at the same
 // time and share its keys through L2 (128 tokens over 102400, 8 row tiles per KV head: see packed_tc.cu).
+//
+// A sequence that ends before it starts also ends the list of sequences: those behind it could own the same rows again,
+// which two CTAs would write at the same time and which no bound on the call's work would cover.
 #pragma once
 
 #include "packed.cuh"
@@ -65,6 +68,8 @@ constexpr int kWaveTries = 12;
 struct PlanShared {
   long long warp_len[32];
   int warp_items[32];
+  int warp_end[32];
+  int n_seq;                   // sequences before one that ends before it starts
   long long start;             // position of the sequence found
   int s;
   long long total;             // length of the axis
@@ -110,7 +115,8 @@ __device__ __forceinline__ void plan_block(const Seqs& q, const SplitCfg& c, Pla
     if constexpr (kThreads == 32) __syncwarp(); else __syncthreads();
   };
   const int per = (q.n_seq + kThreads - 1) / kThreads;
-  const int s0 = min(tid * per, q.n_seq), s1 = min(s0 + per, q.n_seq);
+  const int s0 = min(tid * per, q.n_seq);
+  int s1 = min(s0 + per, q.n_seq);
   if (tid == 0) {
     sh->distinct = 0;
     sh->longest = 0;
@@ -120,15 +126,32 @@ __device__ __forceinline__ void plan_block(const Seqs& q, const SplitCfg& c, Pla
   long long len = 0;
   int items = 0;
   bool clamped = false;
+  int n_seq = q.n_seq;
 #pragma unroll 1
   for (int s = s0; s < s1; ++s) {
     const Seq sq = load_seq(q, s);
     const int R = row_tiles(c, sq.n);
+    clamped |= sq.clamped;
+    if (sq.backwards) {
+      n_seq = s;
+      break;
+    }
     len += c.Hkv * items_length(c, q.causal, sq.base, R);
     items += c.Hkv * R;
-    clamped |= sq.clamped;
   }
   if (clamped && blockIdx.x == 0) atomicMax(d_status, (int)CHECK_SEQ_RANGE);
+  n_seq = __reduce_min_sync(0xffffffffu, n_seq);
+  if constexpr (kThreads > 32) {
+    if (lane == 0) sh->warp_end[warp] = n_seq;
+    sync();
+    n_seq = __reduce_min_sync(0xffffffffu, sh->warp_end[lane < kWarps ? lane : 0]);
+  }
+  if (tid == 0) sh->n_seq = n_seq;
+  s1 = min(s1, n_seq);
+  if (s0 >= n_seq) {
+    len = 0;
+    items = 0;
+  }
   long long incl = len;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -232,7 +255,7 @@ __device__ __forceinline__ void plan_block(const Seqs& q, const SplitCfg& c, Pla
 struct Walker {
   long long chunk, p1, item_start;
   long long total_len;
-  int s, h, r, R;
+  int s, h, r, R, n_seq;
   int w_first, w_n, w_base, w_s0;          // lane i: sequence w_s0 + i
   Seq cur;
   int wave_tiles, unit, unit0, item0, nb;  // calls in waves: next unit, units and items before the current sequence
@@ -243,8 +266,8 @@ struct Walker {
     const int lane = threadIdx.x & 31;
     if (s_ < w_s0 || s_ >= w_s0 + 32) {
       w_s0 = s_;
-      Seq x = {0, 0, 0, false};
-      if (s_ + lane < q.n_seq) x = load_seq(q, s_ + lane);
+      Seq x = {0, 0, 0, false, false};
+      if (s_ + lane < n_seq) x = load_seq(q, s_ + lane);
       w_first = x.first;
       w_n = x.n;
       w_base = x.base;
@@ -278,8 +301,11 @@ struct Walker {
     if (q.n_seq <= 32) {
       // A sequence per lane, nothing through shared memory: 1.6 us of every call's latency, 2.6 us with the general form
       // below (chains of loads and 64-bit arithmetic that only many sequences need).
-      Seq x = {0, 0, 0, false};
+      Seq x = {0, 0, 0, false, false};
       if (lane < q.n_seq) x = load_seq(q, lane);
+      const unsigned back = __ballot_sync(0xffffffffu, x.backwards);
+      n_seq = back != 0 ? __ffs(back) - 1 : q.n_seq;
+      if (lane >= n_seq) x.n = 0;
       const int tiles_x = row_tiles(c, x.n);
       const long long len = c.Hkv * items_length(c, q.causal, x.base, tiles_x);
       const int items = __reduce_add_sync(0xffffffffu, c.Hkv * tiles_x);
@@ -306,6 +332,7 @@ struct Walker {
       }
     }
     if (q.n_seq <= kWarpPlanSeqs) plan_block<32>(q, c, sh, &ch, d_status, lane);
+    n_seq = sh->n_seq;
     total_len = sh->total;
     chunk = ch;
     wave_tiles = sh->wave_tiles;
@@ -355,7 +382,7 @@ struct Walker {
           unit0 += c.Hkv * R * nb;
           item0 += c.Hkv * R;
         }
-        if (++s >= q.n_seq) return false;
+        if (++s >= n_seq) return false;
         fetch(q, s);
         R = row_tiles(c, cur.n);
         // (a sequence whose rows see nothing still gets its rows written)
@@ -437,7 +464,7 @@ struct Walker {
 #pragma unroll 1
             do {
               ++s;
-              if (s >= q.n_seq) { more = false; break; }
+              if (s >= n_seq) { more = false; break; }
               fetch(q, s);
             } while (cur.n == 0);
             if (more) R = row_tiles(c, cur.n);

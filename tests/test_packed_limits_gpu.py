@@ -46,3 +46,24 @@ def test_sequences_that_pass_their_table_are_cut_off(dtype, new, width, page, hi
             check_rows(o[at:at + n], l[at:at + n], ref, dtype, limit, f"sequence {s}: {n} over {lens[s]} of {limit}")
             at += n
         assert (o[at:] == 7.0).all()
+
+
+# ------------------------------------------------------------------------------------------------ offsets that run backwards
+@pytest.mark.parametrize("dtype,hint,span", [("bf16", 2, 2), ("bf16", 0, 20), ("f32", 2, 2), ("f32", 0, 20)])
+@pytest.mark.parametrize("n_seq,at", [(5, 1), (32, 31), (33, 7), (300, 150), (513, 2), (1200, 1000)])
+def test_a_sequence_that_ends_before_it_starts_ends_the_list(dtype, hint, span, n_seq, at):
+    """Those behind it start over on rows that others own: they are empty, the ones before it are what they are alone."""
+    new = [span] * n_seq
+    c = PagedCase(new, [30] * n_seq, 4, 2, 64, 16, dtype, seed=240)
+    off = np.arange(n_seq + 1) * span
+    off[at + 1:] -= min(off[at], span) + 1               # sequence `at` runs backwards, the next ones own rows twice
+    assert (np.diff(off) < 0).sum() == 1 and off.min() >= 0
+    good, good_lse = run_paged(c, max_seq=hint)
+    c.offsets = torch.from_numpy(off.astype(np.int32)).to(DEV)
+    O, lse = run_paged(c, max_seq=hint, poll=7)
+    rows = at * span
+    assert bool((O[rows:] == 7.0).all()) and bool((lse[rows:] == 7.0).all())
+    # another division of the keys may round otherwise, by no more than the two results' own bounds
+    tol = 2.0 ** -6 if dtype == "bf16" else 1e-5
+    assert bool(((O[:rows] - good[:rows]).float().abs() <= tol * good.abs().amax().float()).all())
+    assert bool((lse[:rows] - good_lse[:rows]).abs().le(1e-5).all())
