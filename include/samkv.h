@@ -86,7 +86,9 @@ size_t samkv_workspace_bytes(const samkv_shape_t* shape, int32_t max_q_tokens, i
 
 /* Creates a handle bound to CUDA device `device` and to `workspace` (device pointer, 256-byte
  * aligned, workspace_bytes long, caller-owned, must outlive the handle).  Queries device
- * properties and enqueues one small memset on the default stream; allocates no device memory. */
+ * properties and enqueues one small memset on the default stream; allocates no device memory.
+ * The caller orders that memset behind work of other streams that still writes the workspace, and
+ * before the handle's first call. */
 samkv_status_t samkv_create(samkv_handle_t* out, int device, void* workspace, size_t workspace_bytes);
 samkv_status_t samkv_destroy(samkv_handle_t h);
 /* Host-side switch of a handle (no GPU work, takes effect with the next samkv_attn call on the handle).

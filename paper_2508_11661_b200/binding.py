@@ -219,10 +219,7 @@ class Handle:
         nbytes = samkv_workspace_bytes(shape, max_q_tokens, cache_capacity)
         if nbytes == 0:
             raise SamkvError(1, "samkv_workspace_bytes")
-        self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=f"cuda:{dev}")
-        self._h = ctypes.c_void_p()
-        with torch.cuda.device(dev):
-            _check(lib().samkv_create(ctypes.byref(self._h), dev, self.workspace.data_ptr(), nbytes), "samkv_create")
+        self._create(dev, nbytes)
 
     @classmethod
     def for_packed(cls, packed: "Packed", device: Optional[int] = None) -> "Handle":
@@ -232,13 +229,19 @@ class Handle:
         if nbytes == 0:
             raise SamkvError(1, "samkv_packed_workspace_bytes")
         self = cls.__new__(cls)
-        self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=f"cuda:{dev}")
+        self._create(dev, nbytes)
+        return self
+
+    def _create(self, dev: int, nbytes: int):
         self._h = ctypes.c_void_p()
         with torch.cuda.device(dev):
+            self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=f"cuda:{dev}")
+            # The status block is cleared on the default stream: behind work that the memory's last owner may still have
+            # queued on this stream, and before the first call, whatever stream that is on.
+            default = torch.cuda.default_stream(dev)
+            default.wait_stream(torch.cuda.current_stream(dev))
             _check(lib().samkv_create(ctypes.byref(self._h), dev, self.workspace.data_ptr(), nbytes), "samkv_create")
-            # the status block is cleared on the default stream: a first call on any other stream has to find it clear
-            torch.cuda.default_stream(dev).synchronize()
-        return self
+            default.synchronize()
 
     def close(self):
         if self._h:

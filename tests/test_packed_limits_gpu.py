@@ -3,6 +3,7 @@ import numpy as np
 import pytest
 import torch
 
+from paper_2508_11661_b200 import binding as B
 from packed_testlib import DT, PagedCase, attend64, check_rows, f64
 from test_packed_gpu import DEV, run_paged
 
@@ -67,3 +68,28 @@ def test_a_sequence_that_ends_before_it_starts_ends_the_list(dtype, hint, span, 
     tol = 2.0 ** -6 if dtype == "bf16" else 1e-5
     assert bool(((O[:rows] - good[:rows]).float().abs() <= tol * good.abs().amax().float()).all())
     assert bool((lse[:rows] - good_lse[:rows]).abs().le(1e-5).all())
+
+
+# ------------------------------------------------------------------------------------------------ handles
+def test_a_handle_made_behind_pending_work_of_its_workspace():
+    """The allocator hands out memory that queued work of the same stream still writes; the handle's status block has to be
+    cleared behind that work."""
+    c = PagedCase([1], [9001], 8, 1, 128, 64, "bf16", seed=66)
+    ref, _ = run_paged(c)
+    p = B.Packed(c.Hq, c.Hkv, c.d, c.offsets, c.T, 0, c.dtype)
+    nbytes = B.samkv_packed_workspace_bytes(p)
+    pages = B.Pages(c.Kp, c.Vp, c.table)
+    O = torch.full_like(c.Q, 7.0)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        junk = torch.empty(nbytes, dtype=torch.uint8, device=DEV)
+        where = junk.data_ptr()
+        for _ in range(1500):
+            junk.fill_(255)
+        del junk
+        h = B.Handle.for_packed(p)
+        assert h.workspace.data_ptr() == where
+        B.samkv_paged_attn(h, p, pages, c.cache_len, c.Q, 0.0, True, O)
+        assert B.samkv_poll_status(h) == 0
+    assert torch.equal(O, ref)
