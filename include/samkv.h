@@ -399,7 +399,9 @@ size_t samkv_packed_workspace_bytes(const samkv_packed_t* packed);
  *   lse    fp32 [n_tokens, n_q_heads] optional: log of the softmax denominator
  * K and V may be the [n_kv_heads, L_tot, d] slabs of one request that samkv_score and samkv_compact read later.
  * Values of K and V behind a row's own position never reach that row, infinities and NaN included.
- * Precision as for samkv_attn.  SAMKV_ERR_WORKSPACE if the handle's workspace is too small. */
+ * Precision as for samkv_attn: bf16 probabilities are rounded to bf16 before the second product and O is divided by the
+ * sum of the rounded ones; lse is taken before that rounding.  SAMKV_ERR_WORKSPACE if the handle's workspace is too
+ * small. */
 samkv_status_t samkv_prefill(samkv_handle_t h, const samkv_packed_t* packed, const samkv_rows_t* Q,
                              const samkv_rows_t* K, const samkv_rows_t* V, float scale, const samkv_rows_t* O,
                              float* lse, void* stream);

@@ -68,6 +68,35 @@ __device__ __forceinline__ size_t page_offset(const Pages& p, int s, int j, int 
   return ((((size_t)page * Hkv + h) << p.shift) + (j & ((1 << p.shift) - 1))) * d;
 }
 
+// Two fp32 values in one 64-bit register, for the two-wide instructions: half the issue slots, the same arithmetic.
+typedef unsigned long long f2;
+__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) {
+  f2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ f2 mul2(f2 a, f2 b) {
+  f2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f2 add2(f2 a, f2 b) {
+  f2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f2 join2(float a, float b) {
+  f2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ f2 both(float a) { return join2(a, a); }
+__device__ __forceinline__ float2 split2(f2 v) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
+}
+
 struct RopeTable {
   unsigned long long turn[64]; // fraction of a turn per position, 64-bit fixed point
   int rot_dim, interleaved;    // rot_dim == 0: no rotation

@@ -26,8 +26,9 @@
 // the clock near 1600 MHz: 0.575 ms (670 TFLOP/s).  128 tokens over 102400 slots, 64/8 heads: 0.51 ms (840 TFLOP/s; 0.62
 // without the layout in waves, which keeps the eight row tiles of a KV head on the same keys at the same time).
 //
-// Probabilities are rounded to bf16 for the second product; the denominator sums them before that rounding, so lse is good
-// to fp32.  Every wait is bounded; a wait that runs out sets a flag that ends all others, the CTA drains its copies and
+// Probabilities are rounded to bf16 for the second product.  O is divided by the sum of the rounded ones, so that the
+// rounding of a probability moves the result only by how far its value is from the others' (with the other sum, a row that
+// one key dominates was off by half a step of bf16 besides the output's own); lse takes the sum before rounding.  Every wait is bounded; a wait that runs out sets a flag that ends all others, the CTA drains its copies and
 // frees its tensor memory, and the failure is recorded as a device check.  TMA reads and writes this GPU's memory only,
 // without multicast.
 #include "packed_plan.cuh"
@@ -55,7 +56,7 @@ struct Smem {
   static constexpr int kK = kQ + kQStages * kTile;
   static constexpr int kV = kK + kKStages * kTile;
   static constexpr int kRef = kV + kVStages * kTile;   // reference maxima, [kGroups (piece mod)][128] fp32
-  static constexpr int kSum = kRef + kGroups * 512;    // denominators handed to the finishing group, [2][128] fp32
+  static constexpr int kSum = kRef + kGroups * 512;    // sums handed to the finishing group, [2][128] fp32
   static constexpr int kPieces = kSum + 1024;          // kRing descriptors
   static constexpr int kBar = kPieces + 184;
   static constexpr int kMisc = kBar + 288;             // tensor memory address, failure flag, "merge" and "scrub" flags
@@ -130,6 +131,12 @@ __device__ __forceinline__ void mask_row(float* v, int limit) {
     if (i >= limit) v[i] = -INFINITY;
 }
 
+// lo += the lower, hi += the upper of two packed bf16 values (widened by the addition itself).
+__device__ __forceinline__ void add_bf16_pair(float& lo, float& hi, uint32_t packed) {
+  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tadd.rn.f32.bf16 %0, l, %0;\n\tadd.rn.f32.bf16 %1, h, %1;\n\t}"
+      : "+f"(lo), "+f"(hi) : "r"(packed));
+}
+
 // Pins registers that tcgen05.ld filled behind the wait for it.
 template <int kN>
 __device__ __forceinline__ void settle(float* v) {
@@ -149,7 +156,9 @@ struct Params {
   float scale;
   float* lse;
   float4* part_o;              // [slot][d/4][128]
-  float2* part_ml;             // [slot][128]
+  float2* part_ml;             // [slot][128] reference, sum of the rounded probabilities
+  float* part_l;               // [slot][128] sum of the probabilities
+  float* hand_l;               // [CTA][2][128] such sums on their way to the finishing group
   int* d_status;
   int Hq;
 };
@@ -507,8 +516,11 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
       // rows without a token follow the last one: their results are dropped
       const int vis = visible(p.seqs, sq, min(t_seq, min((pc.r + 1) * p.cfg.tokens, pc.n) - 1));
       float* ref_row = ref_max + (f % kGroups) * 128 + row;
-      float* l_row = x_l + row;                           // [0]: of the tile before the last, [128]: of the one before that
-      float m = -INFINITY, l = 0.f;
+      // sums of the groups with the tile before the last ([0]) and the one before that ([128]): of the rounded probabilities
+      // through shared memory, the exact ones, which only lse needs, through global memory (shared memory is full)
+      float* r_row = x_l + row;
+      volatile float* l_row = p.hand_l + (size_t)blockIdx.x * 256 + row;
+      float m = -INFINITY, l = 0.f, rl = 0.f;             // rl: sum of the rounded probabilities
       bool poison = false, ref_known = false;
 #pragma unroll 1
       for (int t = pc.tile0 + (int)((kGroups + g - T % kGroups) % kGroups); t < pc.tile1; t += kGroups) {
@@ -568,17 +580,29 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
             tmem_st32(tO + c0, o);
           }
           // denominators that other groups have handed over already follow too
-          if (t + 2 >= pc.tile1 && pc.tile1 - pc.tile0 > 2 && l_row[128] > 0.f) l_row[128] *= corr;
-          if (t + 1 == pc.tile1 && l_row[0] > 0.f) l_row[0] *= corr;
+          if (grow && t + 2 >= pc.tile1 && pc.tile1 - pc.tile0 > 2 && r_row[128] > 0.f) {
+            r_row[128] *= corr;
+            l_row[128] = l_row[128] * corr;
+          }
+          if (grow && t + 1 == pc.tile1 && r_row[0] > 0.f) {
+            r_row[0] *= corr;
+            l_row[0] = l_row[0] * corr;
+          }
           settled = true;
         }
         if (m != ref) {
-          l = l > 0.f ? l * fast_exp2(m - ref) : l;
+          const float corr = fast_exp2(m - ref);
+          l = l > 0.f ? l * corr : l;
+          rl = rl > 0.f ? rl * corr : rl;
           m = ref;
         }
         const float mu = m == -INFINITY ? 0.f : m;
         // second pass: probabilities, 32 columns at a time.  (No row sees slots behind `width`: the value product skips them.)
-        float sum0 = 0.f, sum1 = 0.f, sum2 = 0.f, sum3 = 0.f;
+        // The second sum and its hand-over cost 3 % (128 tokens over 102400) to 5 % (20 x 1536) of the time; with the rounded
+        // values widened by shifts and masks instead of the mixed-precision addition they cost 6 and 7 %.
+        f2 exact0 = 0ull, exact1 = 0ull;
+        float r0 = 0.f, r1 = 0.f, r2 = 0.f, r3 = 0.f;
+        const f2 sl22 = both(sl2), mu2 = both(-mu);
 #pragma unroll 1
         for (int c0 = 0; c0 < max(width, 1); c0 += 32) {
           float x[32];
@@ -589,24 +613,30 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
           uint32_t pk[16];
 #pragma unroll
           for (int i = 0; i < 32; i += 4) {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) x[i + k] = fast_exp2(fmaf(x[i + k], sl2, -mu));
-            sum0 += x[i];
-            sum1 += x[i + 1];
-            sum2 += x[i + 2];
-            sum3 += x[i + 3];
+            const float2 a = split2(fma2(join2(x[i], x[i + 1]), sl22, mu2)), b = split2(fma2(join2(x[i + 2], x[i + 3]), sl22, mu2));
+            x[i] = fast_exp2(a.x);
+            x[i + 1] = fast_exp2(a.y);
+            x[i + 2] = fast_exp2(b.x);
+            x[i + 3] = fast_exp2(b.y);
+            exact0 = add2(exact0, join2(x[i], x[i + 1]));
+            exact1 = add2(exact1, join2(x[i + 2], x[i + 3]));
             pk[i / 2] = pack_bf16(x[i], x[i + 1]);
             pk[i / 2 + 1] = pack_bf16(x[i + 2], x[i + 3]);
+            add_bf16_pair(r0, r1, pk[i / 2]);
+            add_bf16_pair(r2, r3, pk[i / 2 + 1]);
           }
           tmem_st16(tS + (c0 >> 1), pk);
         }
-        l += (sum0 + sum1) + (sum2 + sum3);
+        const float2 sums = split2(add2(exact0, exact1));
+        l += sums.x + sums.y;
+        float tile_r = (r0 + r1) + (r2 + r3);
         if (Tt > 0 && !settled) {
           wait(TURN + (Tt - 1) % kGroups, (Tt - 1) / kGroups);
           const float now = *ref_row;
           if (__any_sync(0xffffffffu, now != m)) {       // moved by a tile before this one: follow
             tmem_wait_st();
             const float corr = now != m ? fast_exp2(m - now) : 1.0f;
+            tile_r = 0.f;
 #pragma unroll 1
             for (int c0 = 0; c0 < kBN; c0 += 32) {
               float q[16];
@@ -616,18 +646,26 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
               for (int i = 0; i < 16; ++i)
                 pk[i] = pack_bf16(bf16_lo(__float_as_uint(q[i])) * corr, bf16_hi(__float_as_uint(q[i])) * corr);
               tmem_st16(tS + (c0 >> 1), pk);
+              if (c0 < width) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) tile_r += bf16_lo(pk[i]) + bf16_hi(pk[i]);
+              }
             }
             if (now != m) {
               l = l > 0.f ? l * corr : l;
+              rl = rl > 0.f ? rl * corr : rl;
               m = now;
             }
           }
         } else if (Tt > 0 && first) {
           wait(TURN + (Tt - 1) % kGroups, (Tt - 1) / kGroups);
         }
+        rl += tile_r;
         if (t + 2 == pc.tile1 || t + 3 == pc.tile1) {    // this group's last tile of the piece, but not the piece's last
           if (f > 0) wait(O_FREE, f - 1);                // (the piece before has read its own)
-          l_row[t + 2 == pc.tile1 ? 0 : 128] = poison ? __int_as_float(0x7fffffff) : l;
+          const int at = t + 2 == pc.tile1 ? 0 : 128;
+          r_row[at] = poison ? __int_as_float(0x7fffffff) : rl;
+          if (p.lse != nullptr) l_row[at] = l;
         }
         tmem_wait_st();
         tc_fence_before();
@@ -640,20 +678,24 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
       T = Tend;
       if (finishes) {
         // ---- the piece's result ----
-        if (poison) l = __int_as_float(0x7fffffff);
+        if (poison) l = rl = __int_as_float(0x7fffffff);
+        if (p.lse != nullptr) {                          // (ordered by the turns that the last tile has waited for)
+          if (pc.tile1 - pc.tile0 > 1) l += l_row[0];
+          if (pc.tile1 - pc.tile0 > 2) l += l_row[128];
+        }
         wait(PV_DONE + g, (T - 1) / kGroups);
         tc_fence_after();
 #pragma unroll
         for (int k = 0; k < kGroups - 1; ++k) {          // (their products come before this tile's)
-          const float l_other = pc.tile1 - pc.tile0 > k + 1 ? l_row[k * 128] : 0.f;
-          if (l_other != 0.f) l += l_other;              // (at the last tile's reference)
+          const float r_other = pc.tile1 - pc.tile0 > k + 1 ? r_row[k * 128] : 0.f;
+          if (r_other != 0.f) rl += r_other;             // (at the last tile's reference)
         }
         const bool store = valid && *s_fail == 0;
         const bool scrubbed = s_scrub[f % 4] == f + 1;
         const int tok = pc.first + t_seq, hq = pc.h * G + member;
         const uint32_t sO = base + L::kQ + (f % kQStages) * L::kTile;       // over the piece's Q tile: no product reads it now
         // a whole item is normalised into shared memory, a piece of a cut item goes to the workspace as it is
-        const float inv = l == 0.f ? 0.f : 1.0f / l;
+        const float inv = rl == 0.f ? 0.f : 1.0f / rl;
 #pragma unroll 1
         for (int c0 = 0; c0 < kD; c0 += 16) {
           float o[16];
@@ -673,7 +715,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
           if (pc.slot < 0) {
             uint32_t pk[8];
 #pragma unroll
-            for (int i = 0; i < 16; i += 2) pk[i / 2] = l == 0.f ? 0u : pack_bf16(o[i] * inv, o[i + 1] * inv);
+            for (int i = 0; i < 16; i += 2) pk[i / 2] = rl == 0.f ? 0u : pack_bf16(o[i] * inv, o[i + 1] * inv);
             stage_row<8>(pk, sO + (c0 >> 6) * (kBM * 128), row, (c0 & 63) >> 3);
           } else {
             float4* po = p.part_o + ((size_t)pc.slot * (kD / 4) + c0 / 4) * 128 + row;
@@ -688,7 +730,8 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         float m_out = m;
         if (pc.slot >= 0) {
           // whoever takes the last ticket merges the item's pieces in their order
-          p.part_ml[pc.slot * 128 + row] = make_float2(m, l);
+          p.part_ml[pc.slot * 128 + row] = make_float2(m, rl);
+          p.part_l[pc.slot * 128 + row] = l;
           __threadfence();
           __syncwarp();
           if (lane == 0) mbar_arrive(bar(PARTS + g));
@@ -708,13 +751,17 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
               m_out = x.y == 0.f ? m_out : fmaxf(m_out, x.x);
             }
             const float Mu = m_out == -INFINITY ? 0.f : m_out;
-            l = 0.f;
+            l = rl = 0.f;
 #pragma unroll 1
             for (int k = 0; k < pc.n_pieces; ++k) {
               const float2 x = __ldcg(p.part_ml + piece_slot(pc, k) * 128 + row);
-              if (x.y != 0.f) l += x.y * fast_exp2(x.x - Mu);
+              if (x.y != 0.f) {
+                const float w = fast_exp2(x.x - Mu);
+                rl += x.y * w;
+                l += __ldcg(p.part_l + piece_slot(pc, k) * 128 + row) * w;
+              }
             }
-            const float inv_all = l == 0.f ? 0.f : 1.0f / l;
+            const float inv_all = rl == 0.f ? 0.f : 1.0f / rl;
 #pragma unroll 1
             for (int c0 = 0; c0 < kD; c0 += 32) {
               float o[32];
@@ -739,13 +786,13 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
               }
               uint32_t pk[16];
 #pragma unroll
-              for (int i = 0; i < 32; i += 2) pk[i / 2] = l == 0.f ? 0u : pack_bf16(o[i] * inv_all, o[i + 1] * inv_all);
+              for (int i = 0; i < 32; i += 2) pk[i / 2] = rl == 0.f ? 0u : pack_bf16(o[i] * inv_all, o[i + 1] * inv_all);
               stage_row<16>(pk, sO + (c0 >> 6) * (kBM * 128), row, (c0 & 63) >> 3);
             }
           }
         }
         if (write) {
-          if (store && p.lse != nullptr) p.lse[(size_t)tok * p.Hq + hq] = l == 0.f ? -INFINITY : m_out * kLn2 + logf(l);
+          if (store && p.lse != nullptr) p.lse[(size_t)tok * p.Hq + hq] = rl == 0.f ? -INFINITY : m_out * kLn2 + logf(l);
           fence_proxy_async();
           __syncwarp();
           const unsigned rows_ok = __ballot_sync(0xffffffffu, store);
@@ -825,7 +872,9 @@ static cudaError_t launch(const Params& p, int ctas, cudaStream_t stream) {
 }  // namespace ptc
 
 constexpr int kTcSlots = kMaxUnits > 2 * kMaxPackedCtas ? kMaxUnits : 2 * kMaxPackedCtas;
-size_t packed_tc_scratch_bytes(int d) { return (size_t)kTcSlots * 128 * ((size_t)d * 4 + 8); }
+size_t packed_tc_scratch_bytes(int d) {
+  return (size_t)kTcSlots * 128 * ((size_t)d * 4 + 12) + (size_t)kMaxPackedCtas * 256 * 4;
+}
 
 cudaError_t launch_packed_tc(const samkv_packed_t& d, const Seqs& seqs, const KvSource& kv, const Rows& Q, float scale,
                              const Rows& O, float* lse, const samkv_ctx_impl& h, cudaStream_t stream) {
@@ -857,6 +906,8 @@ cudaError_t launch_packed_tc(const samkv_packed_t& d, const Seqs& seqs, const Kv
   char* ws = h.workspace + kStatusBytes;
   p.part_o = reinterpret_cast<float4*>(ws);
   p.part_ml = reinterpret_cast<float2*>(ws + (size_t)kTcSlots * 128 * d.head_dim * 4);
+  p.part_l = reinterpret_cast<float*>(p.part_ml + (size_t)kTcSlots * 128);
+  p.hand_l = p.part_l + (size_t)kTcSlots * 128;
   p.d_status = h.d_status;
   p.Hq = d.n_q_heads;
   if (d.head_dim == 128)

@@ -4,8 +4,8 @@ import pytest
 import torch
 
 from paper_2508_11661_b200 import binding as B
-from packed_testlib import DT, PagedCase, attend64, check_rows, f64
-from test_packed_gpu import DEV, run_paged
+from packed_testlib import DT, HALF_STEP, PagedCase, attend64, check_rows, f64
+from test_packed_gpu import DEV, check_prefill, randn, run_paged, run_prefill
 
 pytestmark = pytest.mark.gpu
 
@@ -93,3 +93,81 @@ def test_a_handle_made_behind_pending_work_of_its_workspace():
         B.samkv_paged_attn(h, p, pages, c.cache_len, c.Q, 0.0, True, O)
         assert B.samkv_poll_status(h) == 0
     assert torch.equal(O, ref)
+
+
+# ------------------------------------------------------------------------------------------------ rounding
+def tight_bound(q, k, v, vis, scale, O, Es, A, length):
+    """With a denominator that sums the very probabilities the product uses, their rounding errors e_j (half a step of 8
+    bits) move the result by sum_j w_j e_j (v_j - O) / (1 + sum_j w_j e_j): values that agree are not moved at all."""
+    n, Hq, d = q.shape
+    G = Hq // k.shape[0]
+    spread = np.zeros_like(O)
+    for t in range(n):
+        L = int(vis[t])
+        for h in range(k.shape[0]):
+            rows = slice(h * G, (h + 1) * G)
+            x = q[t, rows] @ k[h, :L].T * scale
+            p = np.exp(x - x.max(axis=1, keepdims=True))
+            w = p / p.sum(axis=1, keepdims=True)
+            spread[t, rows] = np.einsum("gl,gld->gd", w, np.abs(v[h, None, :L] - O[t, rows][:, None]))
+    sums = (length + 64) * 2.0 ** -24 + 2.0 ** -21
+    return 1.01 * HALF_STEP["bf16"] * (spread + np.abs(O)) + 1.01 * (2 * Es[..., None] + 2 * sums) * A + 1e-37
+
+
+@pytest.mark.parametrize("sharp", [1.0, 4.0, 12.0])
+def test_rounded_probabilities_cancel_in_prompts(sharp):
+    lens = [1, 40, 300, 777]
+    T, Hq, Hkv, d = sum(lens), 8, 2, 128
+    q, k, v = randn(T, Hq, d, seed=210), randn(T, Hkv, d, seed=211), randn(T, Hkv, d, seed=212)
+    k = (k * sharp).to(torch.bfloat16)
+    O, lse = run_prefill(q, k, v, lens, "bf16")
+    check_prefill(q, k, v, lens, "bf16", O, lse)
+    q6, k6, v6, o6 = f64(q), f64(k), f64(v), f64(O)
+    at = 0
+    for n in lens:
+        rows = np.unique(np.linspace(0, n - 1, 40).astype(int))
+        ks, vs, vis = k6[at:at + n].swapaxes(0, 1), v6[at:at + n].swapaxes(0, 1), rows + 1
+        ref, _, A, Es = attend64(q6[at + rows], ks, vs, vis, d ** -0.5)
+        tol = tight_bound(q6[at + rows], ks, vs, vis, d ** -0.5, ref, Es, A, n)
+        assert (np.abs(o6[at + rows] - ref) <= tol).all(), f"{n} tokens: {np.max(np.abs(o6[at + rows] - ref) / tol):.2f} of its bound"
+        at += n
+
+
+@pytest.mark.parametrize("new,cached,hint", [([1, 1, 2, 1], [33, 900, 64, 5001], 2), ([40, 17, 64], [200, 5001, 0], 0)])
+@pytest.mark.parametrize("sharp", [1.0, 4.0, 12.0])
+def test_rounded_probabilities_cancel_over_pages(new, cached, hint, sharp):
+    c = PagedCase(new, cached, 8, 2, 128, 64, "bf16", seed=213)
+    c.Kp *= sharp
+    O, lse = run_paged(c, max_seq=hint)
+    q, o = f64(c.Q), f64(O)
+    at = 0
+    for s, n in enumerate(new):
+        rows = np.unique(np.linspace(0, n - 1, 12).astype(int))
+        L = cached[s] + n
+        k, v, vis = c.slots(c.Kp, s, L), c.slots(c.Vp, s, L), cached[s] + rows + 1
+        ref, _, A, Es = attend64(q[at + rows], k, v, vis, 128 ** -0.5)
+        tol = tight_bound(q[at + rows], k, v, vis, 128 ** -0.5, ref, Es, A, L)
+        assert (np.abs(o[at + rows] - ref) <= tol).all(), f"{n} over {cached[s]}: {np.max(np.abs(o[at + rows] - ref) / tol):.2f} of its bound"
+        at += n
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("sharp", [1.0, 6.0])
+def test_equal_values_come_out_as_they_are(d, sharp):
+    """All slots hold one value row: whatever the weights, the result is that row.  Numerator and denominator sum the same
+    probabilities in fp32, off by (L + 64) 2^-24 each at most, 1.1e-3 together for L = 9041; half a step of bf16 is 2^-9 =
+    1.95e-3 of the value at least, so that rounding lands on the value itself."""
+    row = randn(2, d, seed=214)
+    lens = [1, 40, 300, 1500]
+    T = sum(lens)
+    q, k = randn(T, 8, d, seed=215), (randn(T, 2, d, seed=216) * sharp).to(torch.bfloat16)
+    v = row[None].expand(T, 2, d).contiguous()
+    want = row.repeat_interleave(4, dim=0)
+    O, _ = run_prefill(q, k, v, lens, "bf16")
+    assert torch.equal(O, want[None].expand_as(O))
+    for new, cached, hint in (([1, 1, 2], [1000, 9001, 17], 2), ([40, 64, 5], [9001, 0, 700], 0)):
+        c = PagedCase(new, cached, 8, 2, d, 64, "bf16", seed=217)
+        c.Kp *= sharp
+        c.Vp = row[None, :, None].expand_as(c.Vp).contiguous()
+        O, _ = run_paged(c, max_seq=hint)
+        assert torch.equal(O, want[None].expand_as(O)), (new, cached)
