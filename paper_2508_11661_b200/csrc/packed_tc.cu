@@ -10,9 +10,12 @@
 //   warp 15     loads V (three stages), sees to value rows that not every query row sees
 // All groups add into ONE accumulator.  They share a reference maximum per row: a piece's first tile sets it, the others
 // use it as it stands, since it only has to be within a factor of 2^64 of the row's maximum (P is bf16 and O, l are fp32:
-// all have the exponent range for it).  A tile that needs a larger one waits for everything before it and rescales O in
-// tensor memory; tiles behind it that used the old one notice before they hand over their probabilities and rescale
-// those.  P(T) overlays the first half of S(T), so tensor memory holds three score buffers and O: 512 columns.
+// all have the exponent range for it).  A tile that needs a
+// larger one waits for everything before it and rescales O in tensor memory; tiles behind it that used the old one rescale
+// their probabilities before they hand them over.  A reference moves by whole steps of log2, so that rescaled
+// probabilities are not rounded again.  Which reference a row's tile starts from is fixed (the first tile's, or the one
+// its group ended the tile three before with), and each row decides for itself, so that results repeat bit for bit and
+// depend on no other row.  P(T) overlays the first half of S(T), so tensor memory holds three score buffers and O: 512 columns.
 // The group with a piece's last tile writes the result while the others are at the next piece's tiles.
 //
 // What bounds it.  A tile costs 1024 cycles on the tensor pipe (16 products of 64 cycles), 1024 on the special-function
@@ -57,12 +60,12 @@ struct Smem {
   static constexpr int kV = kK + kKStages * kTile;
   static constexpr int kRef = kV + kVStages * kTile;   // reference maxima, [kGroups (piece mod)][128] fp32
   static constexpr int kSum = kRef + kGroups * 512;    // sums handed to the finishing group, [2][128] fp32
-  static constexpr int kPieces = kSum + 1024;          // kRing descriptors
-  static constexpr int kBar = kPieces + 184;
-  static constexpr int kMisc = kBar + 288;             // tensor memory address, failure flag, "merge" and "scrub" flags
-  static constexpr int kBytes = kMisc + 40;
+  static constexpr int kBar = kSum + 1024;
+  static constexpr int kPieces = kBar + 296;           // kRing descriptors
+  static constexpr int kMisc = kPieces + 180;          // tensor memory address, failure flag, "merge" and "scrub" flags
+  static constexpr int kBytes = kMisc + 36;
 };
-static_assert(kRing * sizeof(Piece) <= 184, "descriptors");
+static_assert(kRing * sizeof(Piece) <= 180, "descriptors");
 
 static_assert(Smem<128>::kBytes <= 232448, "shared memory of one CTA");
 
@@ -75,9 +78,11 @@ enum Bar {
   S_FULL = V_TMA + 1, PV_DONE = S_FULL + kGroups,
   TURN = PV_DONE + kGroups,             // tile T's probabilities are final
   REF = TURN + kGroups,                 // a piece's first tile has set the reference
-  O_FREE = REF + kGroups, PARTS = O_FREE + 1, MERGE = PARTS + kGroups, kBars = MERGE + kGroups
+  O_FREE = REF + kGroups, PARTS = O_FREE + 1, MERGE = PARTS + kGroups,
+  SEEN = MERGE + kGroups,               // a piece's third tile has read the reference that the first one set
+  kBars = SEEN + 1
 };
-static_assert(kBars * 8 <= 288, "barrier area");
+static_assert(kBars * 8 <= 296, "barrier area");
 static_assert(kVStages == kGroups, "a V stage is free when the value product of its group has completed");
 
 // maximum that keeps NaN
@@ -285,6 +290,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
       mbar_init(bar(MERGE + i), 1);
     }
     mbar_init(bar(O_FREE), 4);
+    mbar_init(bar(SEEN), 4);
     for (int i = 0; i < 4; ++i) s_scrub[i] = 0;
     *s_fail = (base & 1023u) != 0;          // (never seen: the declaration asks for 1024 bytes)
     if (*s_fail) atomicMax(p.d_status, (int)CHECK_SMEM_ALIGNMENT);
@@ -499,7 +505,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     const uint32_t tS = lane_addr + g * kBN, tO = lane_addr + kColO;      // P overlays the first half of the scores
     const float sl2 = p.scale * kLog2e;
     const int t_local = row / G, member = row - t_local * G;
-    uint32_t f = 0, T = 0, n_merged = 0;
+    uint32_t f = 0, T = 0, n_merged = 0, n_seen = 0;     // n_seen: pieces of three or more tiles
     while (true) {
       if (!wait(FR_FULL + f % kRing, f / kRing)) break;
       const Piece pc = ring[f % kRing];
@@ -550,45 +556,53 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         }
         const float cand = max3_nan(max3_nan(mx0, mx1, mx2), mx3, mx3) * sl2;
         poison |= !(cand < INFINITY);                    // NaN or +infinity among the row's scores
-        // The piece's first tile sets the row's reference; the others use it as it stands.  Whether a tile before this one
+        // The piece's first tile sets the row's reference; the others use the one they know.  Whether a tile before this one
         // has moved it meanwhile is looked at when the probabilities are done.
         const bool first = t == pc.tile0;
         if (!first && !ref_known) wait(REF + f % kGroups, f / kGroups);
+        float ref = first ? cand : ref_known ? m : *ref_row;
         ref_known = true;
-        float ref = first ? cand : *ref_row;
-        bool settled = first;
         if (first) {
           *ref_row = ref;
           __syncwarp();
           if (lane == 0) mbar_arrive(bar(REF + f % kGroups));
-        } else if (__any_sync(0xffffffffu, cand - ref > kGrow || (ref == -INFINITY && cand > -INFINITY))) {
-          // some row needs a larger reference: O has to follow, so everything before this tile is finished first
-          wait(TURN + (Tt - 1) % kGroups, (Tt - 1) / kGroups);
-          wait(PV_DONE + (Tt - 1) % kGroups, (Tt - 1) / kGroups);
-          tc_fence_after();
-          ref = *ref_row;
-          const bool grow = cand - ref > kGrow || (ref == -INFINITY && cand > -INFINITY);
-          const float corr = grow ? fast_exp2(ref - cand) : 1.0f;
-          if (grow) *ref_row = cand;
-          if (grow) ref = cand;
+        } else {
+          if (t == pc.tile0 + 2) {                       // (the second tile may move it from here on)
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(SEEN));
+          }
+          auto too_small = [&](float r) { return cand - r > kGrow || (r == -INFINITY && cand > -INFINITY); };
+          const bool far = too_small(ref);
+          if (__any_sync(0xffffffffu, far)) {
+            // some row needs a larger reference: O has to follow, so everything before this tile is finished first
+            wait(TURN + (Tt - 1) % kGroups, (Tt - 1) / kGroups);
+            wait(PV_DONE + (Tt - 1) % kGroups, (Tt - 1) / kGroups);
+            if (t == pc.tile0 + 1 && pc.tile1 - pc.tile0 > 2) wait(SEEN, n_seen);
+            tc_fence_after();
+            const float old = *ref_row;
+            const bool grow = far && too_small(old);
+            const float step = rintf(cand - old), up = step < 1e7f ? old + step : cand;
+            const float corr = grow ? fast_exp2(old - up) : 1.0f;
+            if (grow) *ref_row = up;
+            if (far) ref = grow ? up : old;
 #pragma unroll 1
-          for (int c0 = 0; c0 < kD; c0 += 32) {
-            float o[32];
-            tmem_ld32(tO + c0, o);
+            for (int c0 = 0; c0 < kD; c0 += 32) {
+              float o[32];
+              tmem_ld32(tO + c0, o);
 #pragma unroll
-            for (int i = 0; i < 32; ++i) o[i] *= corr;
-            tmem_st32(tO + c0, o);
+              for (int i = 0; i < 32; ++i) o[i] *= corr;
+              tmem_st32(tO + c0, o);
+            }
+            // denominators that other groups have handed over already follow too
+            if (grow && t + 2 >= pc.tile1 && pc.tile1 - pc.tile0 > 2 && r_row[128] > 0.f) {
+              r_row[128] *= corr;
+              l_row[128] = l_row[128] * corr;
+            }
+            if (grow && t + 1 == pc.tile1 && r_row[0] > 0.f) {
+              r_row[0] *= corr;
+              l_row[0] = l_row[0] * corr;
+            }
           }
-          // denominators that other groups have handed over already follow too
-          if (grow && t + 2 >= pc.tile1 && pc.tile1 - pc.tile0 > 2 && r_row[128] > 0.f) {
-            r_row[128] *= corr;
-            l_row[128] = l_row[128] * corr;
-          }
-          if (grow && t + 1 == pc.tile1 && r_row[0] > 0.f) {
-            r_row[0] *= corr;
-            l_row[0] = l_row[0] * corr;
-          }
-          settled = true;
         }
         if (m != ref) {
           const float corr = fast_exp2(m - ref);
@@ -630,8 +644,8 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         const float2 sums = split2(add2(exact0, exact1));
         l += sums.x + sums.y;
         float tile_r = (r0 + r1) + (r2 + r3);
-        if (Tt > 0 && !settled) {
-          wait(TURN + (Tt - 1) % kGroups, (Tt - 1) / kGroups);
+        if (Tt > 0) wait(TURN + (Tt - 1) % kGroups, (Tt - 1) / kGroups);
+        if (!first) {
           const float now = *ref_row;
           if (__any_sync(0xffffffffu, now != m)) {       // moved by a tile before this one: follow
             tmem_wait_st();
@@ -657,8 +671,6 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
               m = now;
             }
           }
-        } else if (Tt > 0 && first) {
-          wait(TURN + (Tt - 1) % kGroups, (Tt - 1) / kGroups);
         }
         rl += tile_r;
         if (t + 2 == pc.tile1 || t + 3 == pc.tile1) {    // this group's last tile of the piece, but not the piece's last
@@ -676,6 +688,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         }
       }
       T = Tend;
+      if (pc.tile1 - pc.tile0 > 2) ++n_seen;
       if (finishes) {
         // ---- the piece's result ----
         if (poison) l = rl = __int_as_float(0x7fffffff);

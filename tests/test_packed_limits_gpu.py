@@ -1,4 +1,6 @@
 """Packed and paged calls where their rounding, their bounds and their hand-overs are easiest to get wrong."""
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -171,3 +173,50 @@ def test_equal_values_come_out_as_they_are(d, sharp):
         c.Vp = row[None, :, None].expand_as(c.Vp).contiguous()
         O, _ = run_paged(c, max_seq=hint)
         assert torch.equal(O, want[None].expand_as(O)), (new, cached)
+
+
+# ------------------------------------------------------------------------------------------------ references that move
+def ramp_case(new, cached, step, big=1.0, seed=220, jitter=0.0):
+    """Scores that rise by `step` (in units of log 2) from slot to slot, in element 0 of the keys; scale 1."""
+    c = PagedCase(new, cached, 8, 2, 128, 64, "bf16", seed=seed)
+    c.Q[..., 0] = math.log(2.0)
+    c.Q[..., 1:] *= jitter
+    for s, n in enumerate(new):
+        for j in range(cached[s] + n):
+            c.Kp[int(c.table_cpu[s, j // 64]), :, j % 64, 0] = step * j
+    c.Vp *= big
+    return c
+
+
+def check_paged_scaled(c, O, lse):
+    q, o, l = f64(c.Q), f64(O), f64(lse)
+    at = 0
+    for s, n in enumerate(c.new):
+        L = c.cached[s] + n
+        ref = attend64(q[at:at + n], c.slots(c.Kp, s, L), c.slots(c.Vp, s, L), c.cached[s] + np.arange(1, n + 1), 1.0)
+        check_rows(o[at:at + n], l[at:at + n], ref, "bf16", L, f"sequence {s}")
+        at += n
+
+
+@pytest.mark.parametrize("step", [0.05, 0.2, 1.0])
+def test_a_moving_reference_repeats_bit_for_bit(step):
+    """Rows whose reference moves in one tile after the other, while other groups are at work with the old one."""
+    c = ramp_case([40, 128, 300], [700, 2000, 0], step, seed=221, jitter=0.3)
+    O, lse = run_paged(c, scale=1.0)
+    check_paged_scaled(c, O, lse)
+    q, o = f64(c.Q), f64(O)                              # not rounded twice: see tight_bound
+    rows = np.arange(40, 168, 9)
+    k, v, vis = c.slots(c.Kp, 1, 2128), c.slots(c.Vp, 1, 2128), 2000 + rows - 40 + 1
+    ref, _, A, Es = attend64(q[rows], k, v, vis, 1.0)
+    assert (np.abs(o[rows] - ref) <= tight_bound(q[rows], k, v, vis, 1.0, ref, Es, A, 2128)).all()
+    p = B.Packed(c.Hq, c.Hkv, c.d, c.offsets, c.T, 0, c.dtype)
+    h = B.Handle.for_packed(p)
+    pages = B.Pages(c.Kp, c.Vp, c.table)
+    other = torch.empty((64 << 20,), dtype=torch.uint8, device=DEV)
+    for i in range(60):
+        O2, lse2 = torch.zeros_like(O), torch.zeros_like(lse)
+        if i % 3 == 1:
+            other.fill_(i)
+        B.samkv_paged_attn(h, p, pages, c.cache_len, c.Q, 1.0, True, O2, lse2)
+        assert torch.equal(O, O2) and torch.equal(lse, lse2), f"call {i}"
+    assert B.samkv_poll_status(h) == 0
