@@ -400,8 +400,9 @@ size_t samkv_packed_workspace_bytes(const samkv_packed_t* packed);
  * K and V may be the [n_kv_heads, L_tot, d] slabs of one request that samkv_score and samkv_compact read later.
  * Values of K and V behind a row's own position never reach that row, infinities and NaN included.
  * Precision as for samkv_attn: bf16 probabilities are rounded to bf16 before the second product and O is divided by the
- * sum of the rounded ones; lse is taken before that rounding.  SAMKV_ERR_WORKSPACE if the handle's workspace is too
- * small. */
+ * sum of the rounded ones; lse is taken before that rounding.  Sums of weights times values are formed in fp32 before the
+ * division, with weights of up to 2^16.5 in bf16 and 1 in fp32: finite values of V beyond 2^128 / (slots * weight) can come
+ * out as infinities.  SAMKV_ERR_WORKSPACE if the handle's workspace is too small. */
 samkv_status_t samkv_prefill(samkv_handle_t h, const samkv_packed_t* packed, const samkv_rows_t* Q,
                              const samkv_rows_t* K, const samkv_rows_t* V, float scale, const samkv_rows_t* O,
                              float* lse, void* stream);

@@ -9,8 +9,8 @@
 //   warp 14     walks the plan, loads Q (two buffers) and K (two stages) by TMA
 //   warp 15     loads V (three stages), sees to value rows that not every query row sees
 // All groups add into ONE accumulator.  They share a reference maximum per row: a piece's first tile sets it, the others
-// use it as it stands, since it only has to be within a factor of 2^64 of the row's maximum (P is bf16 and O, l are fp32:
-// all have the exponent range for it).  A tile that needs a
+// use it as it stands, since it only has to be within a factor of 2^16 of the row's maximum (P is bf16 and O, l are fp32:
+// all have the exponent range for it, and values of 2^90 over 10^5 slots still add up below 2^128).  A tile that needs a
 // larger one waits for everything before it and rescales O in tensor memory; tiles behind it that used the old one rescale
 // their probabilities before they hand them over.  A reference moves by whole steps of log2, so that rescaled
 // probabilities are not rounded again.  Which reference a row's tile starts from is fixed (the first tile's, or the one
@@ -49,7 +49,7 @@ constexpr int kWarpS = 4 * kGroups, kWarpPV = kWarpS + 1, kWarpK = kWarpS + 2, k
 constexpr int kRegsSoftmax = 144, kRegsOther = 80;     // 384 x 144 + 128 x 80 = 512 x 128, the launch's registers
 // Waits are within a CTA and last microseconds; a poll that suspends takes about 4 us.
 constexpr uint32_t kWaitPolls = 1u << 17, kDrainPolls = 1u << 10;
-constexpr float kGrow = 64.0f;                         // log2
+constexpr float kGrow = 16.0f;                         // log2
 constexpr uint32_t kTmemCols = 512, kColO = 384;       // three score buffers of 128 columns, then O
 
 template <int kD>

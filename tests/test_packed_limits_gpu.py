@@ -188,6 +188,16 @@ def ramp_case(new, cached, step, big=1.0, seed=220, jitter=0.0):
     return c
 
 
+@pytest.mark.parametrize("new,cached,hint", [([1, 2], [400, 300], 2), ([40, 64], [400, 100], 0)])
+def test_large_values_stay_finite_while_scores_rise(new, cached, hint):
+    """Values near 2^90 under scores that rise by 2^19 per 128 slots.  A weight is at most 2^16.5 before its reference moves,
+    so that every sum stays below 2^16.5 * 500 * 2^93 < 2^119."""
+    c = ramp_case(new, cached, 0.15, big=2.0 ** 90)
+    O, lse = run_paged(c, max_seq=hint, scale=1.0)
+    assert bool(O.isfinite().all())
+    check_paged_scaled(c, O, lse)
+
+
 def check_paged_scaled(c, O, lse):
     q, o, l = f64(c.Q), f64(O), f64(lse)
     at = 0
