@@ -377,7 +377,7 @@ typedef struct {
 /* Rotary position encoding of the first rot_dim elements of a row: pair i is (i, i + rot_dim/2), or (2i, 2i+1) when
  * interleaved; (a, b) -> (a cos - b sin, b cos + a sin), angle = position * base^(-2i/rot_dim), or position *
  * inv_freq[i] when inv_freq is given (host double [rot_dim/2], finite, read during the call).  Angles are reduced
- * exactly (64-bit fixed point), so positions may be as large as int32 allows, or negative. */
+ * exactly (64-bit fixed point), so positions may be as large as int32 allows (cache_len[s] + t may pass it), or negative. */
 typedef struct {
   int32_t rot_dim;             /* multiple of 16, 16 .. head_dim */
   int32_t interleaved;

@@ -43,7 +43,7 @@ append_rope_kernel(const __grid_constant__ AppendArgs a, const __grid_constant__
   __shared__ float2 cs[kMaxAppendTokens][kD / 2];
   __shared__ long long page_row[kMaxAppendTokens];   // row of (page, head 0) in the pools, -1: do not write
   __shared__ int live[kMaxAppendTokens];             // the token belongs to a sequence
-  __shared__ int pos[kMaxAppendTokens];
+  __shared__ long long pos[kMaxAppendTokens];        // (cache_len + t passes 32 bits)
   const int tid = threadIdx.x;
   const int tok0 = blockIdx.x * tokens_per_cta;
   const int n_tok = min(tokens_per_cta, a.seqs.n_tokens - tok0);
@@ -57,15 +57,15 @@ append_rope_kernel(const __grid_constant__ AppendArgs a, const __grid_constant__
       const int mid = (lo + hi + 1) >> 1;
       if (a.seqs.off[mid] <= tok) lo = mid; else hi = mid - 1;
     }
-    int mine = 0, p = 0;
-    long long row = -1;
+    int mine = 0;
+    long long p = 0, row = -1;
     if (lo < a.seqs.n_seq) {
       const Seq sq = load_seq(a.seqs, lo);
       if (tok >= sq.first && tok < sq.first + sq.n) {
         mine = 1;
         const long long slot = (long long)sq.base + (tok - sq.first);
         if (sq.clamped) atomicMax(d_status, (int)CHECK_SEQ_RANGE);
-        p = a.positions != nullptr ? a.positions[tok] : (int)slot;
+        p = a.positions != nullptr ? a.positions[tok] : slot;
         if (a.has_pages) {
           const long long col = slot >> a.pages.shift;
           if (col >= a.pages.width) {
@@ -88,7 +88,7 @@ append_rope_kernel(const __grid_constant__ AppendArgs a, const __grid_constant__
   const int half = rope.rot_dim >> 1;
   for (int i = tid; i < n_tok * half; i += kAppendThreads) {
     const int t = i / half, e = i - t * half;
-    cs[t][e] = turn_sincos((unsigned long long)(long long)pos[t] * rope.turn[e]);
+    cs[t][e] = turn_sincos((unsigned long long)pos[t] * rope.turn[e]);
   }
   __syncthreads();
 

@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from paper_2508_11661_b200 import binding as B
-from packed_testlib import DT, HALF_STEP, PagedCase, attend64, check_rows, f64
+from packed_testlib import DT, HALF_STEP, PagedCase, attend64, check_rows, f64, rotate_bound
 from test_packed_gpu import DEV, check_prefill, randn, run_paged, run_prefill
 
 pytestmark = pytest.mark.gpu
@@ -230,3 +230,29 @@ def test_a_moving_reference_repeats_bit_for_bit(step):
         B.samkv_paged_attn(h, p, pages, c.cache_len, c.Q, 1.0, True, O2, lse2)
         assert torch.equal(O, O2) and torch.equal(lse, lse2), f"call {i}"
     assert B.samkv_poll_status(h) == 0
+
+
+# ------------------------------------------------------------------------------------------------ append
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_append_positions_pass_31_bits(dtype):
+    """Without pages cache_len is only where the positions start: the last of them lie behind 2^31 - 1."""
+    c = PagedCase([6, 5], [0, 0], 4, 2, 64, 16, dtype, seed=230)
+    p = B.Packed(4, 2, 64, c.offsets, c.T, 0, dtype)
+    h = B.Handle.for_packed(p)
+    first = [2**31 - 3, 2**31 - 1]
+    # turns of 2^-8 to 2^-39 per position: whole numbers of steps, which the 64-bit form counts exactly
+    freq = [2.0 * math.pi * 2.0 ** -(8 + i) for i in range(32)]
+    K_out, V_out, Q_out = torch.empty_like(c.K), torch.empty_like(c.V), torch.empty_like(c.Q)
+    B.samkv_append(h, p, c.K, c.V, None, torch.tensor(first, dtype=torch.int32, device=DEV), B.Rope(64, inv_freq=freq), None,
+                   c.Q, Q_out, K_out, V_out)
+    assert B.samkv_poll_status(h) == 0
+    pos = np.concatenate([first[0] + np.arange(6), first[1] + np.arange(5)]).astype(np.int64)
+    turn = np.array([[int(x) % 2 ** (8 + i) / 2.0 ** (8 + i) for i in range(32)] for x in pos])
+    for src, got in ((c.K, K_out), (c.Q, Q_out)):
+        x = f64(src)
+        a, b, cs, sn = x[..., :32], x[..., 32:], np.cos(2 * np.pi * turn)[:, None], np.sin(2 * np.pi * turn)[:, None]
+        want = np.concatenate([a * cs - b * sn, b * cs + a * sn], axis=-1)
+        # the doubles 2 pi 2^-k are off by 2^-53, and so is the angle: 2^31 * 2 pi 2^-8 * 2^-53 = 1.3e-8 more
+        tol = rotate_bound(x, want, 64, False, dtype) + 1.3e-8 * (np.abs(a) + np.abs(b)).repeat(2, axis=-1).max()
+        assert (np.abs(f64(got) - want) <= tol).all()
+    assert torch.equal(V_out, c.V)
