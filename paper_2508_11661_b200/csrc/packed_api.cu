@@ -89,7 +89,7 @@ samkv_status_t make_rope(const samkv_packed_t& p, const samkv_rope_t* r, RopeTab
 
 bool same_rows(const Rows& a, const Rows& b) { return a.data == b.data && a.ts == b.ts && a.hs == b.hs; }
 
-// Elements from the first to one past the last of a packed tensor.
+// May two packed tensors share memory?  (No only where their strides show it.)
 bool rows_overlap(const samkv_packed_t& p, const Rows& a, int heads_a, const Rows& b, int heads_b) {
   const long long e = p.dtype == SAMKV_BF16 ? 2 : 4;
   auto bytes = [&](const Rows& r, int heads) {
@@ -97,14 +97,17 @@ bool rows_overlap(const samkv_packed_t& p, const Rows& a, int heads_a, const Row
   };
   const char *a0 = (const char*)a.data, *b0 = (const char*)b.data;
   if (a0 + bytes(a, heads_a) <= b0 || b0 + bytes(b, heads_b) <= a0) return false;
-  // Interleaved slices of one matrix share an address range without sharing rows: with one token stride, two slices
-  // whose heads lie in disjoint column ranges of it do not overlap.
-  if (a.ts == b.ts) {
-    const long long ts = a.ts * e, wa = e * ((heads_a - 1) * a.hs + p.head_dim), wb = e * ((heads_b - 1) * b.hs + p.head_dim);
-    long long gap = (b0 - a0) % ts;
-    if (gap < 0) gap += ts;
-    if (gap >= wa && gap + wb <= ts) return false;
-  }
+  // Slices of one matrix or slab share an address range without sharing rows: with one stride along an axis, two tensors
+  // that lie in disjoint ranges of it at every step do not overlap.  (Columns of one fused matrix: the token axis; heads of
+  // K and V that alternate in one slab: the head axis.)
+  auto apart = [&](long long stride, long long width_a, long long width_b) {
+    long long gap = (b0 - a0) % stride;
+    if (gap < 0) gap += stride;
+    return gap >= width_a && gap + width_b <= stride;
+  };
+  const long long row = e * p.head_dim;
+  if (a.ts == b.ts && apart(a.ts * e, e * (heads_a - 1) * a.hs + row, e * (heads_b - 1) * b.hs + row)) return false;
+  if (a.hs == b.hs && apart(a.hs * e, e * (p.n_tokens - 1) * a.ts + row, e * (p.n_tokens - 1) * b.ts + row)) return false;
   return true;
 }
 
