@@ -29,17 +29,28 @@ cudaError_t launch_packed_attn(const samkv_packed_t& p, const Seqs& seqs, const 
   const int longest = p.max_seq_tokens > 0 ? p.max_seq_tokens : (p.n_tokens <= p.n_seq ? 1 : p.n_tokens);
   const bool few_rows = (long long)longest * G <= 16;
   if (p.dtype == SAMKV_F32) {
-    // Tiles of 64 rows are the quickest per row, but need work for every SM; tiles of 8 rows (their warps on their own) fill
-    // it with less, and waste nothing where a sequence has few rows.  Around the borders, 8/2 heads, 8 rows against 64:
-    // 4 x 156 tokens of 64 elements 23.6 against 21.3 us, 800 of 128 74.7 against 81.2, 33 tokens over 2049 slots (4/2 heads
-    // of 64) 16.8 against 46.1.  Short prompts have one or two key tiles per item, so 8-row items are mostly fixed cost:
-    // 12 x 37 tokens of 64 elements take 14.9 us with 8 rows, 9.2 with 32 and 11.7 with 64.
-    const long long rows = (long long)p.n_tokens * p.n_q_heads;
+    // Tiles of 64 rows are the quickest per row but need work for every SM; tiles of 8 rows fill it with an eighth of that
+    // and waste nothing where a sequence has few rows; 32 rows lie between.  What decides is the number of 8-row tiles per
+    // SM (x below, rows / 8 / SMs).  Measured, us with 8 / 32 / 64 rows:
+    //   prompts, d = 64:   x 1.7 (256 tokens, 8/2 heads) 16.8 / 20.3 / 26.0,  x 2.2 (320) 19.0 / 24.1 / 31.4,  x 2.6 (4 x 192, 4/2)
+    //                      18.2 / 16.5 / 21.7,  x 4.3 (4 x 320, 4/2) 33.3 / 28.8 / 32.0,  x 5.2 (4 x 192, 8/2) 28.8 / 28.0 / 21.2
+    //   prompts, d = 128:  x 2.2 (320, 8/2) 26.9 / 38.2 / 50.1,  x 3.5 (4 x 128) 23.8 / 19.2 / 24.7,  x 5.2 (4 x 192) 40.1 / 45.0 / 33.2
+    //   one key tile, d = 64 (where an item is mostly its fixed cost): x 0.9 (4 x 64, 4/2) 6.3 / 8.8 / 11.6,  x 1.7 (4 x 64, 8/2)
+    //                      9.3 / 8.7 / 11.1,  x 1.8 (16 x 33, 4/2) 11.2 / 8.1 / 10.7
+    //   pages, d = 64:     x 1.8 (16 x 33 over 512) 29.2 / 39.8 / 43.1,  x 3.5 (16 x 64 over 2049) 122 / 130 / 97,  (4 x 256
+    //                      over 512) 50.0 / 51.9 / 49.0, over an empty cache, which the host cannot tell, 21.5 / 20.6 / 27.7
+    //   pages, d = 128:    x 3.6 (16 x 33 over 512) 62.4 / 85.7 / 83.6,  x 6.9 (16 x 64 over 512) 110 / 129 / 92
+    const long long rows = (long long)p.n_tokens * p.n_q_heads, per_x = 8LL * h.sm_count;
     const bool wide = p.head_dim == 128;
     int tile = 8;
     if (!few_rows && rows >= 64LL * p.n_seq * p.n_kv_heads) {
-      if (rows >= (wide ? 40LL : 32LL) * h.sm_count) tile = 64;
-      else if (!kv.paged && p.n_tokens <= (wide ? 48LL : 256LL) * p.n_seq) tile = 32;
+      if (kv.paged) {
+        if (rows >= (wide ? 5 : 3) * per_x) tile = 64;
+      } else {
+        const bool short_prompts = !wide && p.n_tokens <= 64LL * p.n_seq;
+        if (2 * rows >= (wide ? 7 : 9) * per_x) tile = 64;                // x of 3.5 or 4.5
+        else if (4 * rows >= (short_prompts ? 5 : 10) * per_x) tile = 32; // x of 1.25 or 2.5
+      }
     }
     if (G > 8 && tile == 8) tile = 32;
     return launch_packed_f32(p, seqs, kv, Q, scale, O, lse, tile, h, stream);

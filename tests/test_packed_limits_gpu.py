@@ -7,7 +7,7 @@ import torch
 
 from paper_2508_11661_b200 import binding as B
 from packed_testlib import DT, HALF_STEP, PagedCase, attend64, check_rows, f64, rotate_bound
-from test_packed_gpu import DEV, check_prefill, randn, run_paged, run_prefill
+from test_packed_gpu import DEV, check_paged, check_prefill, randn, run_paged, run_prefill
 
 pytestmark = pytest.mark.gpu
 
@@ -256,3 +256,22 @@ def test_append_positions_pass_31_bits(dtype):
         tol = rotate_bound(x, want, 64, False, dtype) + 1.3e-8 * (np.abs(a) + np.abs(b)).repeat(2, axis=-1).max()
         assert (np.abs(f64(got) - want) <= tol).all()
     assert torch.equal(V_out, c.V)
+
+
+# ------------------------------------------------------------------------------------------------ heights of a row tile
+@pytest.mark.parametrize("d,heads,lens", [
+    (64, (8, 2), [250, 150]), (128, (8, 2), [250, 150]), (64, (4, 2), [257] * 4),       # 32 rows
+    (64, (4, 2), [64] * 7), (64, (4, 2), [33] * 16),                                    # prompts of one key tile: 8 and 32
+    (64, (8, 2), [640, 60, 1]), (128, (8, 2), [520]), (64, (4, 2), [1024, 409])])       # 64 rows, at the border
+def test_fp32_prompts_of_every_tile_height(d, heads, lens):
+    T = sum(lens) + 1
+    q, k, v = (randn(T, h, d, dtype="f32", seed=250 + i) for i, h in enumerate((heads[0], heads[1], heads[1])))
+    O, lse = run_prefill(q, k, v, lens, "f32")
+    check_prefill(q, k, v, lens, "f32", O, lse)
+
+
+@pytest.mark.parametrize("d,new", [(64, [200, 40, 210]), (64, [64, 70, 300, 20]), (128, [600, 130, 20])])
+def test_fp32_chunks_of_tall_tiles(d, new):
+    c = PagedCase(new, [100, 0, 513, 64][:len(new)], 8, 2, d, 32, "f32", seed=253, garbage=float("nan"))
+    O, lse = run_paged(c)
+    check_paged(c, O, lse)
