@@ -8,15 +8,18 @@ namespace samkv {
 size_t packed_tc_scratch_bytes(int d);
 cudaError_t launch_packed_tc(const samkv_packed_t& d, const Seqs& seqs, const KvSource& kv, const Rows& Q, float scale,
                              const Rows& O, float* lse, const samkv_ctx_impl& h, cudaStream_t stream);
+size_t packed_decode_scratch_bytes(int d);
 cudaError_t launch_packed_decode(const samkv_packed_t& d, const Seqs& seqs, const KvSource& kv, const Rows& Q, float scale,
                                  const Rows& O, float* lse, const samkv_ctx_impl& h, cudaStream_t stream);
 size_t packed_f32_scratch_bytes(int d);
 cudaError_t launch_packed_f32(const samkv_packed_t& d, const Seqs& seqs, const KvSource& kv, const Rows& Q, float scale,
                               const Rows& O, float* lse, int rows, const samkv_ctx_impl& h, cudaStream_t stream);
 
-// (the decode kernel's partial results are an eighth of the tensor-memory kernel's)
+// (which kernel a call gets depends on its lengths, the workspace does not)
 size_t packed_scratch_bytes(const samkv_packed_t& p) {
-  return p.dtype == SAMKV_BF16 ? packed_tc_scratch_bytes(p.head_dim) : packed_f32_scratch_bytes(p.head_dim);
+  if (p.dtype != SAMKV_BF16) return packed_f32_scratch_bytes(p.head_dim);
+  const size_t tc = packed_tc_scratch_bytes(p.head_dim), decode = packed_decode_scratch_bytes(p.head_dim);
+  return tc > decode ? tc : decode;
 }
 
 cudaError_t launch_packed_attn(const samkv_packed_t& p, const Seqs& seqs, const KvSource& kv, const Rows& Q, float scale,
