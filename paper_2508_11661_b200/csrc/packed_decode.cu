@@ -21,7 +21,6 @@ using namespace tc;
 
 constexpr int kRows = 16, kBN = 64, kStages = 4, kRing = 4;
 constexpr int kConsumers = 8, kThreads = (kConsumers + 1) * 32;
-constexpr uint32_t kWaitPolls = 1u << 17, kDrainPolls = 1u << 10;
 
 template <int kD>
 struct Smem {
@@ -60,26 +59,6 @@ struct Params {
   int Hq;
 };
 
-__device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity) {
-  uint32_t done;
-  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-               : "=r"(done) : "r"(bar), "r"(parity) : "memory");
-  return done != 0;
-}
-__device__ __forceinline__ bool wait_bar(uint32_t bar, uint32_t parity, volatile uint32_t* fail) {
-#pragma unroll 1
-  for (uint32_t i = 0; i < kWaitPolls; ++i) {
-    if (try_wait(bar, parity)) return true;
-    if ((i & 63u) == 63u && *fail) return false;
-  }
-  *fail = 1;
-  return false;
-}
-__device__ __forceinline__ void drain_bar(uint32_t bar, uint32_t parity) {
-#pragma unroll 1
-  for (uint32_t i = 0; i < kDrainPolls; ++i)
-    if (try_wait(bar, parity)) return;
-}
 __device__ __forceinline__ void ldsm_x4(uint32_t addr, uint32_t* r) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");

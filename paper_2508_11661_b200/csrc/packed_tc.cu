@@ -47,8 +47,6 @@ constexpr int kGroups = 3;                             // softmax groups, and sc
 constexpr int kThreads = (4 * kGroups + 4) * 32;
 constexpr int kWarpS = 4 * kGroups, kWarpPV = kWarpS + 1, kWarpK = kWarpS + 2, kWarpV = kWarpS + 3;
 constexpr int kRegsSoftmax = 144, kRegsOther = 80;     // 384 x 144 + 128 x 80 = 512 x 128, the launch's registers
-// Waits are within a CTA and last microseconds; a poll that suspends takes about 4 us.
-constexpr uint32_t kWaitPolls = 1u << 17, kDrainPolls = 1u << 10;
 constexpr float kGrow = 16.0f;                         // log2
 constexpr uint32_t kTmemCols = 512, kColO = 384;       // three score buffers of 128 columns, then O
 
@@ -91,29 +89,6 @@ __device__ __forceinline__ float max3_nan(float a, float b, float c) {
   asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
-__device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity) {
-  uint32_t done;
-  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-               : "=r"(done) : "r"(bar), "r"(parity) : "memory");
-  return done != 0;
-}
-// Bounded; gives up as soon as another role has failed.
-__device__ __forceinline__ bool wait_bar(uint32_t bar, uint32_t parity, volatile uint32_t* fail) {
-#pragma unroll 1
-  for (uint32_t i = 0; i < kWaitPolls; ++i) {
-    if (try_wait(bar, parity)) return true;
-    if ((i & 63u) == 63u && *fail) return false;
-  }
-  *fail = 1;
-  return false;
-}
-// For copies in flight at the end: bounded, whatever has failed.
-__device__ __forceinline__ void drain_bar(uint32_t bar, uint32_t parity) {
-#pragma unroll 1
-  for (uint32_t i = 0; i < kDrainPolls; ++i)
-    if (try_wait(bar, parity)) return;
-}
-
 // 16 columns of this thread's lane.
 __device__ __forceinline__ void tmem_ld16(uint32_t taddr, float* v) {
   asm volatile(

@@ -65,6 +65,31 @@ __device__ __forceinline__ void mbar_wait_warp(uint32_t bar, uint32_t parity, vo
 #endif
   __syncwarp();
 }
+// Waits of the packed kernels: every lane polls, waits are within a CTA and last microseconds (a poll that suspends takes
+// about 4 us).
+constexpr uint32_t kWaitPolls = 1u << 17, kDrainPolls = 1u << 10;
+__device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity) {
+  uint32_t done;
+  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+               : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+  return done != 0;
+}
+// Bounded; gives up as soon as another role has failed.
+__device__ __forceinline__ bool wait_bar(uint32_t bar, uint32_t parity, volatile uint32_t* fail) {
+#pragma unroll 1
+  for (uint32_t i = 0; i < kWaitPolls; ++i) {
+    if (try_wait(bar, parity)) return true;
+    if ((i & 63u) == 63u && *fail) return false;
+  }
+  *fail = 1;
+  return false;
+}
+// For copies in flight at the end: bounded, whatever has failed.
+__device__ __forceinline__ void drain_bar(uint32_t bar, uint32_t parity) {
+#pragma unroll 1
+  for (uint32_t i = 0; i < kDrainPolls; ++i)
+    if (try_wait(bar, parity)) return;
+}
 __device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t lbo_bytes, uint32_t sbo_bytes) {
   uint64_t d = 0;
   d |= (uint64_t)((addr >> 4) & 0x3fffu);
