@@ -222,14 +222,15 @@ class Handle:
         self._create(dev, nbytes)
 
     @classmethod
-    def for_packed(cls, packed: "Packed", device: Optional[int] = None) -> "Handle":
-        """A handle whose workspace fits samkv_prefill and samkv_paged_attn with these heads."""
+    def for_packed(cls, packed: "Packed", device: Optional[int] = None, at_least: int = 0) -> "Handle":
+        """A handle whose workspace fits samkv_prefill and samkv_paged_attn with these heads and has `at_least` bytes: the
+        other calls take it too where that is samkv_workspace_bytes of theirs."""
         dev = torch.cuda.current_device() if device is None else device
         nbytes = samkv_packed_workspace_bytes(packed)
         if nbytes == 0:
             raise SamkvError(1, "samkv_packed_workspace_bytes")
         self = cls.__new__(cls)
-        self._create(dev, nbytes)
+        self._create(dev, max(nbytes, at_least))
         return self
 
     def _create(self, dev: int, nbytes: int):
