@@ -547,7 +547,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
             if (lane == 0) mbar_arrive(bar(SEEN));
           }
           auto too_small = [&](float r) { return cand - r > kGrow || (r == -INFINITY && cand > -INFINITY); };
-          const bool far = too_small(ref);
+          const bool far = valid && too_small(ref);      // (rows without a token have no say)
           if (__any_sync(0xffffffffu, far)) {
             // some row needs a larger reference: O has to follow, so everything before this tile is finished first
             wait(TURN + (Tt - 1) % kGroups, (Tt - 1) / kGroups);
@@ -622,10 +622,11 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         if (Tt > 0) wait(TURN + (Tt - 1) % kGroups, (Tt - 1) / kGroups);
         if (!first) {
           const float now = *ref_row;
-          if (__any_sync(0xffffffffu, now != m)) {       // moved by a tile before this one: follow
+          const bool moved = valid && now != m && now == now;
+          if (__any_sync(0xffffffffu, moved)) {          // by a tile before this one: follow
             tmem_wait_st();
-            const float corr = now != m ? fast_exp2(m - now) : 1.0f;
-            tile_r = 0.f;
+            const float corr = moved ? fast_exp2(m - now) : 1.0f;
+            float again = 0.f;
 #pragma unroll 1
             for (int c0 = 0; c0 < kBN; c0 += 32) {
               float q[16];
@@ -637,10 +638,11 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
               tmem_st16(tS + (c0 >> 1), pk);
               if (c0 < width) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) tile_r += bf16_lo(pk[i]) + bf16_hi(pk[i]);
+                for (int i = 0; i < 16; ++i) again += bf16_lo(pk[i]) + bf16_hi(pk[i]);
               }
             }
-            if (now != m) {
+            if (moved) {                                 // (the others keep their sum, added up in its own order)
+              tile_r = again;
               l = l > 0.f ? l * corr : l;
               rl = rl > 0.f ? rl * corr : rl;
               m = now;

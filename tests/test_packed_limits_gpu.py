@@ -275,3 +275,24 @@ def test_fp32_chunks_of_tall_tiles(d, new):
     c = PagedCase(new, [100, 0, 513, 64][:len(new)], 8, 2, d, 32, "f32", seed=253, garbage=float("nan"))
     O, lse = run_paged(c)
     check_paged(c, O, lse)
+
+
+@pytest.mark.parametrize("Hq,Hkv", [(9, 3), (5, 1), (11, 1), (8, 2)])
+def test_rows_do_not_depend_on_what_shares_their_tile(Hq, Hkv):
+    """Rows of a tile that belong to no token hold whatever an earlier call left there.  Moving references (rising keys)
+    between calls that leave other rows behind: bit for bit the same."""
+    new, cached = [251, 130, 511], [1679, 588, 943]
+    c = PagedCase(new, cached, Hq, Hkv, 128, 64, "bf16", seed=222)
+    for s in range(3):
+        for j in range(cached[s] + new[s]):
+            c.Kp[int(c.table_cpu[s, j // 64]), :, j % 64, 0] += 1.6 * j
+    c.Kp *= 4.0
+    c.Q[..., 0] = 1.0
+    O, lse = run_paged(c)
+    other = PagedCase([3000], [0], 8, 2, 128, 64, "bf16", seed=223)          # every row of its tiles is a token
+    Q0 = other.Q.clone()
+    for i in range(40):
+        other.Q = (Q0 * 10.0 ** (i % 5 - 2)).to(torch.bfloat16) if i % 7 else torch.full_like(Q0, float("nan"))
+        run_paged(other)
+        O2, lse2 = run_paged(c)
+        assert torch.equal(O, O2) and torch.equal(lse, lse2), f"call {i}"
