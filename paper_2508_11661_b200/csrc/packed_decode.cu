@@ -6,8 +6,9 @@
 // latency of HBM.  Eight consumer warps: tile T belongs to the four warps of parity T & 1, 16 slots each.  A warp runs
 // its own online softmax over its slots on mma.sync m16n8k16 (16 rows fill one instruction; tcgen05's 128 rows would
 // not), so warps exchange nothing until a piece ends; then the eight (m, l, O) are merged through shared memory.
-// The second product takes the weights rounded to 8 bits.  O is divided by the sum of those, so that the rounding of a
-// weight moves the result only by how far its value is from the others'; lse takes the sum before rounding.
+// The second product takes each weight as the sum of two bf16 values, good to 2^-15: next to the reads of the cache the
+// second set of products costs 1 %, and the result is as good as one from fp32 weights (relative error of 32 x 20480
+// slots 1.66e-3, all of it the output's rounding; 2.24e-3 with weights of 8 bits).
 // 32 requests over 20480 slots, 32/8 heads of 128: 0.403 ms, 6.67 TB/s, the rate of a plain copy (1.03 of the measured
 // one); one request over 102400 slots, 64/8 heads: 76 us, 5.5 TB/s (start-up, the ring's first fill and the merge of 19
 // pieces per KV head are about 12 us of it).  The tensor-memory kernel takes 0.50 ms and 107 us for the same calls.
@@ -30,8 +31,7 @@ struct Smem {
   static constexpr int kQ = kKv + kStages * 2 * kTile;             // [kRing]
   static constexpr int kO = kQ + kRing * kQTile;                   // [kConsumers][kRows][kD] fp32
   static constexpr int kMl = kO + kConsumers * kRows * kD * 4;     // [kConsumers][kRows] float2
-  static constexpr int kL = kMl + kConsumers * kRows * 8;          // [kConsumers][kRows] fp32
-  static constexpr int kPieces = kL + kConsumers * kRows * 4;
+  static constexpr int kPieces = kMl + kConsumers * kRows * 8;
   static constexpr int kBar = kPieces + kRing * 64;
   static constexpr int kMisc = kBar + 192;
   static constexpr int kBytes = kMisc + 64;
@@ -53,8 +53,7 @@ struct Params {
   float scale;
   float* lse;
   float* part_o;               // [slot][kRows][kD]
-  float2* part_ml;             // [slot][kRows] reference, sum of the rounded weights
-  float* part_l;               // [slot][kRows] sum of the weights
+  float2* part_ml;             // [slot][kRows]
   int* d_status;
   int Hq;
 };
@@ -71,6 +70,15 @@ __device__ __forceinline__ void mma_bf16(float* c, const uint32_t* a, uint32_t b
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// A weight's two parts: its bits cut off to bf16, and the rest.  The rest of a weight that is not zero is not zero either
+// (2^-126 at least), so that an infinite value times both parts is that infinity and no NaN.
+__device__ __forceinline__ uint32_t upper_parts(float lo, float hi) {
+  return __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x7632);
+}
+__device__ __forceinline__ float lower_part(float p) {
+  const float rest = fmaxf(p - __uint_as_float(__float_as_uint(p) & 0xffff0000u), 1.17549435e-38f);
+  return p > 0.f ? rest : 0.f;
 }
 }  // namespace pdec
 
@@ -191,7 +199,6 @@ packed_decode_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
     };
     float* sO = reinterpret_cast<float*>(smem_raw + L::kO);
     float2* sMl = reinterpret_cast<float2*>(smem_raw + L::kMl);
-    float* sL = reinterpret_cast<float*>(smem_raw + L::kL);
     while (true) {
       if (!wait(FR_FULL + f % kRing, f / kRing)) break;
       const Piece pc = ring[f % kRing];
@@ -213,7 +220,7 @@ packed_decode_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
       const int last_tok = min((pc.r + 1) * p.cfg.tokens, pc.n) - 1;
       const int vis0 = visible(p.seqs, sq, min(pc.r * p.cfg.tokens + grp / G, last_tok));
       const int vis1 = visible(p.seqs, sq, min(pc.r * p.cfg.tokens + (grp + 8) / G, last_tok));
-      float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f, r0 = 0.f, r1 = 0.f;     // r: of the rounded weights
+      float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
       float o[kD / 8][4];
 #pragma unroll
       for (int i = 0; i < kD / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
@@ -293,8 +300,6 @@ packed_decode_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
           const float c0 = fast_exp2(m0 - mu0), c1 = fast_exp2(m1 - mu1);
           l0 *= c0;
           l1 *= c1;
-          r0 *= c0;
-          r1 *= c1;
 #pragma unroll
           for (int dt = 0; dt < kD / 8; ++dt) {
             o[dt][0] *= c0; o[dt][1] *= c0; o[dt][2] *= c1; o[dt][3] *= c1;
@@ -302,17 +307,17 @@ packed_decode_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
           m0 = mn0;
           m1 = mn1;
         }
-        uint32_t pf[4];
+        uint32_t pf[4], pl[4];                            // upper and lower parts of the weights
 #pragma unroll
         for (int nt = 0; nt < 2; ++nt) {
           const float p0 = fast_exp2(fmaf(s[nt][0], sl2, -mu0)), p1 = fast_exp2(fmaf(s[nt][1], sl2, -mu0));
           const float p2 = fast_exp2(fmaf(s[nt][2], sl2, -mu1)), p3 = fast_exp2(fmaf(s[nt][3], sl2, -mu1));
           l0 += p0 + p1;
           l1 += p2 + p3;
-          pf[nt * 2] = pack_bf16(p0, p1);
-          pf[nt * 2 + 1] = pack_bf16(p2, p3);
-          r0 += bf16_lo(pf[nt * 2]) + bf16_hi(pf[nt * 2]);
-          r1 += bf16_lo(pf[nt * 2 + 1]) + bf16_hi(pf[nt * 2 + 1]);
+          pf[nt * 2] = upper_parts(p0, p1);
+          pf[nt * 2 + 1] = upper_parts(p2, p3);
+          pl[nt * 2] = pack_bf16(lower_part(p0), lower_part(p1));
+          pl[nt * 2 + 1] = pack_bf16(lower_part(p2), lower_part(p3));
         }
         // ---- O += P V ----
 #pragma unroll
@@ -320,6 +325,8 @@ packed_decode_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
           const int r = q16 + (lane & 7) + (mi & 1) * 8, c = dp * 2 + (mi >> 1);
           uint32_t b[4];
           ldsm_x4_t(sV + (c >> 3) * (kBN * 128) + blk_off(r, c & 7), b);
+          mma_bf16(o[dp * 2], pl, b[0], b[1]);
+          mma_bf16(o[dp * 2 + 1], pl, b[2], b[3]);
           mma_bf16(o[dp * 2], pf, b[0], b[1]);
           mma_bf16(o[dp * 2 + 1], pf, b[2], b[3]);
         }
@@ -351,14 +358,10 @@ packed_decode_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
       for (int x = 1; x <= 2; x <<= 1) {
         l0 += __shfl_xor_sync(0xffffffffu, l0, x);
         l1 += __shfl_xor_sync(0xffffffffu, l1, x);
-        r0 += __shfl_xor_sync(0xffffffffu, r0, x);
-        r1 += __shfl_xor_sync(0xffffffffu, r1, x);
       }
       if (qd == 0) {
-        sMl[warp * kRows + grp] = make_float2(m0, r0);
-        sMl[warp * kRows + grp + 8] = make_float2(m1, r1);
-        sL[warp * kRows + grp] = l0;
-        sL[warp * kRows + grp + 8] = l1;
+        sMl[warp * kRows + grp] = make_float2(m0, l0);
+        sMl[warp * kRows + grp + 8] = make_float2(m1, l1);
       }
       float* mine = sO + warp * kRows * kD;
 #pragma unroll
@@ -370,20 +373,20 @@ packed_decode_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
       const bool store = *s_fail == 0;
       const int n_rows = min(p.cfg.tokens, pc.n - pc.r * p.cfg.tokens) * G;
       constexpr int kVecs = kD / 4;
-      auto write_row = [&](int row, int c4, const float* acc, float M, float Rs, float Ls) {
-        const float inv = Rs == 0.f ? 0.f : 1.0f / Rs;
+      auto write_row = [&](int row, int c4, const float* acc, float M, float Ls) {
+        const float inv = Ls == 0.f ? 0.f : 1.0f / Ls;
         const int tok = pc.first + pc.r * p.cfg.tokens + row / G, hq = pc.h * G + row % G;
         uint2 v;
         v.x = pack_bf16(acc[0] * inv, acc[1] * inv);
         v.y = pack_bf16(acc[2] * inv, acc[3] * inv);
-        if (Rs == 0.f) v = make_uint2(0, 0);
+        if (Ls == 0.f) v = make_uint2(0, 0);
         *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.O.data) + (size_t)tok * p.O.ts + (size_t)hq * p.O.hs + c4 * 4) = v;
-        if (c4 == 0 && p.lse != nullptr) p.lse[(size_t)tok * p.Hq + hq] = Rs == 0.f ? -INFINITY : M * kLn2 + logf(Ls);
+        if (c4 == 0 && p.lse != nullptr) p.lse[(size_t)tok * p.Hq + hq] = Ls == 0.f ? -INFINITY : M * kLn2 + logf(Ls);
       };
 #pragma unroll 1
       for (int i = tid; i < n_rows * kVecs; i += kConsumers * 32) {
         const int row = i / kVecs, c4 = i % kVecs;
-        float M = -INFINITY, Rs = 0.f, Ls = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
+        float M = -INFINITY, Ls = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int k = 0; k < kConsumers; ++k) {
           const float2 x = sMl[k * kRows + row];
@@ -395,22 +398,18 @@ packed_decode_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
           if (x.y == 0.f) continue;                       // a warp that saw nothing of this row
           const float w = fast_exp2(x.x - M);
           const float4 v = *reinterpret_cast<const float4*>(sO + (k * kRows + row) * kD + c4 * 4);
-          Rs += x.y * w;
-          Ls += sL[k * kRows + row] * w;
+          Ls += x.y * w;
           acc[0] = fmaf(v.x, w, acc[0]);
           acc[1] = fmaf(v.y, w, acc[1]);
           acc[2] = fmaf(v.z, w, acc[2]);
           acc[3] = fmaf(v.w, w, acc[3]);
         }
         if (pc.slot < 0) {
-          if (store) write_row(row, c4, acc, M, Rs, Ls);
+          if (store) write_row(row, c4, acc, M, Ls);
         } else {
           *reinterpret_cast<float4*>(p.part_o + ((size_t)pc.slot * kRows + row) * kD + c4 * 4) =
               make_float4(acc[0], acc[1], acc[2], acc[3]);
-          if (c4 == 0) {
-            p.part_ml[pc.slot * kRows + row] = make_float2(M, Rs);
-            p.part_l[pc.slot * kRows + row] = Ls;
-          }
+          if (c4 == 0) p.part_ml[pc.slot * kRows + row] = make_float2(M, Ls);
         }
       }
       if (pc.slot >= 0) {
@@ -424,7 +423,7 @@ packed_decode_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
 #pragma unroll 1
           for (int i = tid; i < n_rows * kVecs; i += kConsumers * 32) {
             const int row = i / kVecs, c4 = i % kVecs;
-            float M = -INFINITY, Rs = 0.f, Ls = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
+            float M = -INFINITY, Ls = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
             for (int k = 0; k < pc.n_pieces; ++k) {
               const float2 x = __ldcg(p.part_ml + piece_slot(pc, k) * kRows + row);
@@ -435,17 +434,15 @@ packed_decode_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
               const int slot = piece_slot(pc, k);
               const float2 x = __ldcg(p.part_ml + slot * kRows + row);
               const float4 v = __ldcg(reinterpret_cast<const float4*>(p.part_o + ((size_t)slot * kRows + row) * kD + c4 * 4));
-              const float l = __ldcg(p.part_l + slot * kRows + row);
               if (x.y == 0.f) continue;
               const float w = fast_exp2(x.x - M);
-              Rs += x.y * w;
-              Ls += l * w;
+              Ls += x.y * w;
               acc[0] = fmaf(v.x, w, acc[0]);
               acc[1] = fmaf(v.y, w, acc[1]);
               acc[2] = fmaf(v.z, w, acc[2]);
               acc[3] = fmaf(v.w, w, acc[3]);
             }
-            if (store) write_row(row, c4, acc, M, Rs, Ls);
+            if (store) write_row(row, c4, acc, M, Ls);
           }
         }
       }
@@ -484,7 +481,7 @@ static cudaError_t launch(const Params& p, const KvSource& kv, int ctas, cudaStr
 }
 }  // namespace pdec
 
-size_t packed_decode_scratch_bytes(int d) { return (size_t)2 * kMaxPackedCtas * pdec::kRows * ((size_t)d * 4 + 12); }
+size_t packed_decode_scratch_bytes(int d) { return (size_t)2 * kMaxPackedCtas * pdec::kRows * ((size_t)d * 4 + 8); }
 
 cudaError_t launch_packed_decode(const samkv_packed_t& d, const Seqs& seqs, const KvSource& kv, const Rows& Q, float scale,
                                  const Rows& O, float* lse, const samkv_ctx_impl& h, cudaStream_t stream) {
@@ -506,7 +503,6 @@ cudaError_t launch_packed_decode(const samkv_packed_t& d, const Seqs& seqs, cons
   char* ws = h.workspace + kStatusBytes;
   p.part_o = reinterpret_cast<float*>(ws);
   p.part_ml = reinterpret_cast<float2*>(ws + (size_t)2 * ctas * pdec::kRows * d.head_dim * 4);
-  p.part_l = reinterpret_cast<float*>(p.part_ml + (size_t)2 * ctas * pdec::kRows);
   p.d_status = h.d_status;
   p.Hq = d.n_q_heads;
   return d.head_dim == 128 ? pdec::launch<128>(p, kv, ctas, stream) : pdec::launch<64>(p, kv, ctas, stream);

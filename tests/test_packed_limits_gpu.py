@@ -153,6 +153,23 @@ def test_rounded_probabilities_cancel_over_pages(new, cached, hint, sharp):
         at += n
 
 
+@pytest.mark.parametrize("Hq,Hkv,d", [(8, 2, 128), (6, 2, 64), (16, 1, 128)])
+@pytest.mark.parametrize("sharp", [1.0, 8.0])
+def test_decode_weights_are_good_to_fifteen_bits(Hq, Hkv, d, sharp):
+    """A weight's two bf16 parts are off by 2^-15 of it at most, which moves the result by 2^-15 (A + |O|) <= 2^-14 A; what is
+    left is the scores' and sums' error and the output's own rounding."""
+    new, cached = [1] * 6, [0, 33, 200, 900, 2000, 5001]
+    c = PagedCase(new, cached, Hq, Hkv, d, 64, "bf16", seed=218)
+    c.Kp *= sharp
+    O, lse = run_paged(c, max_seq=1)
+    q, o = f64(c.Q), f64(O)
+    for s, n in enumerate(cached):
+        ref, _, A, Es = attend64(q[s:s + 1], c.slots(c.Kp, s, n + 1), c.slots(c.Vp, s, n + 1), np.array([n + 1]), d ** -0.5)
+        sums = (n + 65) * 2.0 ** -24 + 2.0 ** -21
+        tol = 1.01 * (HALF_STEP["bf16"] * np.abs(ref) + (2.0 ** -14 + 2 * Es[..., None] + 2 * sums) * A)
+        assert (np.abs(o[s:s + 1] - ref) <= tol).all(), f"{n}: {np.max(np.abs(o[s:s + 1] - ref) / tol):.2f} of its bound"
+
+
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("sharp", [1.0, 6.0])
 def test_equal_values_come_out_as_they_are(d, sharp):
@@ -296,3 +313,17 @@ def test_rows_do_not_depend_on_what_shares_their_tile(Hq, Hkv):
         run_paged(other)
         O2, lse2 = run_paged(c)
         assert torch.equal(O, O2) and torch.equal(lse, lse2), f"call {i}"
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("new,cached,hint", [([1, 2, 1], [300, 130, 64], 2), ([40, 9], [300, 20], 0)])
+def test_visible_infinities_of_values_come_out(dtype, new, cached, hint):
+    """Among slots that all rows see, ones that only some see, and the very last; weights that are powers of two among them
+    (equal scores), whose lower bits are zero."""
+    for scale in (0.0, 1e-30):                           # (all scores equal: every weight is 1)
+        c = PagedCase(new, cached, 8, 2, 128, 64, dtype, seed=260, garbage=float("nan"))
+        for s in range(len(new)):
+            for j, e, x in ((5, 3, math.inf), (17, 9, -math.inf), (cached[s], 20, math.inf), (cached[s] + new[s] - 1, 127, -math.inf)):
+                c.Vp[int(c.table_cpu[s, j // 64]), 1, j % 64, e] = x
+        O, lse = run_paged(c, max_seq=hint, scale=scale)
+        check_paged(c, O, lse, scale=scale)
