@@ -218,7 +218,8 @@ samkv_status_t samkv_update(samkv_handle_t h, const samkv_shape_t* shape, void* 
  *   O         [Bt, T_q, Hq, d] = softmax(scale * Q Kc^T + mask) Vc, query head hq reads KV head hq/G
  *   lse       fp32 [Bt, Hq, T_q] optional: log of the softmax denominator
  * bf16 inputs: products on tensor cores with fp32 accumulation, probabilities rounded to bf16
- * before the PV product.  fp32 inputs: fp32 FMA throughout. */
+ * before the PV product; sums of weights times values are formed in fp32 before the division, with weights of up to 2^64,
+ * so that values of V beyond about 2^60 can overflow.  fp32 inputs: fp32 FMA throughout. */
 samkv_status_t samkv_attn(samkv_handle_t h, const samkv_shape_t* shape, int32_t layer, void* Kc, void* Vc,
                           int32_t cache_capacity, int32_t* cache_len, const void* Q, int32_t T_q, const void* Kq,
                           const void* Vq, float scale, void* O, float* lse, void* stream);
@@ -350,7 +351,8 @@ typedef struct {
   int32_t n_q_heads, n_kv_heads, head_dim, dtype;  /* as in samkv_shape_t; n_q_heads / n_kv_heads <= 32 */
   int32_t n_seq;               /* sequences, 1 .. SAMKV_MAX_SEQ */
   int32_t n_tokens;            /* rows of the packed tensors (0: the call does nothing) */
-  int32_t max_seq_tokens;      /* expected longest sequence of the call, 0 = unknown; chooses the kernel, never the result */
+  int32_t max_seq_tokens;      /* expected longest sequence of the call, 0 = unknown; chooses the kernel, so that results
+                                * may differ by rounding, within the same bounds */
   const int32_t* seq_offsets;  /* device [n_seq+1], ascending from >= 0 to <= n_tokens */
 } samkv_packed_t;
 
@@ -397,11 +399,12 @@ size_t samkv_packed_workspace_bytes(const samkv_packed_t* packed);
  *   Q, O   packed with n_q_heads; K, V packed with n_kv_heads.  O must not overlap the inputs.
  *   scale  <= 0 selects 1/sqrt(d)
  *   lse    fp32 [n_tokens, n_q_heads] optional: log of the softmax denominator
+ * lse must not overlap any other tensor of the call.
  * K and V may be the [n_kv_heads, L_tot, d] slabs of one request that samkv_score and samkv_compact read later.
  * Values of K and V behind a row's own position never reach that row, infinities and NaN included.
  * Precision as for samkv_attn: bf16 probabilities are rounded to bf16 before the second product and O is divided by the
- * sum of the rounded ones; lse is taken before that rounding.  Sums of weights times values are formed in fp32 before the
- * division, with weights of up to 2^16.5 in bf16 and 1 in fp32: finite values of V beyond 2^128 / (slots * weight) can come
+ * sum of the rounded ones (decode steps keep 15 bits of them); lse is taken before that rounding.  Sums of weights times values are formed in fp32 before the
+ * division, with weights of up to 2^16.5 (1 in decode steps and in fp32): finite values of V beyond 2^128 / (slots * weight) can come
  * out as infinities.  SAMKV_ERR_WORKSPACE if the handle's workspace is too small. */
 samkv_status_t samkv_prefill(samkv_handle_t h, const samkv_packed_t* packed, const samkv_rows_t* Q,
                              const samkv_rows_t* K, const samkv_rows_t* V, float scale, const samkv_rows_t* O,

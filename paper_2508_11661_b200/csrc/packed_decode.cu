@@ -9,9 +9,9 @@
 // The second product takes each weight as the sum of two bf16 values, good to 2^-15: next to the reads of the cache the
 // second set of products costs 1 %, and the result is as good as one from fp32 weights (relative error of 32 x 20480
 // slots 1.66e-3, all of it the output's rounding; 2.24e-3 with weights of 8 bits).
-// 32 requests over 20480 slots, 32/8 heads of 128: 0.403 ms, 6.67 TB/s, the rate of a plain copy (1.03 of the measured
-// one); one request over 102400 slots, 64/8 heads: 76 us, 5.5 TB/s (start-up, the ring's first fill and the merge of 19
-// pieces per KV head are about 12 us of it).  The tensor-memory kernel takes 0.50 ms and 107 us for the same calls.
+// 32 requests over 20480 slots, 32/8 heads of 128: 0.405 ms, 6.63 TB/s, the rate of a plain copy (1.03 of the measured
+// one); one request over 102400 slots, 64/8 heads: 78 us, 5.4 TB/s (start-up, the ring's first fill and the merge of 19
+// pieces per KV head are about 12 us of it).  The tensor-memory kernel takes 0.42-0.43 ms and 155 us for the same calls.
 // Every wait is bounded; a wait that runs out ends the others and is recorded as a device check.
 #include "packed_plan.cuh"
 #include "tc_common.cuh"

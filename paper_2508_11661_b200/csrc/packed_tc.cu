@@ -21,13 +21,13 @@
 // What bounds it.  A tile costs 1024 cycles on the tensor pipe (16 products of 64 cycles), 1024 on the special-function
 // unit, and 1280 of shared-memory bandwidth (operands 768, TMA writes 512), but the three groups run a tile each through
 // a chain of about 6000 cycles (poll, maximum, exponentials, hand-over, two products, polls), about 2000 per tile: tensor
-// pipe 37-45 % busy.  Measured steps: two groups taking turns 4000 cycles per tile; the loops rolled so that a tile's code
+// pipe 36-45 % busy.  Measured steps: two groups taking turns 4000 cycles per tile; the loops rolled so that a tile's code
 // fits the schedulers' instruction caches (straight-line code ran at 5 cycles an instruction) 2550; three groups 2100.
 // One thread issuing both kinds of products, packed two-wide arithmetic, 64 scores at a time, every fourth exponential as
 // a polynomial, and not loading K and V at all (as an experiment) change nothing or cost up to 15 %.
-// 20 documents of 1536 tokens, 32/8 heads: 0.49 ms (790 TFLOP/s) at 1965 MHz; back to back the board's 1000 W cap settles
-// the clock near 1600 MHz: 0.575 ms (670 TFLOP/s).  128 tokens over 102400 slots, 64/8 heads: 0.51 ms (840 TFLOP/s; 0.62
-// without the layout in waves, which keeps the eight row tiles of a KV head on the same keys at the same time).
+// 20 documents of 1536 tokens, 32/8 heads: 0.52 ms (740 TFLOP/s) with pauses between the calls; back to back the board's
+// 1000 W cap lowers the clock: 0.59 ms (650 TFLOP/s).  128 tokens over 102400 slots, 64/8 heads: 0.53 ms (810 TFLOP/s; a
+// fifth more without the layout in waves, which keeps the eight row tiles of a KV head on the same keys at the same time).
 //
 // Probabilities are rounded to bf16 for the second product.  O is divided by the sum of the rounded ones, so that the
 // rounding of a probability moves the result only by how far its value is from the others' (with the other sum, a row that
