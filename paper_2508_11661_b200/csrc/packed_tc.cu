@@ -15,7 +15,8 @@
 // their probabilities before they hand them over.  A reference moves by whole steps of log2, so that rescaled
 // probabilities are not rounded again.  Which reference a row's tile starts from is fixed (the first tile's, or the one
 // its group ended the tile three before with), and each row decides for itself, so that results repeat bit for bit and
-// depend on no other row.  P(T) overlays the first half of S(T), so tensor memory holds three score buffers and O: 512 columns.
+// depend on no other row.
+// P(T) overlays the first half of S(T), so tensor memory holds three score buffers and O: 512 columns.
 // The group with a piece's last tile writes the result while the others are at the next piece's tiles.
 //
 // What bounds it.  A tile costs 1024 cycles on the tensor pipe (16 products of 64 cycles), 1024 on the special-function
@@ -31,9 +32,10 @@
 //
 // Probabilities are rounded to bf16 for the second product.  O is divided by the sum of the rounded ones, so that the
 // rounding of a probability moves the result only by how far its value is from the others' (with the other sum, a row that
-// one key dominates was off by half a step of bf16 besides the output's own); lse takes the sum before rounding.  Every wait is bounded; a wait that runs out sets a flag that ends all others, the CTA drains its copies and
-// frees its tensor memory, and the failure is recorded as a device check.  TMA reads and writes this GPU's memory only,
-// without multicast.
+// one key dominates was off by half a step of bf16 besides the output's own); lse takes the sum before rounding.
+// Every wait is bounded; a wait that runs out sets a flag that ends all others, the CTA drains its copies and frees its
+// tensor memory, and the failure is recorded as a device check.  TMA reads and writes this GPU's memory only, without
+// multicast.
 #include "packed_plan.cuh"
 #include "tc_common.cuh"
 
