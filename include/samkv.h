@@ -443,6 +443,112 @@ samkv_status_t samkv_paged_attn(samkv_handle_t h, const samkv_packed_t* packed, 
                                 const int32_t* cache_len, const samkv_rows_t* Q, float scale, int32_t causal,
                                 const samkv_rows_t* O, float* lse, void* stream);
 
+/* ---- pages handed out on the GPU ----------------------------------------------------------------------- */
+
+/* The two calls below keep the block table of a paged cache on the device: which pages a request needs follows from its
+ * length, so a step needs no round trip to the host, and a captured step can be replayed while requests grow.
+ *
+ * Free pages lie on a stack: free_pages int32 [n_pages], of which the first *n_free (device) are free.  n_free_out may be
+ * n_free itself; otherwise *n_free stays as it was.  A count outside [0, n_pages] is clamped and recorded as a device check.
+ * Pages are taken from the top and put back on top.  page_size, n_pages, table_width: as in samkv_pages_t. */
+
+/* Gives every sequence the pages that its new tokens need, and lays out the step.
+ *   packed       new tokens per sequence (heads and type are not used, but n_kv_heads bounds the pool's size)
+ *   cache_len    int32 [n_seq] device: slots in the cache before this step; NULL: 0 for every sequence
+ *   block_table  int32 [n_seq, table_width]: the columns ceil(cache_len / page) .. ceil((cache_len + n) / page) - 1 of a
+ *                sequence's row are written, the others stay.  The k-th page that the step needs, counted sequence by
+ *                sequence, column by column, is free_pages[*n_free - 1 - k]
+ *   slots        int32 [n_tokens]: page * page_size + row of every new token, -1 for a token that got no slot and for rows
+ *                that belong to no sequence
+ *   positions    int32 [n_tokens]: cache_len + t, 0 for rows that belong to no sequence
+ *   total_len    int32 [n_seq]: slots after this step, the next step's cache_len
+ *   slots, positions and total_len are optional; each of them NULL: not written.
+ * Without enough pages the first sequences get theirs, -1 goes into the columns that stay without, total_len ends where the
+ * pages end, and a device check is recorded; so it is for slots at or behind table_width * page_size, and for ids on the
+ * stack or in the table that are no pages (their tokens get slot -1).  Offsets that run backwards end the list of sequences
+ * as for samkv_prefill.  Outputs must not overlap one another or the inputs.  With n_tokens == 0 total_len and n_free_out are
+ * still written. */
+samkv_status_t samkv_page_tables(samkv_handle_t h, const samkv_packed_t* packed, const int32_t* cache_len, int32_t page_size,
+                                 int32_t n_pages, int32_t* block_table, int32_t table_width, const int32_t* free_pages,
+                                 const int32_t* n_free, int32_t* n_free_out, int32_t* slots, int32_t* positions,
+                                 int32_t* total_len, void* stream);
+
+/* Puts the pages of finished sequences back: for every s with done[s] != 0 the first ceil(lengths[s] / page_size) entries of
+ * its row go on the stack, the last sequence's last page first (so that handing the same pages out again restores the table).
+ *   lengths  int32 [n_seq] device: slots the sequence holds (clamped to [0, table_width * page_size] with a device check)
+ *   done     uint8 [n_seq] device
+ * Table and lengths are not changed: a row is used again by giving it length 0.  What the stack cannot hold (n_pages
+ * entries) is dropped and recorded as a device check; an entry that is no page is recorded, too, and put on the stack, from
+ * which samkv_page_tables hands it to nobody.  1 <= n_seq <= SAMKV_MAX_SEQ. */
+samkv_status_t samkv_release_pages(samkv_handle_t h, int32_t n_seq, const int32_t* block_table, int32_t table_width,
+                                   int32_t page_size, int32_t n_pages, const int32_t* lengths, const uint8_t* done,
+                                   int32_t* free_pages, const int32_t* n_free, int32_t* n_free_out, void* stream);
+
+/* ---- positions of several axes, append through the slot map ------------------------------------------------ */
+
+#define SAMKV_MAX_AXES 4
+
+/* Rotary encoding by positions of several axes (time, height and width of an image's or video's patches): pair i turns by
+ * positions[pair_axis[i]][t] * base^(-2i/rot_dim), or * inv_freq[i].  Sections of the pairs and axes that take turns are both
+ * such maps. */
+typedef struct {
+  samkv_rope_t rope;
+  int32_t n_axes;              /* 1 .. SAMKV_MAX_AXES */
+  const int32_t* pair_axis;    /* host [rot_dim/2], each in [0, n_axes); read during the call */
+} samkv_rope_axes_t;
+
+/* samkv_append with positions of several axes and with the slot map of samkv_page_tables.
+ *   rope         NULL: no rotation
+ *   positions    int32 device: axis a of token t at positions[a * axis_stride + t]; axis_stride (elements) >= n_tokens, or 0:
+ *                every axis has the same positions (text).  NULL (only without slots): cache_len[s] + t on every axis
+ *   slots        int32 [n_tokens] device: token t goes to slot slots[t] of the pools, counted page * page_size + row; tokens
+ *                with a negative one are left out altogether (nothing of theirs is written anywhere), one at or behind n_pages *
+ *                page_size is left out, too, and recorded as a device check.  The sequences, cache_len and the block table are
+ *                then not looked at.  Two tokens must not share a slot.  NULL: as samkv_append finds them
+ * Everything else as for samkv_append.  slots without pages: SAMKV_ERR_INVALID_ARG. */
+samkv_status_t samkv_append_axes(samkv_handle_t h, const samkv_packed_t* packed, const samkv_rows_t* K,
+                                 const samkv_rows_t* V, const samkv_pages_t* pages, const int32_t* cache_len,
+                                 const int32_t* slots, const samkv_rope_axes_t* rope, const int32_t* positions,
+                                 int64_t axis_stride, const samkv_rows_t* Q, const samkv_rows_t* Q_out,
+                                 const samkv_rows_t* K_out, const samkv_rows_t* V_out, void* stream);
+
+/* ---- attention with modified scores ------------------------------------------------------------------------ */
+
+/* What happens to a score between the product and the softmax, and which slots a token sees.  A token at position p (slot p
+ * of its sequence: cache_len[s] + t, or t in samkv_prefill_scores) and slot j of the same sequence:
+ *   x = scale * <q, k_j>
+ *   x = softcap * tanh(x / softcap)             if softcap > 0
+ *   x = x - slopes[hq] * |p - j|                if slopes are given
+ * and j is seen if j < prefix_len[s] (whatever p is), or if
+ *   j <= p (j < cache_len[s] for samkv_paged_attn_scores without causal),  j >= doc_start[token],  and  p - j < window.
+ * Documents that do not see one another, behind a shared instruction that all see (the prefix) and before a question that
+ * sees all of them (doc_start 0), are one sequence; the initial tokens that a sliding window keeps are a prefix, too.
+ * Slots a token does not see never reach it, infinities and NaN included; a token that sees none gets O = 0, lse = -inf. */
+typedef struct {
+  float softcap;               /* >= 0, finite; 0: scores are not capped.  scale / softcap must be finite */
+  int32_t window;              /* >= 0; 0: no window */
+  const float* slopes;         /* device [n_q_heads], finite, any sign; NULL: none */
+  const int32_t* prefix_len;   /* device [n_seq], any value (a sequence's own slots bound it); NULL: 0 */
+  const int32_t* doc_start;    /* device [n_tokens], any value; NULL: 0 */
+} samkv_scores_t;
+
+/* Bytes of workspace that the two calls below need in their handle, never less than samkv_packed_workspace_bytes, so that
+ * such a handle serves the calls above as well.  It holds the division of the work, which depends on the masks, besides the
+ * partial results.  0 on a bad description. */
+size_t samkv_scores_workspace_bytes(const samkv_packed_t* packed);
+
+/* samkv_prefill with modified scores.  scores == NULL, or a description that modifies nothing: samkv_prefill itself. */
+samkv_status_t samkv_prefill_scores(samkv_handle_t h, const samkv_packed_t* packed, const samkv_rows_t* Q,
+                                    const samkv_rows_t* K, const samkv_rows_t* V, float scale, const samkv_scores_t* scores,
+                                    const samkv_rows_t* O, float* lse, void* stream);
+
+/* samkv_paged_attn with modified scores.  Table entries of pages none of whose slots any token sees are not used (any value),
+ * so that pages a window has passed can be given back.  scores == NULL, or a description that modifies nothing:
+ * samkv_paged_attn itself. */
+samkv_status_t samkv_paged_attn_scores(samkv_handle_t h, const samkv_packed_t* packed, const samkv_pages_t* pages,
+                                       const int32_t* cache_len, const samkv_rows_t* Q, float scale, int32_t causal,
+                                       const samkv_scores_t* scores, const samkv_rows_t* O, float* lse, void* stream);
+
 /* ---- scoring without any allocation ------------------------------------------------------ */
 
 /* (No counterpart in the paper: this entry point exists for deployment reasons only.)

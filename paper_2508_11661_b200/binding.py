@@ -28,7 +28,9 @@ EXPORTS = ["samkv_workspace_bytes", "samkv_create", "samkv_destroy", "samkv_poll
            "samkv_attn", "samkv_score_static", "samkv_topp", "samkv_topp_plan", "samkv_select_cross",
            "samkv_select_cross_scratch_bytes", "samkv_compact_units", "samkv_align", "samkv_compact_protected",
            "samkv_block_means", "samkv_score_blocks", "samkv_attn_kernel_count", "samkv_attn_share_sm", "samkv_attn_layers", "samkv_select_compact",
-           "samkv_sparsify", "samkv_packed_workspace_bytes", "samkv_prefill", "samkv_append", "samkv_paged_attn"]
+           "samkv_sparsify", "samkv_packed_workspace_bytes", "samkv_prefill", "samkv_append", "samkv_paged_attn",
+           "samkv_page_tables", "samkv_release_pages", "samkv_append_axes", "samkv_scores_workspace_bytes",
+           "samkv_prefill_scores", "samkv_paged_attn_scores"]
 
 
 class SamkvError(RuntimeError):
@@ -63,6 +65,15 @@ class samkv_pages_t(ctypes.Structure):
 class samkv_rope_t(ctypes.Structure):
     _fields_ = [("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("base", ctypes.c_double),
                 ("inv_freq", ctypes.POINTER(ctypes.c_double))]
+
+
+class samkv_rope_axes_t(ctypes.Structure):
+    _fields_ = [("rope", samkv_rope_t), ("n_axes", ctypes.c_int32), ("pair_axis", ctypes.POINTER(ctypes.c_int32))]
+
+
+class samkv_scores_t(ctypes.Structure):
+    _fields_ = [("softcap", ctypes.c_float), ("window", ctypes.c_int32), ("slopes", ctypes.c_void_p),
+                ("prefix_len", ctypes.c_void_p), ("doc_start", ctypes.c_void_p)]
 
 
 def lib() -> ctypes.CDLL:
@@ -128,9 +139,18 @@ def load_library(path: str) -> ctypes.CDLL:
     L.samkv_prefill.argtypes = [vp, packed, rows, rows, rows, f32, rows, vp, vp]
     L.samkv_append.argtypes = [vp, packed, rows, rows, pages, vp, ctypes.POINTER(samkv_rope_t), vp, rows, rows, rows, rows, vp]
     L.samkv_paged_attn.argtypes = [vp, packed, pages, vp, rows, f32, i32, rows, vp, vp]
+    L.samkv_page_tables.argtypes = [vp, packed, vp, i32, i32, vp, i32, vp, vp, vp, vp, vp, vp, vp]
+    L.samkv_release_pages.argtypes = [vp, i32, vp, i32, i32, i32, vp, vp, vp, vp, vp, vp]
+    L.samkv_append_axes.argtypes = [vp, packed, rows, rows, pages, vp, vp, ctypes.POINTER(samkv_rope_axes_t), vp, ctypes.c_int64,
+                                    rows, rows, rows, rows, vp]
+    scores = ctypes.POINTER(samkv_scores_t)
+    L.samkv_scores_workspace_bytes.argtypes = [packed]
+    L.samkv_scores_workspace_bytes.restype = sz
+    L.samkv_prefill_scores.argtypes = [vp, packed, rows, rows, rows, f32, scores, rows, vp, vp]
+    L.samkv_paged_attn_scores.argtypes = [vp, packed, pages, vp, rows, f32, i32, scores, rows, vp, vp]
     for name in EXPORTS:
         if name not in ("samkv_status_string", "samkv_workspace_bytes", "samkv_select_cross_scratch_bytes",
-                        "samkv_packed_workspace_bytes"):
+                        "samkv_packed_workspace_bytes", "samkv_scores_workspace_bytes"):
             getattr(L, name).restype = ctypes.c_int
     if hasattr(L, "samkv_debug_score_with_lost_copy"):          # only the debug build exports it
         L.samkv_debug_score_with_lost_copy.argtypes = [vp, shp, vp, vp, i32, vp, i32, i32, vp, ctypes.c_uint32, vp]
@@ -232,6 +252,14 @@ class Handle:
         self = cls.__new__(cls)
         self._create(dev, max(nbytes, at_least))
         return self
+
+    @classmethod
+    def for_scores(cls, packed: "Packed", device: Optional[int] = None, at_least: int = 0) -> "Handle":
+        """A handle for samkv_prefill_scores and samkv_paged_attn_scores with these sizes; it serves all packed calls."""
+        nbytes = samkv_scores_workspace_bytes(packed)
+        if nbytes == 0:
+            raise SamkvError(1, "samkv_scores_workspace_bytes")
+        return cls.for_packed(packed, device, max(nbytes, at_least))
 
     def _create(self, dev: int, nbytes: int):
         self._h = ctypes.c_void_p()
@@ -543,3 +571,137 @@ def samkv_paged_attn(handle: Handle, packed: Packed, pages: Pages, cache_len, Q,
                                     _device_ptr(lse, "lse", torch.float32, packed._lse, dev), _raw_stream(dev))
     if status:
         raise SamkvError(status, "samkv_paged_attn")
+
+
+# ------------------------------------------------------------------ pages handed out on the GPU
+def _table(t: torch.Tensor, n_seq: Optional[int], device: int):
+    """Pointer and width of an int32 block table [n_seq, width]."""
+    if t.dim() != 2 or (n_seq is not None and t.shape[0] != n_seq):
+        raise ValueError(f"block_table: expected {'n_seq' if n_seq is None else n_seq} rows")
+    return _device_ptr(t, "block_table", torch.int32, t.shape, device), t.shape[1]
+
+
+def samkv_page_tables(handle: Handle, packed: Packed, cache_len, page_size: int, block_table, free_pages, n_free, n_free_out,
+                      slots=None, positions=None, total_len=None):
+    """free_pages int32 [n_pages], n_free and n_free_out int32 [1] (n_free_out may be n_free)."""
+    dev, i32 = packed.device(), torch.int32
+    table, width = _table(block_table, packed.n_seq, dev)
+    n_pages = free_pages.shape[0]
+    status = lib().samkv_page_tables(handle._h, packed.c, _device_ptr(cache_len, "cache_len", i32, packed._per_seq, dev), page_size,
+                                     n_pages, table, width, _device_ptr(free_pages, "free_pages", i32, (n_pages,), dev),
+                                     _device_ptr(n_free, "n_free", i32, (1,), dev),
+                                     _device_ptr(n_free_out, "n_free_out", i32, (1,), dev),
+                                     _device_ptr(slots, "slots", i32, packed._per_token, dev),
+                                     _device_ptr(positions, "positions", i32, packed._per_token, dev),
+                                     _device_ptr(total_len, "total_len", i32, packed._per_seq, dev), _raw_stream(dev))
+    if status:
+        raise SamkvError(status, "samkv_page_tables")
+
+
+def samkv_release_pages(handle: Handle, block_table, page_size: int, lengths, done, free_pages, n_free, n_free_out):
+    """done: bool or uint8 [n_seq]; the others as in samkv_page_tables."""
+    dev, i32 = _current_device(), torch.int32
+    table, width = _table(block_table, None, dev)
+    n_seq, n_pages = block_table.shape[0], free_pages.shape[0]
+    if done.dtype not in (torch.bool, torch.uint8):
+        raise ValueError("done: expected bool or uint8")
+    status = lib().samkv_release_pages(handle._h, n_seq, table, width, page_size, n_pages,
+                                       _device_ptr(lengths, "lengths", i32, (n_seq,), dev),
+                                       _device_ptr(done, "done", done.dtype, (n_seq,), dev),
+                                       _device_ptr(free_pages, "free_pages", i32, (n_pages,), dev),
+                                       _device_ptr(n_free, "n_free", i32, (1,), dev),
+                                       _device_ptr(n_free_out, "n_free_out", i32, (1,), dev), _raw_stream(dev))
+    if status:
+        raise SamkvError(status, "samkv_release_pages")
+
+
+# ------------------------------------------------------------------ positions of several axes, append through the slot map
+class RopeAxes:
+    """A samkv_rope_axes_t: pair i turns by the position on axis pair_axis[i]; the rest as in Rope."""
+
+    def __init__(self, rot_dim: int, pair_axis: Sequence[int], base: float = 10000.0, interleaved: bool = False,
+                 inv_freq: Optional[Sequence[float]] = None):
+        if len(pair_axis) != rot_dim // 2:
+            raise ValueError("pair_axis: expected rot_dim / 2 axes")
+        self._rope = Rope(rot_dim, base, interleaved, inv_freq)
+        self.n_axes = max(int(a) for a in pair_axis) + 1
+        self._axis = _i32_array(pair_axis)
+        self.c = samkv_rope_axes_t(self._rope.c, self.n_axes, ctypes.cast(self._axis, ctypes.POINTER(ctypes.c_int32)))
+
+    @classmethod
+    def sections(cls, lengths: Sequence[int], base: float = 10000.0, interleaved: bool = False,
+                 inv_freq: Optional[Sequence[float]] = None) -> "RopeAxes":
+        """The first lengths[0] pairs by the first axis, the next lengths[1] by the second, ..."""
+        axes = [a for a, n in enumerate(lengths) for _ in range(int(n))]
+        return cls(2 * len(axes), axes, base, interleaved, inv_freq)
+
+
+def samkv_append_axes(handle: Handle, packed: Packed, K, V, pages: Optional[Pages] = None, cache_len=None, slots=None,
+                      rope: Optional[RopeAxes] = None, positions=None, Q=None, Q_out=None, K_out=None, V_out=None):
+    """positions: int32 [n_axes, n_tokens], or [n_tokens] for the same ones on every axis; at least as many axes as `rope` has."""
+    dev, q, kv = packed.device(), packed._q, packed._kv
+    stride = 0
+    if positions is not None:
+        if positions.dim() == 2 and rope is not None and positions.shape[0] >= rope.n_axes:
+            stride = packed.n_tokens
+            want = (positions.shape[0], packed.n_tokens)
+        else:
+            want = packed._per_token
+    status = lib().samkv_append_axes(handle._h, packed.c, packed.rows(K, kv, "K", dev), packed.rows(V, kv, "V", dev),
+                                     None if pages is None else pages.checked(packed),
+                                     _device_ptr(cache_len, "cache_len", torch.int32, packed._per_seq, dev),
+                                     _device_ptr(slots, "slots", torch.int32, packed._per_token, dev),
+                                     None if rope is None else rope.c,
+                                     None if positions is None else _device_ptr(positions, "positions", torch.int32, want, dev),
+                                     stride, packed.rows(Q, q, "Q", dev), packed.rows(Q_out, q, "Q_out", dev),
+                                     packed.rows(K_out, kv, "K_out", dev), packed.rows(V_out, kv, "V_out", dev), _raw_stream(dev))
+    if status:
+        raise SamkvError(status, "samkv_append_axes")
+
+
+# ------------------------------------------------------------------ attention with modified scores
+class Scores:
+    """A samkv_scores_t.  slopes fp32 [n_q_heads], prefix_len int32 [n_seq], doc_start int32 [n_tokens]: CUDA tensors, kept
+    alive here; their values may change between calls."""
+
+    def __init__(self, softcap: float = 0.0, window: int = 0, slopes=None, prefix_len=None, doc_start=None):
+        self.slopes, self.prefix_len, self.doc_start = slopes, prefix_len, doc_start
+        for t, what, dtype in ((slopes, "slopes", torch.float32), (prefix_len, "prefix_len", torch.int32),
+                               (doc_start, "doc_start", torch.int32)):
+            if t is not None and (t.dtype is not dtype or t.dim() != 1 or not t.is_contiguous()):
+                raise ValueError(f"{what}: expected a contiguous {dtype} tensor of one dimension")
+        self.c = samkv_scores_t(softcap, window, *(None if t is None else t.data_ptr() for t in (slopes, prefix_len, doc_start)))
+
+    def checked(self, packed: Packed):
+        """The description for a call with these sequences."""
+        dev = packed._device
+        _device_ptr(self.slopes, "slopes", torch.float32, (packed.n_q_heads,), dev)
+        _device_ptr(self.prefix_len, "prefix_len", torch.int32, packed._per_seq, dev)
+        _device_ptr(self.doc_start, "doc_start", torch.int32, packed._per_token, dev)
+        return self.c
+
+
+def samkv_scores_workspace_bytes(packed: Packed) -> int:
+    return int(lib().samkv_scores_workspace_bytes(packed.ref()))
+
+
+def samkv_prefill_scores(handle: Handle, packed: Packed, Q, K, V, scale: float, scores: Optional[Scores], O, lse=None):
+    dev, q, kv = packed.device(), packed._q, packed._kv
+    status = lib().samkv_prefill_scores(handle._h, packed.c, packed.rows(Q, q, "Q", dev), packed.rows(K, kv, "K", dev),
+                                        packed.rows(V, kv, "V", dev), scale, None if scores is None else scores.checked(packed),
+                                        packed.rows(O, q, "O", dev),
+                                        _device_ptr(lse, "lse", torch.float32, packed._lse, dev), _raw_stream(dev))
+    if status:
+        raise SamkvError(status, "samkv_prefill_scores")
+
+
+def samkv_paged_attn_scores(handle: Handle, packed: Packed, pages: Pages, cache_len, Q, scale: float, causal: bool,
+                            scores: Optional[Scores], O, lse=None):
+    dev, q = packed.device(), packed._q
+    status = lib().samkv_paged_attn_scores(handle._h, packed.c, pages.checked(packed),
+                                           _device_ptr(cache_len, "cache_len", torch.int32, packed._per_seq, dev),
+                                           packed.rows(Q, q, "Q", dev), scale, bool(causal),
+                                           None if scores is None else scores.checked(packed), packed.rows(O, q, "O", dev),
+                                           _device_ptr(lse, "lse", torch.float32, packed._lse, dev), _raw_stream(dev))
+    if status:
+        raise SamkvError(status, "samkv_paged_attn_scores")

@@ -102,7 +102,8 @@ AttnPlan plan_attn(const samkv_shape_t& s, int T_q, int capacity, int sm_count, 
 // The 128-row tcgen05 kernel with exactly two KV splits merges them inside a two-CTA cluster: no merge kernel.
 inline bool attn_merges_in_cluster(const AttnPlan& p) { return p.rows_per_cta == 128 && p.n_splits == 2; }
 // Status block of the workspace (256 bytes, zero between calls): int 0 is the device check word, this int counts the
-// finished CTAs of an attention grid that bumps cache_len itself; the others hold the tickets of packed_plan.cuh.
+// finished CTAs of an attention grid that bumps cache_len itself, int 62 those of packed_pages.cu; the others hold the
+// tickets of packed_plan.cuh.
 constexpr int kAttnTicketInt = 32;
 cudaError_t launch_attn(const samkv_shape_t& s, int layer, void* Kc, void* Vc, int capacity, int32_t* cache_len,
                         const void* Q, int T_q, const void* Kq, const void* Vq, float scale, void* O, float* lse,
@@ -135,7 +136,8 @@ enum DeviceCheck : int {
   CHECK_SMEM_ALIGNMENT = 4,  // dynamic shared memory not aligned as the tensor-core tiles need
   CHECK_LIST_CAPACITY = 5,   // an output list is longer than the capacity the caller gave (it was truncated)
   CHECK_SEQ_RANGE = 6,       // a sequence offset or a cache length lies outside its bounds (it was clamped)
-  CHECK_PAGE_RANGE = 7       // a needed block-table entry is not a page
+  CHECK_PAGE_RANGE = 7,      // a needed block-table entry, or a slot of the slot map, is not in the pool
+  CHECK_NO_PAGES = 8         // the stack of free pages ran out
 };
 
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }

@@ -97,6 +97,29 @@ __device__ __forceinline__ float2 split2(f2 v) {
   return r;
 }
 
+// A block table by itself.
+struct PageTable {
+  int32_t* table;              // [n_seq][width]
+  int width, n_pages, shift;   // page size == 1 << shift
+};
+
+// Positions of several axes and the slot map of samkv_append_axes.
+struct AppendAxes {
+  const int32_t* slots;        // [n_tokens], null: from the block table
+  long long axis_stride;       // of the positions
+  int n_axes;
+  unsigned char axis[64];      // of each pair
+};
+
+// What happens to scores between the product and the softmax, and which slots are seen besides Seqs' bounds.
+struct ScoreMods {
+  float softcap;               // 0: none
+  int window;                  // INT_MAX: none
+  const float* slopes;         // [Hq]
+  const int32_t* prefix_len;   // [n_seq]
+  const int32_t* doc_start;    // [n_tokens]
+};
+
 struct RopeTable {
   unsigned long long turn[64]; // fraction of a turn per position, 64-bit fixed point
   int rot_dim, interleaved;    // rot_dim == 0: no rotation
@@ -105,7 +128,17 @@ struct RopeTable {
 // ----- launchers (all enqueue on `stream`) ----------------------------------------------------------------
 cudaError_t launch_append(const samkv_packed_t& p, const Seqs& seqs, const Rows& K, const Rows& V, const Pages* pages,
                           const RopeTable& rope, const int32_t* positions, const Rows* Q, const Rows* Q_out,
-                          const Rows* K_out, const Rows* V_out, int sm_count, int* d_status, cudaStream_t stream);
+                          const Rows* K_out, const Rows* V_out, const AppendAxes* axes, int sm_count, int* d_status,
+                          cudaStream_t stream);
+cudaError_t launch_page_tables(const Seqs& seqs, const PageTable& t, const int32_t* free_pages, const int32_t* n_free,
+                               int32_t* n_free_out, int32_t* slots, int32_t* positions, int32_t* total_len, int sm_count,
+                               int* d_status, cudaStream_t stream);
+cudaError_t launch_release_pages(int n_seq, const PageTable& t, const int32_t* lengths, const uint8_t* done,
+                                 int32_t* free_pages, const int32_t* n_free, int32_t* n_free_out, int sm_count, int* d_status,
+                                 cudaStream_t stream);
+cudaError_t launch_scores_attn(const samkv_packed_t& p, const Seqs& seqs, const KvSource& kv, const Rows& Q, float scale,
+                               const ScoreMods& mods, const Rows& O, float* lse, const samkv_ctx_impl& h, cudaStream_t stream);
+size_t scores_scratch_bytes(const samkv_packed_t& p);
 cudaError_t launch_packed_attn(const samkv_packed_t& p, const Seqs& seqs, const KvSource& kv, const Rows& Q, float scale,
                                const Rows& O, float* lse, const samkv_ctx_impl& h, cudaStream_t stream);
 size_t packed_scratch_bytes(const samkv_packed_t& p);

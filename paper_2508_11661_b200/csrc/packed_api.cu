@@ -121,58 +121,22 @@ bool meets_pools(const samkv_packed_t& p, const Pages& g, const Rows* r, int hea
   return (a < k + pool && k < b) || (a < v + pool && v < b);
 }
 
-samkv_status_t check_workspace(const samkv_ctx_impl* h, const samkv_packed_t& p) {
-  return h->workspace_bytes < kStatusBytes + packed_scratch_bytes(p) ? SAMKV_ERR_WORKSPACE : SAMKV_OK;
+samkv_status_t check_workspace(const samkv_ctx_impl* h, const samkv_packed_t& p, bool modified) {
+  const size_t scratch = modified ? scores_scratch_bytes(p) : packed_scratch_bytes(p);
+  return h->workspace_bytes < kStatusBytes + scratch ? SAMKV_ERR_WORKSPACE : SAMKV_OK;
 }
 
-}  // namespace
-
-extern "C" {
-
-size_t samkv_packed_workspace_bytes(const samkv_packed_t* packed) {
-  // (the offsets need not exist yet when the workspace is sized)
-  if (packed == nullptr) return 0;
-  samkv_packed_t p = *packed;
-  static const int32_t kSomeOffsets = 0;
-  if (p.seq_offsets == nullptr) p.seq_offsets = &kSomeOffsets;
-  if (check_packed(&p) != SAMKV_OK) return 0;
-  return kStatusBytes + packed_scratch_bytes(p);
-}
-
-samkv_status_t samkv_prefill(samkv_handle_t handle, const samkv_packed_t* packed, const samkv_rows_t* Q,
-                             const samkv_rows_t* K, const samkv_rows_t* V, float scale, const samkv_rows_t* O,
-                             float* lse, void* stream) {
-  samkv_ctx_impl* h = reinterpret_cast<samkv_ctx_impl*>(handle);
-  samkv_status_t st = check_packed(packed);
-  if (st != SAMKV_OK || h == nullptr) return SAMKV_OK == st ? SAMKV_ERR_INVALID_ARG : st;
-  if (packed->n_tokens == 0) return check_handle(h);
-  Rows q, o;
-  KvSource kv = {};
-  if ((st = check_rows(*packed, Q, packed->n_q_heads, false, &q)) != SAMKV_OK) return st;
-  if ((st = check_rows(*packed, K, packed->n_kv_heads, false, &kv.K)) != SAMKV_OK) return st;
-  if ((st = check_rows(*packed, V, packed->n_kv_heads, false, &kv.V)) != SAMKV_OK) return st;
-  if ((st = check_rows(*packed, O, packed->n_q_heads, true, &o)) != SAMKV_OK) return st;
-  if (scale != scale || (reinterpret_cast<uintptr_t>(lse) & 3u) != 0) return SAMKV_ERR_INVALID_ARG;
-  const int Hq = packed->n_q_heads, Hkv = packed->n_kv_heads;
-  if (rows_overlap(*packed, o, Hq, q, Hq) || rows_overlap(*packed, o, Hq, kv.K, Hkv) ||
-      rows_overlap(*packed, o, Hq, kv.V, Hkv))
-    return SAMKV_ERR_INVALID_ARG;
-  if ((st = check_handle(h)) != SAMKV_OK) return st;
-  if ((st = check_workspace(h, *packed)) != SAMKV_OK) return st;
-  const Seqs seqs = {packed->seq_offsets, nullptr, packed->n_seq, packed->n_tokens, INT_MAX, 1};
-  return from_cuda(launch_packed_attn(*packed, seqs, kv, q, scale, o, lse, *h, static_cast<cudaStream_t>(stream)));
-}
-
-samkv_status_t samkv_append(samkv_handle_t handle, const samkv_packed_t* packed, const samkv_rows_t* K,
-                            const samkv_rows_t* V, const samkv_pages_t* pages, const int32_t* cache_len,
-                            const samkv_rope_t* rope, const int32_t* positions, const samkv_rows_t* Q,
-                            const samkv_rows_t* Q_out, const samkv_rows_t* K_out, const samkv_rows_t* V_out,
-                            void* stream) {
+// samkv_append, and samkv_append_axes (`axes` given).
+samkv_status_t append(samkv_handle_t handle, const samkv_packed_t* packed, const samkv_rows_t* K,
+                      const samkv_rows_t* V, const samkv_pages_t* pages, const int32_t* cache_len,
+                      const samkv_rope_t* rope, const int32_t* positions, const AppendAxes* axes, const samkv_rows_t* Q,
+                      const samkv_rows_t* Q_out, const samkv_rows_t* K_out, const samkv_rows_t* V_out, void* stream) {
   samkv_ctx_impl* h = reinterpret_cast<samkv_ctx_impl*>(handle);
   samkv_status_t st = check_packed(packed);
   if (st != SAMKV_OK || h == nullptr) return SAMKV_OK == st ? SAMKV_ERR_INVALID_ARG : st;
   if ((Q == nullptr) != (Q_out == nullptr) || (K_out == nullptr) != (V_out == nullptr)) return SAMKV_ERR_INVALID_ARG;
-  if (pages == nullptr && K_out == nullptr) return SAMKV_ERR_INVALID_ARG;       // no destination
+  if (pages == nullptr && (K_out == nullptr || (axes != nullptr && axes->slots != nullptr)))
+    return SAMKV_ERR_INVALID_ARG;                                  // no destination
   if (((reinterpret_cast<uintptr_t>(cache_len) | reinterpret_cast<uintptr_t>(positions)) & 3u) != 0)
     return SAMKV_ERR_INVALID_ARG;
   RopeTable table;
@@ -220,13 +184,89 @@ samkv_status_t samkv_append(samkv_handle_t handle, const samkv_packed_t* packed,
   const Seqs seqs = {packed->seq_offsets, cache_len, packed->n_seq, packed->n_tokens, INT_MAX, 0};
   return from_cuda(launch_append(*packed, seqs, k, v, pages != nullptr ? &pg : nullptr, table, positions,
                                  Q != nullptr ? &q : nullptr, Q != nullptr ? &qo : nullptr,
-                                 K_out != nullptr ? &ko : nullptr, K_out != nullptr ? &vo : nullptr, h->sm_count,
+                                 K_out != nullptr ? &ko : nullptr, K_out != nullptr ? &vo : nullptr, axes, h->sm_count,
                                  h->d_status, static_cast<cudaStream_t>(stream)));
 }
 
-samkv_status_t samkv_paged_attn(samkv_handle_t handle, const samkv_packed_t* packed, const samkv_pages_t* pages,
-                                const int32_t* cache_len, const samkv_rows_t* Q, float scale, int32_t causal,
-                                const samkv_rows_t* O, float* lse, void* stream) {
+samkv_status_t check_page_table(const int32_t* table, int width, int page_size, int n_pages, int n_kv_heads, PageTable* out) {
+  if (table == nullptr || (reinterpret_cast<uintptr_t>(table) & 3u) != 0) return SAMKV_ERR_INVALID_ARG;
+  if (n_pages < 1 || width < 1) return SAMKV_ERR_INVALID_ARG;
+  int shift = 4;
+  while (shift <= 8 && (1 << shift) != page_size) ++shift;
+  if (shift > 8) return SAMKV_ERR_UNSUPPORTED;
+  if ((long long)width * page_size > (1LL << 30)) return SAMKV_ERR_UNSUPPORTED;
+  if ((long long)n_pages * n_kv_heads * page_size > INT_MAX) return SAMKV_ERR_UNSUPPORTED;
+  *out = {const_cast<int32_t*>(table), width, n_pages, shift};
+  return SAMKV_OK;
+}
+
+// Memory of an argument that is an array of 32-bit (done: 8-bit) values.
+struct Array {
+  const void* data;
+  long long bytes;
+  bool output;
+};
+// Null where none is allowed, misaligned, or an output on another array's memory (n_free_out on n_free itself is allowed).
+samkv_status_t check_arrays(const Array* arrays, int n) {
+  for (int i = 0; i < n; ++i)
+    for (int j = 0; j < n; ++j) {
+      if (i == j || !arrays[i].output || arrays[i].data == nullptr || arrays[j].data == nullptr) continue;
+      const char *a = (const char*)arrays[i].data, *b = (const char*)arrays[j].data;
+      if (a < b + arrays[j].bytes && b < a + arrays[i].bytes) return SAMKV_ERR_INVALID_ARG;
+    }
+  return SAMKV_OK;
+}
+bool misaligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) != 0; }
+
+// The modifications of a call; *any: there are some.
+samkv_status_t check_scores(const samkv_scores_t* s, const samkv_packed_t& p, float scale, ScoreMods* out, bool* any) {
+  *any = false;
+  if (s == nullptr) return SAMKV_OK;
+  if (!(s->softcap >= 0.f) || !isfinite(s->softcap) || s->window < 0) return SAMKV_ERR_INVALID_ARG;
+  if (misaligned4(s->slopes) || misaligned4(s->prefix_len) || misaligned4(s->doc_start)) return SAMKV_ERR_INVALID_ARG;
+  if (s->softcap > 0.f) {
+    const float sc = scale > 0.f ? scale : 1.0f / sqrtf((float)p.head_dim);
+    if (!isfinite(sc / s->softcap) || s->softcap > 1e30f) return SAMKV_ERR_INVALID_ARG;
+  }
+  *out = {s->softcap, s->window > 0 ? s->window : INT_MAX, s->slopes, s->prefix_len, s->doc_start};
+  *any = s->softcap > 0.f || s->window > 0 || s->slopes != nullptr || s->prefix_len != nullptr || s->doc_start != nullptr;
+  return SAMKV_OK;
+}
+
+// samkv_prefill, and samkv_prefill_scores.
+samkv_status_t prefill(samkv_handle_t handle, const samkv_packed_t* packed, const samkv_rows_t* Q, const samkv_rows_t* K,
+                       const samkv_rows_t* V, float scale, const samkv_scores_t* scores, const samkv_rows_t* O, float* lse,
+                       void* stream) {
+  samkv_ctx_impl* h = reinterpret_cast<samkv_ctx_impl*>(handle);
+  samkv_status_t st = check_packed(packed);
+  if (st != SAMKV_OK || h == nullptr) return SAMKV_OK == st ? SAMKV_ERR_INVALID_ARG : st;
+  if (packed->n_tokens == 0) return check_handle(h);
+  Rows q, o;
+  KvSource kv = {};
+  if ((st = check_rows(*packed, Q, packed->n_q_heads, false, &q)) != SAMKV_OK) return st;
+  if ((st = check_rows(*packed, K, packed->n_kv_heads, false, &kv.K)) != SAMKV_OK) return st;
+  if ((st = check_rows(*packed, V, packed->n_kv_heads, false, &kv.V)) != SAMKV_OK) return st;
+  if ((st = check_rows(*packed, O, packed->n_q_heads, true, &o)) != SAMKV_OK) return st;
+  if (scale != scale || (reinterpret_cast<uintptr_t>(lse) & 3u) != 0) return SAMKV_ERR_INVALID_ARG;
+  const int Hq = packed->n_q_heads, Hkv = packed->n_kv_heads;
+  if (rows_overlap(*packed, o, Hq, q, Hq) || rows_overlap(*packed, o, Hq, kv.K, Hkv) ||
+      rows_overlap(*packed, o, Hq, kv.V, Hkv))
+    return SAMKV_ERR_INVALID_ARG;
+  ScoreMods mods;
+  bool modified;
+  if ((st = check_scores(scores, *packed, scale, &mods, &modified)) != SAMKV_OK) return st;
+  if ((st = check_handle(h)) != SAMKV_OK) return st;
+  if ((st = check_workspace(h, *packed, modified)) != SAMKV_OK) return st;
+  const Seqs seqs = {packed->seq_offsets, nullptr, packed->n_seq, packed->n_tokens, INT_MAX, 1};
+  if (modified)
+    return from_cuda(launch_scores_attn(*packed, seqs, kv, q, scale, mods, o, lse, *h, static_cast<cudaStream_t>(stream)));
+  return from_cuda(launch_packed_attn(*packed, seqs, kv, q, scale, o, lse, *h, static_cast<cudaStream_t>(stream)));
+}
+
+// samkv_paged_attn, and samkv_paged_attn_scores.
+samkv_status_t paged_attn(samkv_handle_t handle, const samkv_packed_t* packed, const samkv_pages_t* pages,
+                          const int32_t* cache_len, const samkv_rows_t* Q, float scale, int32_t causal,
+                          const samkv_scores_t* scores, const samkv_rows_t* O, float* lse, void* stream) {
   samkv_ctx_impl* h = reinterpret_cast<samkv_ctx_impl*>(handle);
   samkv_status_t st = check_packed(packed);
   if (st != SAMKV_OK || h == nullptr) return SAMKV_OK == st ? SAMKV_ERR_INVALID_ARG : st;
@@ -242,11 +282,145 @@ samkv_status_t samkv_paged_attn(samkv_handle_t handle, const samkv_packed_t* pac
   if ((st = check_pages(*packed, pages, &kv.pages)) != SAMKV_OK) return st;
   if (rows_overlap(*packed, o, packed->n_q_heads, q, packed->n_q_heads)) return SAMKV_ERR_INVALID_ARG;
   if (meets_pools(*packed, kv.pages, &o, packed->n_q_heads)) return SAMKV_ERR_INVALID_ARG;
+  ScoreMods mods;
+  bool modified;
+  if ((st = check_scores(scores, *packed, scale, &mods, &modified)) != SAMKV_OK) return st;
   if ((st = check_handle(h)) != SAMKV_OK) return st;
-  if ((st = check_workspace(h, *packed)) != SAMKV_OK) return st;
+  if ((st = check_workspace(h, *packed, modified)) != SAMKV_OK) return st;
   const Seqs seqs = {packed->seq_offsets, cache_len, packed->n_seq, packed->n_tokens,
                      pages->table_width * pages->page_size, causal != 0};
+  if (modified)
+    return from_cuda(launch_scores_attn(*packed, seqs, kv, q, scale, mods, o, lse, *h, static_cast<cudaStream_t>(stream)));
   return from_cuda(launch_packed_attn(*packed, seqs, kv, q, scale, o, lse, *h, static_cast<cudaStream_t>(stream)));
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t samkv_packed_workspace_bytes(const samkv_packed_t* packed) {
+  // (the offsets need not exist yet when the workspace is sized)
+  if (packed == nullptr) return 0;
+  samkv_packed_t p = *packed;
+  static const int32_t kSomeOffsets = 0;
+  if (p.seq_offsets == nullptr) p.seq_offsets = &kSomeOffsets;
+  if (check_packed(&p) != SAMKV_OK) return 0;
+  return kStatusBytes + packed_scratch_bytes(p);
+}
+
+size_t samkv_scores_workspace_bytes(const samkv_packed_t* packed) {
+  const size_t plain = samkv_packed_workspace_bytes(packed);
+  if (plain == 0) return 0;
+  const size_t mine = kStatusBytes + scores_scratch_bytes(*packed);
+  return mine > plain ? mine : plain;
+}
+
+samkv_status_t samkv_prefill(samkv_handle_t handle, const samkv_packed_t* packed, const samkv_rows_t* Q,
+                             const samkv_rows_t* K, const samkv_rows_t* V, float scale, const samkv_rows_t* O,
+                             float* lse, void* stream) {
+  return prefill(handle, packed, Q, K, V, scale, nullptr, O, lse, stream);
+}
+
+samkv_status_t samkv_prefill_scores(samkv_handle_t handle, const samkv_packed_t* packed, const samkv_rows_t* Q,
+                                    const samkv_rows_t* K, const samkv_rows_t* V, float scale, const samkv_scores_t* scores,
+                                    const samkv_rows_t* O, float* lse, void* stream) {
+  return prefill(handle, packed, Q, K, V, scale, scores, O, lse, stream);
+}
+
+samkv_status_t samkv_append(samkv_handle_t handle, const samkv_packed_t* packed, const samkv_rows_t* K,
+                            const samkv_rows_t* V, const samkv_pages_t* pages, const int32_t* cache_len,
+                            const samkv_rope_t* rope, const int32_t* positions, const samkv_rows_t* Q,
+                            const samkv_rows_t* Q_out, const samkv_rows_t* K_out, const samkv_rows_t* V_out,
+                            void* stream) {
+  return append(handle, packed, K, V, pages, cache_len, rope, positions, nullptr, Q, Q_out, K_out, V_out, stream);
+}
+
+samkv_status_t samkv_append_axes(samkv_handle_t handle, const samkv_packed_t* packed, const samkv_rows_t* K,
+                                 const samkv_rows_t* V, const samkv_pages_t* pages, const int32_t* cache_len,
+                                 const int32_t* slots, const samkv_rope_axes_t* rope, const int32_t* positions,
+                                 int64_t axis_stride, const samkv_rows_t* Q, const samkv_rows_t* Q_out,
+                                 const samkv_rows_t* K_out, const samkv_rows_t* V_out, void* stream) {
+  const samkv_status_t st = check_packed(packed);
+  if (st != SAMKV_OK) return st;
+  AppendAxes axes = {};
+  axes.slots = slots;
+  axes.n_axes = 1;
+  if ((reinterpret_cast<uintptr_t>(slots) & 3u) != 0) return SAMKV_ERR_INVALID_ARG;
+  if (rope != nullptr) {
+    if (rope->n_axes < 1 || rope->n_axes > SAMKV_MAX_AXES || rope->pair_axis == nullptr) return SAMKV_ERR_INVALID_ARG;
+    if (rope->rope.rot_dim < 16 || rope->rope.rot_dim > packed->head_dim) return SAMKV_ERR_INVALID_ARG;
+    for (int i = 0; i < rope->rope.rot_dim / 2; ++i) {
+      if (rope->pair_axis[i] < 0 || rope->pair_axis[i] >= rope->n_axes) return SAMKV_ERR_INVALID_ARG;
+      axes.axis[i] = (unsigned char)rope->pair_axis[i];
+    }
+    axes.n_axes = rope->n_axes;
+    axes.axis_stride = axis_stride;
+    if (positions != nullptr && axis_stride != 0 && axis_stride < packed->n_tokens) return SAMKV_ERR_INVALID_ARG;
+    if (axis_stride > (1LL << 40)) return SAMKV_ERR_UNSUPPORTED;
+    if (positions == nullptr && slots != nullptr) return SAMKV_ERR_INVALID_ARG;
+  } else {
+    positions = nullptr;
+  }
+  return append(handle, packed, K, V, pages, cache_len, rope != nullptr ? &rope->rope : nullptr, positions, &axes, Q, Q_out,
+                K_out, V_out, stream);
+}
+
+samkv_status_t samkv_paged_attn(samkv_handle_t handle, const samkv_packed_t* packed, const samkv_pages_t* pages,
+                                const int32_t* cache_len, const samkv_rows_t* Q, float scale, int32_t causal,
+                                const samkv_rows_t* O, float* lse, void* stream) {
+  return paged_attn(handle, packed, pages, cache_len, Q, scale, causal, nullptr, O, lse, stream);
+}
+
+samkv_status_t samkv_paged_attn_scores(samkv_handle_t handle, const samkv_packed_t* packed, const samkv_pages_t* pages,
+                                       const int32_t* cache_len, const samkv_rows_t* Q, float scale, int32_t causal,
+                                       const samkv_scores_t* scores, const samkv_rows_t* O, float* lse, void* stream) {
+  return paged_attn(handle, packed, pages, cache_len, Q, scale, causal, scores, O, lse, stream);
+}
+
+samkv_status_t samkv_page_tables(samkv_handle_t handle, const samkv_packed_t* packed, const int32_t* cache_len,
+                                 int32_t page_size, int32_t n_pages, int32_t* block_table, int32_t table_width,
+                                 const int32_t* free_pages, const int32_t* n_free, int32_t* n_free_out, int32_t* slots,
+                                 int32_t* positions, int32_t* total_len, void* stream) {
+  samkv_ctx_impl* h = reinterpret_cast<samkv_ctx_impl*>(handle);
+  samkv_status_t st = check_packed(packed);
+  if (st != SAMKV_OK || h == nullptr) return SAMKV_OK == st ? SAMKV_ERR_INVALID_ARG : st;
+  PageTable t;
+  if ((st = check_page_table(block_table, table_width, page_size, n_pages, packed->n_kv_heads, &t)) != SAMKV_OK) return st;
+  if (free_pages == nullptr || n_free == nullptr || n_free_out == nullptr) return SAMKV_ERR_INVALID_ARG;
+  const void* all[] = {cache_len, free_pages, n_free, n_free_out, slots, positions, total_len};
+  for (const void* p : all)
+    if (misaligned4(p)) return SAMKV_ERR_INVALID_ARG;
+  const long long seqs4 = 4LL * packed->n_seq, tokens4 = 4LL * packed->n_tokens;
+  const Array arrays[] = {{packed->seq_offsets, seqs4 + 4, false}, {cache_len, seqs4, false}, {free_pages, 4LL * n_pages, false},
+                          {n_free == n_free_out ? nullptr : n_free, 4, false}, {block_table, seqs4 * table_width, true},
+                          {n_free_out, 4, true}, {slots, tokens4, true}, {positions, tokens4, true}, {total_len, seqs4, true}};
+  if ((st = check_arrays(arrays, sizeof(arrays) / sizeof(arrays[0]))) != SAMKV_OK) return st;
+  if ((st = check_handle(h)) != SAMKV_OK) return st;
+  const Seqs seqs = {packed->seq_offsets, cache_len, packed->n_seq, packed->n_tokens, table_width * page_size, 0};
+  return from_cuda(launch_page_tables(seqs, t, free_pages, n_free, n_free_out, slots, positions, total_len, h->sm_count,
+                                      h->d_status, static_cast<cudaStream_t>(stream)));
+}
+
+samkv_status_t samkv_release_pages(samkv_handle_t handle, int32_t n_seq, const int32_t* block_table, int32_t table_width,
+                                   int32_t page_size, int32_t n_pages, const int32_t* lengths, const uint8_t* done,
+                                   int32_t* free_pages, const int32_t* n_free, int32_t* n_free_out, void* stream) {
+  samkv_ctx_impl* h = reinterpret_cast<samkv_ctx_impl*>(handle);
+  if (h == nullptr || n_seq < 1) return SAMKV_ERR_INVALID_ARG;
+  if (n_seq > SAMKV_MAX_SEQ) return SAMKV_ERR_UNSUPPORTED;
+  PageTable t;
+  samkv_status_t st = check_page_table(block_table, table_width, page_size, n_pages, 1, &t);
+  if (st != SAMKV_OK) return st;
+  const void* all[] = {lengths, free_pages, n_free, n_free_out};
+  for (const void* p : all)
+    if (p == nullptr || misaligned4(p)) return SAMKV_ERR_INVALID_ARG;
+  if (done == nullptr) return SAMKV_ERR_INVALID_ARG;
+  const Array arrays[] = {{block_table, 4LL * n_seq * table_width, false}, {lengths, 4LL * n_seq, false}, {done, n_seq, false},
+                          {n_free == n_free_out ? nullptr : n_free, 4, false}, {free_pages, 4LL * n_pages, true},
+                          {n_free_out, 4, true}};
+  if ((st = check_arrays(arrays, sizeof(arrays) / sizeof(arrays[0]))) != SAMKV_OK) return st;
+  if ((st = check_handle(h)) != SAMKV_OK) return st;
+  return from_cuda(launch_release_pages(n_seq, t, lengths, done, free_pages, n_free, n_free_out, h->sm_count, h->d_status,
+                                        static_cast<cudaStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -34,22 +34,32 @@ __device__ __forceinline__ float2 turn_sincos(unsigned long long phase) {
   return r;
 }
 
-template <typename T, int kD>
+// kAxes: positions of several axes, and rows found by a slot map where one is given.
+template <typename T, int kD, bool kAxes>
 __global__ void __launch_bounds__(kAppendThreads)
-append_rope_kernel(const __grid_constant__ AppendArgs a, const __grid_constant__ RopeTable rope, int tokens_per_cta,
-                   int* __restrict__ d_status) {
+append_rope_kernel(const __grid_constant__ AppendArgs a, const __grid_constant__ RopeTable rope,
+                   const __grid_constant__ AppendAxes axes, int tokens_per_cta, int* __restrict__ d_status) {
   constexpr int kVec = 16 / (int)sizeof(T);      // elements per 16 bytes
   constexpr int kItems = kD / (2 * kVec);        // an item is two 16-byte pieces of a row
   __shared__ float2 cs[kMaxAppendTokens][kD / 2];
   __shared__ long long page_row[kMaxAppendTokens];   // row of (page, head 0) in the pools, -1: do not write
   __shared__ int live[kMaxAppendTokens];             // the token belongs to a sequence
-  __shared__ long long pos[kMaxAppendTokens];        // (cache_len + t passes 32 bits)
+  __shared__ long long pos[kMaxAppendTokens * (kAxes ? SAMKV_MAX_AXES : 1)];   // (cache_len + t passes 32 bits)
   const int tid = threadIdx.x;
   const int tok0 = blockIdx.x * tokens_per_cta;
   const int n_tok = min(tokens_per_cta, a.seqs.n_tokens - tok0);
   pdl_launch_dependents();
   pdl_wait();
-  if (tid < n_tok) {
+  const bool mapped = kAxes && axes.slots != nullptr;
+  if (mapped && tid < n_tok) {
+    const int slot = axes.slots[tok0 + tid];
+    const bool in_pool = slot < a.pages.n_pages << a.pages.shift;
+    if (!in_pool) atomicMax(d_status, (int)CHECK_PAGE_RANGE);
+    const int page = slot >> a.pages.shift;
+    live[tid] = slot >= 0 && in_pool;
+    page_row[tid] = (((long long)page * a.Hkv) << a.pages.shift) + (slot & ((1 << a.pages.shift) - 1));
+  }
+  if (!mapped && tid < n_tok) {
     const int tok = tok0 + tid;
     // last sequence whose first row is <= tok; with empty sequences in between that is the one that owns the row
     int lo = 0, hi = a.seqs.n_seq;
@@ -65,7 +75,7 @@ append_rope_kernel(const __grid_constant__ AppendArgs a, const __grid_constant__
         mine = 1;
         const long long slot = (long long)sq.base + (tok - sq.first);
         if (sq.clamped) atomicMax(d_status, (int)CHECK_SEQ_RANGE);
-        p = a.positions != nullptr ? a.positions[tok] : slot;
+        p = !kAxes && a.positions != nullptr ? a.positions[tok] : slot;
         if (a.has_pages) {
           const long long col = slot >> a.pages.shift;
           if (col >= a.pages.width) {
@@ -81,14 +91,29 @@ append_rope_kernel(const __grid_constant__ AppendArgs a, const __grid_constant__
       }
     }
     live[tid] = mine;
-    pos[tid] = p;
     page_row[tid] = row;
+    if constexpr (kAxes) {
+#pragma unroll
+      for (int i = 0; i < SAMKV_MAX_AXES; ++i) pos[tid * SAMKV_MAX_AXES + i] = p;
+    } else {
+      pos[tid] = p;
+    }
+  }
+  if constexpr (kAxes) {
+    if (a.positions != nullptr) {
+      __syncthreads();
+      if (tid < n_tok * axes.n_axes) {
+        const int t = tid / axes.n_axes, i = tid - t * axes.n_axes;
+        pos[t * SAMKV_MAX_AXES + i] = a.positions[i * axes.axis_stride + tok0 + t];
+      }
+    }
   }
   __syncthreads();
   const int half = rope.rot_dim >> 1;
   for (int i = tid; i < n_tok * half; i += kAppendThreads) {
     const int t = i / half, e = i - t * half;
-    cs[t][e] = turn_sincos((unsigned long long)pos[t] * rope.turn[e]);
+    const long long at = kAxes ? pos[t * SAMKV_MAX_AXES + axes.axis[e]] : pos[t];
+    cs[t][e] = turn_sincos((unsigned long long)at * rope.turn[e]);
   }
   __syncthreads();
 
@@ -162,7 +187,8 @@ append_rope_kernel(const __grid_constant__ AppendArgs a, const __grid_constant__
 
 cudaError_t launch_append(const samkv_packed_t& p, const Seqs& seqs, const Rows& K, const Rows& V, const Pages* pages,
                           const RopeTable& rope, const int32_t* positions, const Rows* Q, const Rows* Q_out,
-                          const Rows* K_out, const Rows* V_out, int sm_count, int* d_status, cudaStream_t stream) {
+                          const Rows* K_out, const Rows* V_out, const AppendAxes* axes, int sm_count, int* d_status,
+                          cudaStream_t stream) {
   AppendArgs a = {};
   a.seqs = seqs;
   a.K = K;
@@ -185,12 +211,13 @@ cudaError_t launch_append(const samkv_packed_t& p, const Seqs& seqs, const Rows&
   attr.val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
-  if (p.dtype == SAMKV_BF16)
-    return p.head_dim == 128
-               ? cudaLaunchKernelEx(&cfg, append_rope_kernel<__nv_bfloat16, 128>, a, rope, per_cta, d_status)
-               : cudaLaunchKernelEx(&cfg, append_rope_kernel<__nv_bfloat16, 64>, a, rope, per_cta, d_status);
-  return p.head_dim == 128 ? cudaLaunchKernelEx(&cfg, append_rope_kernel<float, 128>, a, rope, per_cta, d_status)
-                           : cudaLaunchKernelEx(&cfg, append_rope_kernel<float, 64>, a, rope, per_cta, d_status);
+  const AppendAxes none = {};
+#define SAMKV_APPEND(T, D) \
+  (axes != nullptr ? cudaLaunchKernelEx(&cfg, append_rope_kernel<T, D, true>, a, rope, *axes, per_cta, d_status) \
+                   : cudaLaunchKernelEx(&cfg, append_rope_kernel<T, D, false>, a, rope, none, per_cta, d_status))
+  if (p.dtype == SAMKV_BF16) return p.head_dim == 128 ? SAMKV_APPEND(__nv_bfloat16, 128) : SAMKV_APPEND(__nv_bfloat16, 64);
+  return p.head_dim == 128 ? SAMKV_APPEND(float, 128) : SAMKV_APPEND(float, 64);
+#undef SAMKV_APPEND
 }
 
 }  // namespace samkv
