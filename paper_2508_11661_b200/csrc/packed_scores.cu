@@ -132,14 +132,16 @@ static cudaError_t launch(const Params& p, cudaStream_t stream) {
 }
 }  // namespace pscore
 
-size_t scores_scratch_bytes(const samkv_packed_t& p) { return packed_scratch_bytes(p); }
+cudaError_t launch_packed_tc_scores(const samkv_packed_t& d, const Seqs& seqs, const KvSource& kv, const Rows& Q, float scale,
+                                    const ScoreMods& mods, const Rows& O, float* lse, const samkv_ctx_impl& h,
+                                    cudaStream_t stream);
 
 cudaError_t launch_scores_attn(const samkv_packed_t& d, const Seqs& seqs, const KvSource& kv, const Rows& Q, float scale,
                                const ScoreMods& mods, const Rows& O, float* lse, const samkv_ctx_impl& h, cudaStream_t stream) {
   if (scale <= 0.f) scale = 1.0f / sqrtf((float)d.head_dim);
+  if (d.dtype == SAMKV_BF16) return launch_packed_tc_scores(d, seqs, kv, Q, scale, mods, O, lse, h, stream);
   const pscore::Params p = {seqs, mods, kv, Q, O, scale, lse, h.d_status, d.n_q_heads, d.n_kv_heads};
-  if (d.dtype == SAMKV_F32) return d.head_dim == 128 ? pscore::launch<float, 128>(p, stream) : pscore::launch<float, 64>(p, stream);
-  return d.head_dim == 128 ? pscore::launch<__nv_bfloat16, 128>(p, stream) : pscore::launch<__nv_bfloat16, 64>(p, stream);
+  return d.head_dim == 128 ? pscore::launch<float, 128>(p, stream) : pscore::launch<float, 64>(p, stream);
 }
 
 }  // namespace samkv
