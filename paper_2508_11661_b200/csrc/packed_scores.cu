@@ -132,14 +132,20 @@ static cudaError_t launch(const Params& p, cudaStream_t stream) {
 }
 }  // namespace pscore
 
-cudaError_t launch_packed_tc_scores(const samkv_packed_t& d, const Seqs& seqs, const KvSource& kv, const Rows& Q, float scale,
-                                    const ScoreMods& mods, const Rows& O, float* lse, const samkv_ctx_impl& h,
-                                    cudaStream_t stream);
+cudaError_t launch_packed_tc_mask(const samkv_packed_t& d, const Seqs& seqs, const KvSource& kv, const Rows& Q, float scale,
+                               const ScoreMods& mods, const Rows& O, float* lse, const samkv_ctx_impl& h, cudaStream_t stream);
+cudaError_t launch_packed_tc_cap(const samkv_packed_t& d, const Seqs& seqs, const KvSource& kv, const Rows& Q, float scale,
+                               const ScoreMods& mods, const Rows& O, float* lse, const samkv_ctx_impl& h, cudaStream_t stream);
+cudaError_t launch_packed_tc_bias(const samkv_packed_t& d, const Seqs& seqs, const KvSource& kv, const Rows& Q, float scale,
+                               const ScoreMods& mods, const Rows& O, float* lse, const samkv_ctx_impl& h, cudaStream_t stream);
 
 cudaError_t launch_scores_attn(const samkv_packed_t& d, const Seqs& seqs, const KvSource& kv, const Rows& Q, float scale,
                                const ScoreMods& mods, const Rows& O, float* lse, const samkv_ctx_impl& h, cudaStream_t stream) {
   if (scale <= 0.f) scale = 1.0f / sqrtf((float)d.head_dim);
-  if (d.dtype == SAMKV_BF16) return launch_packed_tc_scores(d, seqs, kv, Q, scale, mods, O, lse, h, stream);
+  if (d.dtype == SAMKV_BF16) {
+    auto launch = mods.slopes != nullptr ? launch_packed_tc_bias : mods.softcap > 0.f ? launch_packed_tc_cap : launch_packed_tc_mask;
+    return launch(d, seqs, kv, Q, scale, mods, O, lse, h, stream);
+  }
   const pscore::Params p = {seqs, mods, kv, Q, O, scale, lse, h.d_status, d.n_q_heads, d.n_kv_heads};
   return d.head_dim == 128 ? pscore::launch<float, 128>(p, stream) : pscore::launch<float, 64>(p, stream);
 }

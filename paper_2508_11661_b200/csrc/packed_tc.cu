@@ -12,8 +12,8 @@ cudaError_t launch_packed_tc(const samkv_packed_t& d, const Seqs& seqs, const Kv
   const ptc::Params p = ptc::make_params(d, seqs, kv, Q, scale, O, lse, h);
   const int ctas = h.sm_count < kMaxPackedCtas ? h.sm_count : kMaxPackedCtas;
   if (d.head_dim == 128)
-    return kv.paged ? ptc::launch<128, true, false>(p, ctas, stream) : ptc::launch<128, false, false>(p, ctas, stream);
-  return kv.paged ? ptc::launch<64, true, false>(p, ctas, stream) : ptc::launch<64, false, false>(p, ctas, stream);
+    return kv.paged ? ptc::launch<128, true, ptc::MOD_NONE>(p, ctas, stream) : ptc::launch<128, false, ptc::MOD_NONE>(p, ctas, stream);
+  return kv.paged ? ptc::launch<64, true, ptc::MOD_NONE>(p, ctas, stream) : ptc::launch<64, false, ptc::MOD_NONE>(p, ctas, stream);
 }
 
 }  // namespace samkv

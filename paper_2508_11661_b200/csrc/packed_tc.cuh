@@ -54,7 +54,6 @@ constexpr int kThreads = (4 * kGroups + 4) * 32;
 constexpr int kWarpS = 4 * kGroups, kWarpPV = kWarpS + 1, kWarpK = kWarpS + 2, kWarpV = kWarpS + 3;
 constexpr int kRegsSoftmax = 144, kRegsOther = 80;     // 384 x 144 + 128 x 80 = 512 x 128, the launch's registers
 constexpr float kGrow = 16.0f;                         // log2
-constexpr int kModStep = 16;                           // columns that are modified at a time: a loop of 32 does not fit the instruction caches
 constexpr uint32_t kTmemCols = 512, kColO = 384;       // three score buffers of 128 columns, then O
 
 template <int kD>
@@ -98,20 +97,37 @@ __device__ __forceinline__ float max3_nan(float a, float b, float c) {
   return r;
 }
 // 16 columns of this thread's lane.
-__device__ __forceinline__ void tmem_ld16_nowait(uint32_t taddr, float* v) {
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, float* v) {
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
       : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]),
         "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
       : "r"(taddr) : "memory");
-}
-__device__ __forceinline__ void tmem_ld16(uint32_t taddr, float* v) {
-  tmem_ld16_nowait(taddr, v);
   tmem_wait_ld();
 #pragma unroll
   for (int i = 0; i < 16; i += 8)
     asm volatile("" : "+f"(v[i]), "+f"(v[i + 1]), "+f"(v[i + 2]), "+f"(v[i + 3]), "+f"(v[i + 4]), "+f"(v[i + 5]),
                  "+f"(v[i + 6]), "+f"(v[i + 7]));
+}
+// Pins registers that tcgen05.ld filled behind the wait for it.
+template <int kN>
+__device__ __forceinline__ void settle(float* v) {
+#pragma unroll
+  for (int i = 0; i < kN; i += 8)
+    asm volatile("" : "+f"(v[i]), "+f"(v[i + 1]), "+f"(v[i + 2]), "+f"(v[i + 3]), "+f"(v[i + 4]), "+f"(v[i + 5]),
+                 "+f"(v[i + 6]), "+f"(v[i + 7]));
+}
+
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, float* v) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7])
+               : "r"(taddr) : "memory");
+  tmem_wait_ld();
+  asm volatile("" : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]));
+}
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const float* v) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+               ::"r"(taddr), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]) : "memory");
 }
 
 // Scores at and behind `limit` become -infinity.
@@ -128,15 +144,6 @@ __device__ __forceinline__ float max3_abs(float a, float b, float c) { return fm
 __device__ __forceinline__ void add_bf16_pair(float& lo, float& hi, uint32_t packed) {
   asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tadd.rn.f32.bf16 %0, l, %0;\n\tadd.rn.f32.bf16 %1, h, %1;\n\t}"
       : "+f"(lo), "+f"(hi) : "r"(packed));
-}
-
-// Pins registers that tcgen05.ld filled behind the wait for it.
-template <int kN>
-__device__ __forceinline__ void settle(float* v) {
-#pragma unroll
-  for (int i = 0; i < kN; i += 8)
-    asm volatile("" : "+f"(v[i]), "+f"(v[i + 1]), "+f"(v[i + 2]), "+f"(v[i + 3]), "+f"(v[i + 4]), "+f"(v[i + 5]),
-                 "+f"(v[i + 6]), "+f"(v[i + 7]));
 }
 
 struct Params {
@@ -265,16 +272,19 @@ __device__ __forceinline__ bool any_nonfinite(uint32_t tile, int r0, int r1) {
   return __any_sync(0xffffffffu, (hit & 0x80008000u) != 0);
 }
 
+// What a kernel does to scores, each kind a kernel of its own: branches that are not taken still cost instruction fetches
+// (one kernel for all three: a masked call without cap or slopes takes a fifth longer).
+enum Mod { MOD_NONE, MOD_MASK, MOD_CAP, MOD_BIAS };    // the last three with masks, slopes also with a cap
+
 // The cap, c tanh(x / c): x by `in` = scale / c to y, the result by `out` = c log2(e).  Up to |y| = 1, where heads spend their
-// time, tanh(y) = y P(y^2) with P interpolated at the Chebyshev points of [0, 1] (degree 6: 2^-22.6 off in fp32), two values
-// an instruction on the FMA pipe; a special-function exponential and reciprocal each would take twice the time of the
-// softmax's own exponentials, and serve larger scores, in the chunks of 32 x 32 that hold some.
-constexpr float kTanh0 = 0.9999999486f, kTanh1 = -0.3333282798f, kTanh2 = 0.1332507615f, kTanh3 = -0.0534516464f,
-                kTanh4 = 0.0202797083f, kTanh5 = -0.0061943248f, kTanh6 = 0.0010380251f;
+// time, tanh(y) = y P(y^2), P the polynomial of degree 5 with the least relative error on [0, 1]: 2^-20.4 with its evaluation
+// in fp32.  It runs on the FMA pipe, two values an instruction; an exponential and a reciprocal would take twice the time of
+// the softmax's own exponentials on the special-function pipe, and serve larger scores, in the chunks that hold some.
+constexpr float kTanh0 = 0.9999994136f, kTanh1 = -0.3332904230f, kTanh2 = 0.1328143324f, kTanh3 = -0.0516056571f,
+                kTanh4 = 0.0167430969f, kTanh5 = -0.0030670534f;
 __device__ __forceinline__ float cap_one(float x, float in, float out) {
   const float y = x * in, z = y * y;
-  float q = fmaf(kTanh6 * out, z, kTanh5 * out);
-  q = fmaf(q, z, kTanh4 * out);
+  float q = fmaf(kTanh5 * out, z, kTanh4 * out);
   q = fmaf(q, z, kTanh3 * out);
   q = fmaf(q, z, kTanh2 * out);
   q = fmaf(q, z, kTanh1 * out);
@@ -284,25 +294,35 @@ __device__ __forceinline__ float cap_one(float x, float in, float out) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(e + 1.f));
   return z <= 1.f ? y * q : fmaf(-2.f * out, r, out);
 }
-// A row's chunk; all lanes of the warp.
-template <int kN>
-__device__ __forceinline__ void cap_chunk(float* x, float in, float out) {
+// 32 columns of the warp's rows, loaded to x from tensor memory at `at`.
+__device__ __forceinline__ void cap_chunk(float* x, uint32_t at, float in, float out) {
   const f2 in2 = both(in);
   float top = 0.f;
 #pragma unroll
-  for (int i = 0; i < kN; i += 2) top = max3_abs(top, x[i], x[i + 1]);
-  if (__any_sync(0xffffffffu, !(top * in <= 1.f))) {
+  for (int i = 0; i < 32; i += 2) top = max3_abs(top, x[i], x[i + 1]);
+  if (__builtin_expect(__any_sync(0xffffffffu, !(top * in <= 1.f)), 0)) {
+    // rare, so in few instructions: eight columns at a time, by way of tensor memory.  (Each score decides for itself: the same
+    // bits whatever the others are.)
+#pragma unroll 1
+    for (int c = 0; c < 32; c += 8) {
+      float y[8];
+      tmem_ld8(at + c, y);
 #pragma unroll
-    for (int i = 0; i < kN; ++i) x[i] = cap_one(x[i], in, out);   // (each score decides for itself: the same bits either way)
+      for (int i = 0; i < 8; ++i) y[i] = cap_one(y[i], in, out);
+      tmem_st8(at + c, y);
+    }
+    tmem_wait_st();
+    tmem_ld32_nowait(at, x);
+    tmem_wait_ld();
+    settle<32>(x);
     return;
   }
   const f2 c0 = both(kTanh0 * out), c1 = both(kTanh1 * out), c2 = both(kTanh2 * out), c3 = both(kTanh3 * out), c4 = both(kTanh4 * out),
-           c5 = both(kTanh5 * out), c6 = both(kTanh6 * out);
+           c5 = both(kTanh5 * out);
 #pragma unroll
-  for (int i = 0; i < kN; i += 2) {
+  for (int i = 0; i < 32; i += 2) {
     const f2 y = mul2(join2(x[i], x[i + 1]), in2), z = mul2(y, y);
-    f2 q = fma2(c6, z, c5);
-    q = fma2(q, z, c4);
+    f2 q = fma2(c5, z, c4);
     q = fma2(q, z, c3);
     q = fma2(q, z, c2);
     q = fma2(q, z, c1);
@@ -339,14 +359,15 @@ __device__ __forceinline__ void bias_chunk(float* x, float mul, float slope, int
 }
 }  // namespace ptc
 
-template <int kD, bool kPaged, bool kMod>
+template <int kD, bool kPaged, int kMod>
 __global__ void __launch_bounds__(ptc::kThreads, 1)
 packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                  const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmO,
                  const __grid_constant__ ptc::Params p) {
   using namespace ptc;
   using L = Smem<kD>;
-  using P = std::conditional_t<kMod, MaskedPiece, Piece>;
+  constexpr bool kAny = kMod != MOD_NONE;
+  using P = std::conditional_t<kAny, MaskedPiece, Piece>;
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   const uint32_t base = smem_u32(smem_raw);
   const uint32_t sBar = base + L::kBar;
@@ -366,7 +387,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     for (int i = 0; i < kRing; ++i) { mbar_init(bar(FR_FULL + i), 1); mbar_init(bar(FR_FREE + i), 3 + 4 * kGroups); }
     for (int i = 0; i < kQStages; ++i) { mbar_init(bar(Q_FULL + i), 1); mbar_init(bar(Q_FREE + i), 4); }
     mbar_init(bar(V_TMA), 1);
-    if constexpr (kMod) mbar_init(bar(V_TMA_2), 1);
+    if constexpr (kAny) mbar_init(bar(V_TMA_2), 1);
     for (int i = 0; i < kGroups; ++i) {
       mbar_init(bar(S_GO + i), 1 + 1);
       mbar_init(bar(GO + i), 4 + 1);
@@ -396,7 +417,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
   const uint32_t tmem = *s_tmem;
   pdl_wait();                               // everything below reads what earlier kernels may have written
   long long chunk = 0;
-  if constexpr (!kMod) {
+  if constexpr (!kAny) {
     if (p.seqs.n_seq > kWarpPlanSeqs) plan_block<kThreads>(p.seqs, p.cfg, &plan, &chunk, p.d_status, tid);
   }
 
@@ -406,8 +427,8 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOther));
     if (warp == kWarpK) {
       // ================= plan and K =================
-      std::conditional_t<kMod, TileWalker, Walker> w;
-      if constexpr (kMod) {
+      std::conditional_t<kAny, TileWalker, Walker> w;
+      if constexpr (kAny) {
         w.begin(p.seqs, p.mods, p.cfg, p.plan, p.d_status);
       } else {
         w.begin(p.seqs, p.cfg, &plan, chunk, p.d_status);
@@ -420,7 +441,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
       bool bad = false;
       while (true) {
         bool have = *s_fail == 0;
-        if constexpr (kMod) have = have && w.next(p.seqs, p.cfg, p.plan, kPaged, &pc);
+        if constexpr (kAny) have = have && w.next(p.seqs, p.cfg, p.plan, kPaged, &pc);
         else have = have && w.next(p.seqs, p.cfg, &pc);
         if (f >= kRing) wait(FR_FREE + f % kRing, f / kRing - 1);
         if (lane == 0) {
@@ -504,7 +525,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         if (!wait(FR_FULL + f % kRing, f / kRing)) break;
         const int t0 = ring[f % kRing].tile0, t1 = ring[f % kRing].tile1, seen = ring[f % kRing].seen;
         int pre = 0, gap = 0;
-        if constexpr (kMod) {
+        if constexpr (kAny) {
           pre = ring[f % kRing].pre;
           gap = ring[f % kRing].gap;
         }
@@ -521,7 +542,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
           if (lane == 0) {
             const uint64_t dV = dV0 + (uint64_t)(g * (L::kTile >> 4));
             int at = t;
-            if constexpr (kMod) {                          // from the last tile to the first
+            if constexpr (kAny) {                          // from the last tile to the first
               const int v = t1 - 1 - (t - t0);
               at = v * kBN < pre ? v : v + gap;
             }
@@ -579,7 +600,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         __syncwarp();
       };
       while (true) {
-        if constexpr (kMod) {
+        if constexpr (kAny) {
           if (late.look && !is_over(FR_FULL + f % kRing, f / kRing)) finish(late);
         }
         if (!wait(FR_FULL + f % kRing, f / kRing)) break;
@@ -603,7 +624,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
           for (int i = 0; i < n; ++i, ++T) {
             const int t = tile_of(pc, i), j0 = t * kBN;
             int zone0, zone1;
-            if constexpr (kMod) {
+            if constexpr (kAny) {
               zone0 = j0;
               zone1 = min(j0 + kBN, pc.seen);
               hidden_from_some(pc, &zone0, &zone1);
@@ -614,7 +635,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
             int next = 0;
             if constexpr (kPaged) { if (i + 1 < n) next = tile_page(p, pc, tile_of(pc, i + 1), &bad); }
             const uint32_t st = T % kVStages, dst = base + L::kV + st * L::kTile;
-            if constexpr (kMod) {
+            if constexpr (kAny) {
               // (a tile that has to be looked through waits for the next one's copies to be on their way, if their stage is free)
               if (late.look && T >= kVStages && !is_over(PV_DONE + st, T / kVStages - 1)) finish(late);
             }
@@ -631,12 +652,12 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
             if (!now.look) {
               load_tile<kD, kPaged>(p, &tmV, pc, t, dst, bar(GO + st), page);
             } else {
-              now.landed = kMod && (partial_tiles & 1u) ? V_TMA_2 : V_TMA;
-              now.phase = kMod ? partial_tiles >> 1 : partial_tiles;
+              now.landed = kAny && (partial_tiles & 1u) ? V_TMA_2 : V_TMA;
+              now.phase = kAny ? partial_tiles >> 1 : partial_tiles;
               ++partial_tiles;
               load_tile<kD, kPaged>(p, &tmV, pc, t, dst, bar(now.landed), page);
             }
-            if constexpr (kMod) {
+            if constexpr (kAny) {
               if (late.look) finish(late);
               late = now;
             } else {
@@ -677,10 +698,10 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
       RowView view = {};
       float slope = 0.f;
       // rows without a token follow the last one: their results are dropped
-      if constexpr (kMod) {
+      if constexpr (kAny) {
         valid = t_local < pc.n_tok;
         view = row_view(p.seqs, p.mods, pc, t_local);
-        if (p.mods.slopes != nullptr) slope = p.mods.slopes[h * G + member] * kLog2e;
+        if constexpr (kMod == MOD_BIAS) slope = p.mods.slopes[h * G + member] * kLog2e;
       } else {
         const int t_seq = pc.r * p.cfg.tokens + t_local;
         valid = t_local < p.cfg.tokens && t_seq < pc.n;
@@ -705,40 +726,40 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         // instruction caches, straight-line code that does not runs at 3-5 cycles an instruction.)
         const int limit = vis - j0;
         const int width = min(pc.seen - j0, kBN);        // slots that some row sees
-        const bool masked = __any_sync(0xffffffffu, kMod ? !view.sees_all(j0, j0 + kBN) : limit < kBN);
+        const bool masked = __any_sync(0xffffffffu, kAny ? !view.sees_all(j0, j0 + kBN) : limit < kBN);
         float mx0 = -INFINITY, mx1 = -INFINITY, mx2 = -INFINITY, mx3 = -INFINITY;
         // With modifications the scores that come out of them, in the exponent's units, take the others' place; so do those of a
         // tile that is not seen in full, so that masks and caps are worked out once.
-        const bool done = kMod && (p.mods.slopes != nullptr || p.cap_out > 0.f);
-        constexpr int kStep = kMod ? kModStep : 32;
+        constexpr bool kDone = kMod == MOD_CAP || kMod == MOD_BIAS;
 #pragma unroll 1
-        for (int c0 = 0; c0 < kBN; c0 += kStep) {
-          float sv[kStep];
-          if constexpr (kStep == 32) tmem_ld32_nowait(tS + c0, sv); else tmem_ld16_nowait(tS + c0, sv);
+        for (int c0 = 0; c0 < kBN; c0 += 32) {
+          float sv[32];
+          tmem_ld32_nowait(tS + c0, sv);
           tmem_wait_ld();
-          settle<kStep>(sv);
-          if constexpr (kMod) {
-            if (p.cap_out > 0.f) cap_chunk<kStep>(sv, p.cap_in, p.cap_out);
-            if (p.mods.slopes != nullptr) bias_chunk<kStep>(sv, p.cap_out > 0.f ? 1.f : sl2, slope, view.pos, j0 + c0);
-            if (masked) mask_bits<kStep>(sv, view.bits(j0 + c0));
-            if (done || masked) {
-              if constexpr (kStep == 32) tmem_st32(tS + c0, sv); else tmem_st16(tS + c0, reinterpret_cast<const uint32_t*>(sv));
-            }
+          settle<32>(sv);
+          if constexpr (kMod == MOD_CAP) cap_chunk(sv, tS + c0, p.cap_in, p.cap_out);
+          if constexpr (kMod == MOD_BIAS) {
+            if (p.cap_out > 0.f) cap_chunk(sv, tS + c0, p.cap_in, p.cap_out);
+            bias_chunk<32>(sv, p.cap_out > 0.f ? 1.f : sl2, slope, view.pos, j0 + c0);
+          }
+          if constexpr (kMod == MOD_NONE) {
+            if (masked) mask_row<32>(sv, limit - c0);
           } else {
-            if (masked) mask_row<kStep>(sv, limit - c0);
+            if (masked) mask_bits<32>(sv, view.bits(j0 + c0));
+            if (kDone || masked) tmem_st32(tS + c0, sv);
           }
 #pragma unroll
-          for (int k = 0; k < kStep; k += 8) {
+          for (int k = 0; k < 32; k += 8) {
             mx0 = max3_nan(mx0, sv[k], sv[k + 1]);
             mx1 = max3_nan(mx1, sv[k + 2], sv[k + 3]);
             mx2 = max3_nan(mx2, sv[k + 4], sv[k + 5]);
             mx3 = max3_nan(mx3, sv[k + 6], sv[k + 7]);
           }
         }
-        if constexpr (kMod) {
-          if (done || masked) tmem_wait_st();
+        if constexpr (kAny) {
+          if (kDone || masked) tmem_wait_st();
         }
-        const float unit = done ? 1.f : sl2;               // what turns a score into the exponent's units
+        const float unit = kDone ? 1.f : sl2;              // what turns a score into the exponent's units
         const float cand = max3_nan(max3_nan(mx0, mx1, mx2), mx3, mx3) * unit;
         poison |= !(cand < INFINITY);                    // NaN or +infinity among the row's scores
         // The piece's first tile sets the row's reference; the others use the one they know.  Whether a tile before this one
@@ -808,7 +829,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
           tmem_ld32_nowait(tS + c0, x);
           tmem_wait_ld();
           settle<32>(x);
-          if constexpr (!kMod) {
+          if constexpr (!kAny) {
             if (masked) mask_row<32>(x, limit - c0);
           }
           uint32_t pk[16];
@@ -912,7 +933,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
                 if (!(fabsf(y) < INFINITY)) o[i] += y;
               }
             };
-            if constexpr (kMod) {
+            if constexpr (kAny) {
 #pragma unroll 1
               for (int k = 0; k < n; ++k) {
                 int j = pc.tile(k, kBN) * kBN, j1 = min(j + kBN, pc.seen);
@@ -1051,7 +1072,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
 }
 
 namespace ptc {
-template <int kD, bool kPaged, bool kMod>
+template <int kD, bool kPaged, int kMod>
 static cudaError_t launch(const Params& p, int ctas, cudaStream_t stream) {
   CUtensorMap q, k, v, o;
   const int G = p.cfg.G, Hkv = p.cfg.Hkv;
@@ -1069,7 +1090,7 @@ static cudaError_t launch(const Params& p, int ctas, cudaStream_t stream) {
       return cudaErrorInvalidValue;
   }
   auto kern = packed_tc_kernel<kD, kPaged, kMod>;
-  cudaError_t e = ensure_dynamic_smem<3000 + kD * 4 + kPaged * 2 + kMod>(kern, Smem<kD>::kBytes);
+  cudaError_t e = ensure_dynamic_smem<3000 + kD * 8 + kPaged * 4 + kMod>(kern, Smem<kD>::kBytes);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)ctas);
@@ -1123,6 +1144,23 @@ inline Params make_params(const samkv_packed_t& d, const Seqs& seqs, const KvSou
   p.d_status = h.d_status;
   p.Hq = d.n_q_heads;
   return p;
+}
+
+template <int kMod>
+cudaError_t launch_scores(const samkv_packed_t& d, const Seqs& seqs, const KvSource& kv, const Rows& Q, float scale,
+                          const ScoreMods& mods, const Rows& O, float* lse, const samkv_ctx_impl& h, cudaStream_t stream) {
+  Params p = make_params(d, seqs, kv, Q, scale, O, lse, h);
+  p.cfg.wave_slots = 0;
+  p.mods = mods;
+  if (mods.softcap > 0.f) {
+    p.cap_in = scale / mods.softcap;
+    p.cap_out = mods.softcap * tc::kLog2e;
+  }
+  const cudaError_t e = make_score_plan(d, seqs, mods, p.cfg, h, &p.plan, stream);
+  if (e != cudaSuccess) return e;
+  const int ctas = h.sm_count < kMaxPackedCtas ? h.sm_count : kMaxPackedCtas;
+  if (d.head_dim == 128) return kv.paged ? launch<128, true, kMod>(p, ctas, stream) : launch<128, false, kMod>(p, ctas, stream);
+  return kv.paged ? launch<64, true, kMod>(p, ctas, stream) : launch<64, false, kMod>(p, ctas, stream);
 }
 }  // namespace ptc
 
