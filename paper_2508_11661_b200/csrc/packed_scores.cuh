@@ -10,8 +10,8 @@
 // Token i of a row tile sees the slots below the sequence's prefix and those of [low_i, end_i): low_i is the largest of 0,
 // its document's start and the window's edge, end_i rises with i.  A row tile's key tiles are those of the prefix and those
 // of [any0, any1), any0 the lowest low_i and any1 the last end_i: a list with at most one gap, counted from 0 ("virtual").
-// A piece's tiles are taken from the last to the first: with slopes the scores rise towards the diagonal, so that the
-// running maximum is found at once.
+// With slopes a piece's tiles are taken from the last to the first: the scores rise towards the diagonal, so that the running
+// maximum is found at once.  Without, from the first to the last, since the last one often shows a row few of its slots.
 #pragma once
 
 #include "packed_plan.cuh"
@@ -105,14 +105,16 @@ struct MaskedPiece {
   int tok0, pos0, end0;        // as in RowTile
   int pre, any0, all0;
   int gap;                     // TileList
-  int tile0, tile1;            // virtual tiles, taken from the last to the first; tile0 < 0: no more pieces
+  int tile0, tile1;            // virtual tiles; tile0 < 0: no more pieces
   int seen;                    // slots behind which no token sees anything
   short h_, n_tok;
   short slot, slot0;           // workspace slot of the partial result (-1: the piece is the whole item), and of the first one
   short ticket, n_pieces;
   __device__ __forceinline__ int h() const { return (unsigned short)h_; }
-  __device__ __forceinline__ int tile(int i, int slots) const {      // i-th tile taken, of so many slots
-    const int v = tile1 - 1 - i;
+  // tile that is taken i-th, of so many slots
+  template <bool kDown>
+  __device__ __forceinline__ int tile(int i, int slots) const {
+    const int v = kDown ? tile1 - 1 - i : tile0 + i;
     return v * slots < pre ? v : v + gap;
   }
 };

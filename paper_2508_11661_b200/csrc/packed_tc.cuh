@@ -174,8 +174,10 @@ __device__ __forceinline__ int key_row_of(const Piece& pc) { return pc.first; }
 __device__ __forceinline__ int key_row_of(const MaskedPiece& pc) { return pc.kv; }
 __device__ __forceinline__ int head_of(const Piece& pc) { return pc.h; }
 __device__ __forceinline__ int head_of(const MaskedPiece& pc) { return pc.h(); }
+template <bool kDown>
 __device__ __forceinline__ int tile_of(const Piece& pc, int i) { return pc.tile0 + i; }
-__device__ __forceinline__ int tile_of(const MaskedPiece& pc, int i) { return pc.tile(i, kBN); }
+template <bool kDown>
+__device__ __forceinline__ int tile_of(const MaskedPiece& pc, int i) { return pc.tile<kDown>(i, kBN); }
 // Whether the page of slots [j0, j1) is looked up.
 __device__ __forceinline__ bool wanted(const Params&, const Piece& pc, int j0, int) { return j0 < pc.seen; }
 __device__ __forceinline__ bool wanted(const Params& p, const MaskedPiece& pc, int j0, int j1) {
@@ -366,7 +368,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
                  const __grid_constant__ ptc::Params p) {
   using namespace ptc;
   using L = Smem<kD>;
-  constexpr bool kAny = kMod != MOD_NONE;
+  constexpr bool kAny = kMod != MOD_NONE, kDown = kMod == MOD_BIAS;
   using P = std::conditional_t<kAny, MaskedPiece, Piece>;
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   const uint32_t base = smem_u32(smem_raw);
@@ -452,7 +454,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         __syncwarp();
         if (!have) break;
         int page = 0;
-        if constexpr (kPaged) page = tile_page(p, pc, tile_of(pc, 0), &bad);
+        if constexpr (kPaged) page = tile_page(p, pc, tile_of<kDown>(pc, 0), &bad);
         if (f >= kQStages) wait(Q_FREE + f % kQStages, f / kQStages - 1);
         if (lane == 0) {
           const uint32_t q = bar(Q_FULL + f % kQStages), dst = base + L::kQ + (f % kQStages) * L::kTile;
@@ -465,9 +467,9 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         const int n = pc.tile1 - pc.tile0;
 #pragma unroll 1
         for (int i = 0; i < n; ++i, ++T) {
-          const int t = tile_of(pc, i);
+          const int t = tile_of<kDown>(pc, i);
           int next = 0;
-          if constexpr (kPaged) { if (i + 1 < n) next = tile_page(p, pc, tile_of(pc, i + 1), &bad); }
+          if constexpr (kPaged) { if (i + 1 < n) next = tile_page(p, pc, tile_of<kDown>(pc, i + 1), &bad); }
           if (T >= kKStages) wait(S_FULL + (T - kKStages) % kGroups, (T - kKStages) / kGroups);     // its score product is done
           load_tile<kD, kPaged>(p, &tmK, pc, t, base + L::kK + (T % kKStages) * L::kTile, bar(S_GO + T % kGroups), page);
           page = next;
@@ -542,8 +544,8 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
           if (lane == 0) {
             const uint64_t dV = dV0 + (uint64_t)(g * (L::kTile >> 4));
             int at = t;
-            if constexpr (kAny) {                          // from the last tile to the first
-              const int v = t1 - 1 - (t - t0);
+            if constexpr (kAny) {
+              const int v = kDown ? t1 - 1 - (t - t0) : t;
               at = v * kBN < pre ? v : v + gap;
             }
             const int slots = seen - at * kBN;             // steps of 16 slots that some row sees
@@ -618,11 +620,11 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
           // added back, row by row, when the result is written.
           int page = 0;
           bool bad = false;                                        // (reported by the K loader)
-          if constexpr (kPaged) page = tile_page(p, pc, tile_of(pc, 0), &bad);
+          if constexpr (kPaged) page = tile_page(p, pc, tile_of<kDown>(pc, 0), &bad);
           const int n = pc.tile1 - pc.tile0;
 #pragma unroll 1
           for (int i = 0; i < n; ++i, ++T) {
-            const int t = tile_of(pc, i), j0 = t * kBN;
+            const int t = tile_of<kDown>(pc, i), j0 = t * kBN;
             int zone0, zone1;
             if constexpr (kAny) {
               zone0 = j0;
@@ -633,7 +635,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
               zone1 = min(pc.seen, pc.tile1 * kBN);
             }
             int next = 0;
-            if constexpr (kPaged) { if (i + 1 < n) next = tile_page(p, pc, tile_of(pc, i + 1), &bad); }
+            if constexpr (kPaged) { if (i + 1 < n) next = tile_page(p, pc, tile_of<kDown>(pc, i + 1), &bad); }
             const uint32_t st = T % kVStages, dst = base + L::kV + st * L::kTile;
             if constexpr (kAny) {
               // (a tile that has to be looked through waits for the next one's copies to be on their way, if their stage is free)
@@ -719,7 +721,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
 #pragma unroll 1
       for (int i = (int)((kGroups + g - T % kGroups) % kGroups); i < n; i += kGroups) {
         const uint32_t Tt = T + (uint32_t)i;
-        const int j0 = tile_of(pc, i) * kBN;
+        const int j0 = tile_of<kDown>(pc, i) * kBN;
         wait(S_FULL + g, Tt / kGroups);
         tc_fence_after();
         // first pass over the scores: their maximum.  (The loops stay rolled: the code of a tile has to fit the schedulers'
@@ -766,7 +768,9 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         // has moved it meanwhile is looked at when the probabilities are done.
         const bool first = i == 0;
         if (!first && !ref_known) wait(REF + f % kGroups, f / kGroups);
-        float ref = first ? cand : ref_known ? m : *ref_row;
+        // (From the diagonal down the first tile shows some rows few slots, and its maximum is a poor guess: with 2^16 to spare the
+        // next ones seldom pass it by more than the 2^16 that they may.)
+        float ref = first ? (kDown ? cand + kGrow : cand) : ref_known ? m : *ref_row;
         ref_known = true;
         if (first) {
           *ref_row = ref;
@@ -936,7 +940,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
             if constexpr (kAny) {
 #pragma unroll 1
               for (int k = 0; k < n; ++k) {
-                int j = pc.tile(k, kBN) * kBN, j1 = min(j + kBN, pc.seen);
+                int j = tile_of<kDown>(pc, k) * kBN, j1 = min(j + kBN, pc.seen);
                 hidden_from_some(pc, &j, &j1);                     // (what was looked through)
 #pragma unroll 1
                 for (; j < j1; ++j)
