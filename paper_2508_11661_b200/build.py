@@ -12,7 +12,7 @@ CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "libsamkv.so")
 DEBUG_LIB_PATH = os.path.join(PKG_DIR, "libsamkv_debug.so")   # same sources with -DSAMKV_DEBUG_CHECKS (test hooks)
 SOURCES = ["api.cu", "score.cu", "score_static.cu", "select.cu", "topp.cu", "align.cu", "means.cu", "compact.cu", "attn.cu", "attn_mma.cu", "attn_tc2.cu", "attn_tc3.cu", "attn_tc4.cu",
-           "packed_api.cu", "packed_append.cu", "packed_pages.cu", "packed_scores.cu", "packed_attn.cu", "packed_tc.cu", "packed_tc_mask.cu", "packed_tc_cap.cu", "packed_tc_bias.cu", "packed_score_plan.cu", "packed_decode.cu", "packed_f32.cu"]
+           "packed_api.cu", "packed_append.cu", "packed_pages.cu", "packed_scores.cu", "packed_attn.cu", "packed_tc.cu", "packed_tc_mask.cu", "packed_tc_cap.cu", "packed_tc_bias.cu", "packed_score_plan.cu", "packed_decode.cu", "packed_decode_scores.cu", "packed_f32.cu", "packed_f32_scores.cu"]
 
 
 def nvcc_path() -> str:

@@ -142,5 +142,7 @@ size_t scores_scratch_bytes(const samkv_packed_t& p);
 cudaError_t launch_packed_attn(const samkv_packed_t& p, const Seqs& seqs, const KvSource& kv, const Rows& Q, float scale,
                                const Rows& O, float* lse, const samkv_ctx_impl& h, cudaStream_t stream);
 size_t packed_scratch_bytes(const samkv_packed_t& p);
+int f32_row_tile(const samkv_packed_t& p, bool paged, int sm_count);   // rows of the fp32 kernels' row tiles: 8, 32 or 64
+bool few_rows(const samkv_packed_t& p);        // by the hint: what the kernels with short row tiles are for
 
 }  // namespace samkv

@@ -40,8 +40,8 @@
 
 #include <type_traits>
 
+#include "packed_cap.cuh"
 #include "packed_scores.cuh"
-#include "tc_common.cuh"
 
 namespace samkv {
 namespace ptc {
@@ -138,8 +138,6 @@ __device__ __forceinline__ void mask_row(float* v, int limit) {
     if (i >= limit) v[i] = -INFINITY;
 }
 
-// larger of the sizes, NaN left out
-__device__ __forceinline__ float max3_abs(float a, float b, float c) { return fmaxf(fmaxf(a, fabsf(b)), fabsf(c)); }
 // lo += the lower, hi += the upper of two packed bf16 values (widened by the addition itself).
 __device__ __forceinline__ void add_bf16_pair(float& lo, float& hi, uint32_t packed) {
   asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tadd.rn.f32.bf16 %0, l, %0;\n\tadd.rn.f32.bf16 %1, h, %1;\n\t}"
@@ -278,31 +276,9 @@ __device__ __forceinline__ bool any_nonfinite(uint32_t tile, int r0, int r1) {
 // (one kernel for all three: a masked call without cap or slopes takes a fifth longer).
 enum Mod { MOD_NONE, MOD_MASK, MOD_CAP, MOD_BIAS };    // the last three with masks, slopes also with a cap
 
-// The cap, c tanh(x / c): x by `in` = scale / c to y, the result by `out` = c log2(e).  Up to |y| = 1, where heads spend their
-// time, tanh(y) = y P(y^2), P the polynomial of degree 5 with the least relative error on [0, 1]: 2^-20.4 with its evaluation
-// in fp32.  It runs on the FMA pipe, two values an instruction; an exponential and a reciprocal would take twice the time of
-// the softmax's own exponentials on the special-function pipe, and serve larger scores, in the chunks that hold some.
-constexpr float kTanh0 = 0.9999994136f, kTanh1 = -0.3332904230f, kTanh2 = 0.1328143324f, kTanh3 = -0.0516056571f,
-                kTanh4 = 0.0167430969f, kTanh5 = -0.0030670534f;
-__device__ __forceinline__ float cap_one(float x, float in, float out) {
-  const float y = x * in, z = y * y;
-  float q = fmaf(kTanh5 * out, z, kTanh4 * out);
-  q = fmaf(q, z, kTanh3 * out);
-  q = fmaf(q, z, kTanh2 * out);
-  q = fmaf(q, z, kTanh1 * out);
-  q = fmaf(q, z, kTanh0 * out);
-  const float e = fast_exp2(y * (2.f * kLog2e));                   // (infinite and 0 give the ends)
-  float r;
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(e + 1.f));
-  return z <= 1.f ? y * q : fmaf(-2.f * out, r, out);
-}
 // 32 columns of the warp's rows, loaded to x from tensor memory at `at`.
 __device__ __forceinline__ void cap_chunk(float* x, uint32_t at, float in, float out) {
-  const f2 in2 = both(in);
-  float top = 0.f;
-#pragma unroll
-  for (int i = 0; i < 32; i += 2) top = max3_abs(top, x[i], x[i + 1]);
-  if (__builtin_expect(__any_sync(0xffffffffu, !(top * in <= 1.f)), 0)) {
+  if (__builtin_expect(__any_sync(0xffffffffu, beyond<32>(x, in)), 0)) {
     // rare, so in few instructions: eight columns at a time, by way of tensor memory.  (Each score decides for itself: the same
     // bits whatever the others are.)
 #pragma unroll 1
@@ -319,20 +295,7 @@ __device__ __forceinline__ void cap_chunk(float* x, uint32_t at, float in, float
     settle<32>(x);
     return;
   }
-  const f2 c0 = both(kTanh0 * out), c1 = both(kTanh1 * out), c2 = both(kTanh2 * out), c3 = both(kTanh3 * out), c4 = both(kTanh4 * out),
-           c5 = both(kTanh5 * out);
-#pragma unroll
-  for (int i = 0; i < 32; i += 2) {
-    const f2 y = mul2(join2(x[i], x[i + 1]), in2), z = mul2(y, y);
-    f2 q = fma2(c5, z, c4);
-    q = fma2(q, z, c3);
-    q = fma2(q, z, c2);
-    q = fma2(q, z, c1);
-    q = fma2(q, z, c0);
-    const float2 r = split2(mul2(y, q));
-    x[i] = r.x;
-    x[i + 1] = r.y;
-  }
+  cap_pairs<32>(x, in, out);
 }
 // Scores whose bit is not set become -infinity.
 template <int kN>
