@@ -63,7 +63,7 @@ struct Params {
   // calls with modified scores
   ScoreMods mods;
   ScorePlan plan;
-  float cap_in, cap_out;       // scale / softcap, softcap * log2(e); 0: no cap
+  tc::Cap cap;
 };
 static_assert(sizeof(Piece) <= 64 && sizeof(MaskedPiece) <= 64, "descriptors");
 
@@ -341,12 +341,12 @@ packed_decode_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
         }
         if constexpr (kMod) {
           // into the exponent's units
-          if (p.cap_out > 0.f) {
-            if (__builtin_expect(__any_sync(0xffffffffu, beyond<8>(s[0], p.cap_in)), 0)) {
+          if (p.cap.out > 0.f) {
+            if (__builtin_expect(__any_sync(0xffffffffu, beyond<8>(s[0], p.cap)), 0)) {
 #pragma unroll
-              for (int e = 0; e < 8; ++e) s[e >> 2][e & 3] = cap_one(s[e >> 2][e & 3], p.cap_in, p.cap_out);
+              for (int e = 0; e < 8; ++e) s[e >> 2][e & 3] = cap_one(s[e >> 2][e & 3], p.cap);
             } else {
-              cap_pairs<8>(s[0], p.cap_in, p.cap_out);
+              cap_pairs<8>(s[0], p.cap);
             }
           } else {
 #pragma unroll

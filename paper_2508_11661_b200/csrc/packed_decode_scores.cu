@@ -9,10 +9,7 @@ cudaError_t launch_packed_decode_scores(const samkv_packed_t& d, const Seqs& seq
   const int ctas = h.sm_count < kMaxPackedCtas ? h.sm_count : kMaxPackedCtas;
   pdec::Params p = pdec::make_params(d, seqs, kv, Q, scale, O, lse, h, ctas);
   p.mods = mods;
-  if (mods.softcap > 0.f) {
-    p.cap_in = scale / mods.softcap;
-    p.cap_out = mods.softcap * tc::kLog2e;
-  }
+  p.cap = tc::make_cap(mods.softcap, scale);
   const cudaError_t e = make_score_plan(d, seqs, mods, p.cfg, h, &p.plan, stream);
   if (e != cudaSuccess) return e;
   return d.head_dim == 128 ? pdec::launch<128, true>(p, kv, ctas, stream) : pdec::launch<64, true>(p, kv, ctas, stream);

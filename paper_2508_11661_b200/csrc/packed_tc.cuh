@@ -162,7 +162,7 @@ struct Params {
   // calls with modified scores
   ScoreMods mods;
   ScorePlan plan;
-  float cap_in, cap_out;       // scale / softcap, softcap * log2(e); 0: no cap
+  Cap cap;
 };
 
 // What the two kinds of pieces have in common: sequence, first packed key row, head, tile that is taken i-th.
@@ -277,8 +277,8 @@ __device__ __forceinline__ bool any_nonfinite(uint32_t tile, int r0, int r1) {
 enum Mod { MOD_NONE, MOD_MASK, MOD_CAP, MOD_BIAS };    // the last three with masks, slopes also with a cap
 
 // 32 columns of the warp's rows, loaded to x from tensor memory at `at`.
-__device__ __forceinline__ void cap_chunk(float* x, uint32_t at, float in, float out) {
-  if (__builtin_expect(__any_sync(0xffffffffu, beyond<32>(x, in)), 0)) {
+__device__ __forceinline__ void cap_chunk(float* x, uint32_t at, const Cap& cap) {
+  if (__builtin_expect(__any_sync(0xffffffffu, beyond<32>(x, cap)), 0)) {
     // rare, so in few instructions: eight columns at a time, by way of tensor memory.  (Each score decides for itself: the same
     // bits whatever the others are.)
 #pragma unroll 1
@@ -286,7 +286,7 @@ __device__ __forceinline__ void cap_chunk(float* x, uint32_t at, float in, float
       float y[8];
       tmem_ld8(at + c, y);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) y[i] = cap_one(y[i], in, out);
+      for (int i = 0; i < 8; ++i) y[i] = cap_one(y[i], cap);
       tmem_st8(at + c, y);
     }
     tmem_wait_st();
@@ -295,7 +295,7 @@ __device__ __forceinline__ void cap_chunk(float* x, uint32_t at, float in, float
     settle<32>(x);
     return;
   }
-  cap_pairs<32>(x, in, out);
+  cap_pairs<32>(x, cap);
 }
 // Scores whose bit is not set become -infinity.
 template <int kN>
@@ -702,10 +702,10 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
           tmem_ld32_nowait(tS + c0, sv);
           tmem_wait_ld();
           settle<32>(sv);
-          if constexpr (kMod == MOD_CAP) cap_chunk(sv, tS + c0, p.cap_in, p.cap_out);
+          if constexpr (kMod == MOD_CAP) cap_chunk(sv, tS + c0, p.cap);
           if constexpr (kMod == MOD_BIAS) {
-            if (p.cap_out > 0.f) cap_chunk(sv, tS + c0, p.cap_in, p.cap_out);
-            bias_chunk<32>(sv, p.cap_out > 0.f ? 1.f : sl2, slope, view.pos, j0 + c0);
+            if (p.cap.out > 0.f) cap_chunk(sv, tS + c0, p.cap);
+            bias_chunk<32>(sv, p.cap.out > 0.f ? 1.f : sl2, slope, view.pos, j0 + c0);
           }
           if constexpr (kMod == MOD_NONE) {
             if (masked) mask_row<32>(sv, limit - c0);
@@ -731,9 +731,9 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         // has moved it meanwhile is looked at when the probabilities are done.
         const bool first = i == 0;
         if (!first && !ref_known) wait(REF + f % kGroups, f / kGroups);
-        // (From the diagonal down the first tile shows some rows few slots, and its maximum is a poor guess: with 2^16 to spare the
-        // next ones seldom pass it by more than the 2^16 that they may.)
-        float ref = first ? (kDown ? cand + kGrow : cand) : ref_known ? m : *ref_row;
+        // (With masks the first tile often shows a row few slots, and its maximum is a poor guess: with 2^16 to spare the next ones
+        // seldom pass it by more than the 2^16 that they may.)
+        float ref = first ? (kAny ? cand + kGrow : cand) : ref_known ? m : *ref_row;
         ref_known = true;
         if (first) {
           *ref_row = ref;
@@ -1117,12 +1117,8 @@ template <int kMod>
 cudaError_t launch_scores(const samkv_packed_t& d, const Seqs& seqs, const KvSource& kv, const Rows& Q, float scale,
                           const ScoreMods& mods, const Rows& O, float* lse, const samkv_ctx_impl& h, cudaStream_t stream) {
   Params p = make_params(d, seqs, kv, Q, scale, O, lse, h);
-  p.cfg.wave_slots = 0;
   p.mods = mods;
-  if (mods.softcap > 0.f) {
-    p.cap_in = scale / mods.softcap;
-    p.cap_out = mods.softcap * tc::kLog2e;
-  }
+  p.cap = make_cap(mods.softcap, scale);
   const cudaError_t e = make_score_plan(d, seqs, mods, p.cfg, h, &p.plan, stream);
   if (e != cudaSuccess) return e;
   const int ctas = h.sm_count < kMaxPackedCtas ? h.sm_count : kMaxPackedCtas;
