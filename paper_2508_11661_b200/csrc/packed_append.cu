@@ -10,6 +10,7 @@ namespace samkv {
 
 constexpr int kAppendThreads = 128;
 constexpr int kMaxAppendTokens = 2;            // tokens per CTA
+constexpr int kBatch = 2;                       // items of a thread under way at a time
 
 struct AppendArgs {
   Seqs seqs;
@@ -50,6 +51,44 @@ append_rope_kernel(const __grid_constant__ AppendArgs a, const __grid_constant__
   const int n_tok = min(tokens_per_cta, a.seqs.n_tokens - tok0);
   pdl_launch_dependents();
   pdl_wait();
+  // items: [token][Q heads, K heads, V heads][kItems]; a thread's first kBatch are fetched before the positions are known
+  const int half = rope.rot_dim >> 1;
+  const int n_q = a.has_q ? a.Hq : 0;
+  const int per_tok = (n_q + 2 * a.Hkv) * kItems, n_items = n_tok * per_tok;
+  const int rot_items = half / kVec;             // items of a row that hold rotated pairs (both layouts)
+  struct Item {
+    int t, h, e0, e1;                            // token, head, element offsets of the two pieces
+    bool is_q, is_v, rotated;
+  };
+  auto item = [&](int i) {
+    Item x;
+    x.t = i >= per_tok ? 1 : 0;
+    static_assert(kMaxAppendTokens == 2, "tokens of a CTA");
+    const int r = i - x.t * per_tok, head = r / kItems, it = r % kItems;
+    x.is_q = head < n_q;
+    x.is_v = head >= n_q + a.Hkv;
+    x.h = x.is_q ? head : head - n_q - (x.is_v ? a.Hkv : 0);
+    x.rotated = !x.is_v && it < rot_items;
+    // halves of the rotated part when pairs are (i, i + half), else neighbours
+    const bool halves = x.rotated && !rope.interleaved;
+    x.e0 = halves ? it * kVec : it * 2 * kVec;
+    x.e1 = halves ? half + it * kVec : x.e0 + kVec;
+    return x;
+  };
+  uint4 x0[kBatch], x1[kBatch];
+  auto fetch = [&](int first) {
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      const int i = first + k * kAppendThreads;
+      if (i >= n_items) break;
+      const Item x = item(i);
+      const Rows& src = x.is_q ? a.Q : x.is_v ? a.V : a.K;
+      const T* sp = static_cast<const T*>(src.data) + (size_t)(tok0 + x.t) * src.ts + (size_t)x.h * src.hs;
+      x0[k] = *reinterpret_cast<const uint4*>(sp + x.e0);
+      x1[k] = *reinterpret_cast<const uint4*>(sp + x.e1);
+    }
+  };
+  fetch(tid);
   const bool mapped = kAxes && axes.slots != nullptr;
   if (mapped && tid < n_tok) {
     const int slot = axes.slots[tok0 + tid];
@@ -109,7 +148,6 @@ append_rope_kernel(const __grid_constant__ AppendArgs a, const __grid_constant__
     }
   }
   __syncthreads();
-  const int half = rope.rot_dim >> 1;
   for (int i = tid; i < n_tok * half; i += kAppendThreads) {
     const int t = i / half, e = i - t * half;
     const long long at = kAxes ? pos[t * SAMKV_MAX_AXES + axes.axis[e]] : pos[t];
@@ -117,70 +155,56 @@ append_rope_kernel(const __grid_constant__ AppendArgs a, const __grid_constant__
   }
   __syncthreads();
 
-  // items: [token][Q heads, K heads, V heads][kItems]
-  const int n_q = a.has_q ? a.Hq : 0;
-  const int heads = n_q + 2 * a.Hkv;
-  const int per_tok = heads * kItems;
-  const int rot_items = half / kVec;             // items of a row that hold rotated pairs (both layouts)
-  for (int i = tid; i < n_tok * per_tok; i += kAppendThreads) {
-    const int t = i / per_tok, r = i - t * per_tok;
-    const int head = r / kItems, it = r - head * kItems;
-    if (!live[t]) continue;
-    const int tok = tok0 + t;
-    const bool is_q = head < n_q, is_v = head >= n_q + a.Hkv;
-    const int h = is_q ? head : head - n_q - (is_v ? a.Hkv : 0);
-    const bool rotated = !is_v && it < rot_items;
-    // element offsets of the two pieces: halves of the rotated part when pairs are (i, i + half), else neighbours
-    int e0, e1;
-    if (rotated && !rope.interleaved) {
-      e0 = it * kVec;
-      e1 = half + it * kVec;
-    } else {
-      e0 = it * 2 * kVec;
-      e1 = e0 + kVec;
-    }
-    const Rows& src = is_q ? a.Q : is_v ? a.V : a.K;
-    const T* sp = static_cast<const T*>(src.data) + (size_t)tok * src.ts + (size_t)h * src.hs;
-    uint4 x0 = *reinterpret_cast<const uint4*>(sp + e0), x1 = *reinterpret_cast<const uint4*>(sp + e1);
-    if (rotated) {
-      float u[kVec], w[kVec];
-      ElemTraits<T>::unpack(x0, u);
-      ElemTraits<T>::unpack(x1, w);
-      if (rope.interleaved) {
+#pragma unroll 1
+  for (int first = tid; first < n_items; first += kBatch * kAppendThreads) {
+    if (first != tid) fetch(first);
 #pragma unroll
-        for (int k = 0; k < kVec; k += 2) {
-          const float2 c0 = cs[t][(e0 + k) >> 1], c1 = cs[t][(e1 + k) >> 1];
-          const float a0 = u[k], b0 = u[k + 1], a1 = w[k], b1 = w[k + 1];
-          u[k] = a0 * c0.x - b0 * c0.y;
-          u[k + 1] = b0 * c0.x + a0 * c0.y;
-          w[k] = a1 * c1.x - b1 * c1.y;
-          w[k + 1] = b1 * c1.x + a1 * c1.y;
+    for (int k = 0; k < kBatch; ++k) {
+      const int i = first + k * kAppendThreads;
+      if (i >= n_items) break;
+      const Item x = item(i);
+      if (!live[x.t]) continue;
+      if (x.rotated) {
+        float u[kVec], w[kVec];
+        ElemTraits<T>::unpack(x0[k], u);
+        ElemTraits<T>::unpack(x1[k], w);
+        if (rope.interleaved) {
+#pragma unroll
+          for (int e = 0; e < kVec; e += 2) {
+            const float2 c0 = cs[x.t][(x.e0 + e) >> 1], c1 = cs[x.t][(x.e1 + e) >> 1];
+            const float a0 = u[e], b0 = u[e + 1], a1 = w[e], b1 = w[e + 1];
+            u[e] = a0 * c0.x - b0 * c0.y;
+            u[e + 1] = b0 * c0.x + a0 * c0.y;
+            w[e] = a1 * c1.x - b1 * c1.y;
+            w[e + 1] = b1 * c1.x + a1 * c1.y;
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) {
+            const float2 c = cs[x.t][x.e0 + e];
+            const float a0 = u[e], b0 = w[e];
+            u[e] = a0 * c.x - b0 * c.y;
+            w[e] = b0 * c.x + a0 * c.y;
+          }
         }
+        x0[k] = ElemTraits<T>::pack(u);
+        x1[k] = ElemTraits<T>::pack(w);
+      }
+      const int tok = tok0 + x.t;
+      auto put = [&](T* dst) {
+        *reinterpret_cast<uint4*>(dst + x.e0) = x0[k];
+        *reinterpret_cast<uint4*>(dst + x.e1) = x1[k];
+      };
+      if (x.is_q) {
+        put(static_cast<T*>(a.Q_out.data) + (size_t)tok * a.Q_out.ts + (size_t)x.h * a.Q_out.hs);
       } else {
-#pragma unroll
-        for (int k = 0; k < kVec; ++k) {
-          const float2 c = cs[t][e0 + k];
-          const float a0 = u[k], b0 = w[k];
-          u[k] = a0 * c.x - b0 * c.y;
-          w[k] = b0 * c.x + a0 * c.y;
+        if (a.has_rows) {
+          const Rows& dst = x.is_v ? a.V_out : a.K_out;
+          put(static_cast<T*>(dst.data) + (size_t)tok * dst.ts + (size_t)x.h * dst.hs);
         }
+        if (page_row[x.t] >= 0)
+          put(static_cast<T*>(x.is_v ? a.pages.V : a.pages.K) + ((size_t)page_row[x.t] + ((size_t)x.h << a.pages.shift)) * kD);
       }
-      x0 = ElemTraits<T>::pack(u);
-      x1 = ElemTraits<T>::pack(w);
-    }
-    auto put = [&](T* dst) {
-      *reinterpret_cast<uint4*>(dst + e0) = x0;
-      *reinterpret_cast<uint4*>(dst + e1) = x1;
-    };
-    if (is_q) {
-      put(static_cast<T*>(a.Q_out.data) + (size_t)tok * a.Q_out.ts + (size_t)h * a.Q_out.hs);
-    } else {
-      if (a.has_rows) {
-        const Rows& dst = is_v ? a.V_out : a.K_out;
-        put(static_cast<T*>(dst.data) + (size_t)tok * dst.ts + (size_t)h * dst.hs);
-      }
-      if (page_row[t] >= 0)
-        put(static_cast<T*>(is_v ? a.pages.V : a.pages.K) + ((size_t)page_row[t] + ((size_t)h << a.pages.shift)) * kD);
     }
   }
 }
