@@ -15,6 +15,7 @@ import torch
 
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libsamkv.so")
 _lib = None
+_addresses: dict = {}            # of the library's functions, by name
 
 SAMKV_F32, SAMKV_BF16 = 0, 1
 SAMKV_UPDATE_OVERWRITE, SAMKV_UPDATE_FUSION = 0, 1
@@ -89,6 +90,7 @@ def use_library(path: str) -> None:
     libsamkv_debug.so this way); handles created before the switch must not be used after it."""
     global _lib
     _lib = load_library(path)
+    _addresses.clear()
 
 
 def load_library(path: str) -> ctypes.CDLL:
@@ -451,6 +453,40 @@ def _device_ptr(t: Optional[torch.Tensor], what: str, dtype: torch.dtype, shape:
     return t.data_ptr()
 
 
+def _rows(t: torch.Tensor, what: str, dtype: torch.dtype, shape: tuple, device: int) -> tuple:
+    """Pointer, token stride and head stride of a tensor [n_tokens, heads, head_dim] on this CUDA device."""
+    if t.get_device() != device:
+        raise ValueError(f"{what}: expected a CUDA tensor on the current device")
+    if t.dtype is not dtype or t.shape != shape:
+        raise ValueError(f"{what}: expected {dtype} of shape {shape}, got {t.dtype} of shape {tuple(t.shape)}")
+    strides = t.stride()
+    if strides[2] != 1:
+        raise ValueError(f"{what}: the head dimension must be contiguous")
+    return t.data_ptr(), strides[0], strides[1]
+
+
+def _call(name: str, *args) -> int:
+    """Status of a packed call: integers, None, one float, descriptions (ctypes structures), packed tensors (what _rows says)."""
+    return getattr(lib(), name)(*[samkv_rows_t(*a) if type(a) is tuple else a for a in args])
+
+
+try:        # the same without Python's and ctypes' overhead, where build.py has built it
+    from . import _marshal
+    _marshal.otherwise(_device_ptr, _rows)
+    _device_ptr, _rows = _marshal.device_ptr, _marshal.rows
+
+    def _call(name: str, *args) -> int:  # noqa: F811
+        return _marshal.call(_addresses.get(name) or _address(name), *args)
+except ImportError:
+    pass
+
+
+def _address(name: str) -> int:
+    """Where the library in use has this function."""
+    _addresses[name] = ctypes.cast(getattr(lib(), name), ctypes.c_void_p).value
+    return _addresses[name]
+
+
 class Packed:
     """A samkv_packed_t: sequences packed behind one another.  seq_offsets is an int32 CUDA tensor [n_seq + 1] and is
     kept alive here; its values may change between calls."""
@@ -480,18 +516,12 @@ class Packed:
             raise ValueError("seq_offsets: expected a CUDA tensor on the current device")
         return d
 
+    def _rows(self, t: Optional[torch.Tensor], want: tuple, what: str, device: int):
+        return None if t is None else _rows(t, what, self._dtype, want, device)
+
     def rows(self, t: Optional[torch.Tensor], want: tuple, what: str, device: int):
         """samkv_rows_t of a tensor [n_tokens, heads, head_dim] with any token and head strides."""
-        if t is None:
-            return None
-        if t.get_device() != device:
-            raise ValueError(f"{what}: expected a CUDA tensor on the current device")
-        if t.dtype is not self._dtype or t.shape != want:
-            raise ValueError(f"{what}: expected {self._dtype} of shape {want}, got {t.dtype} of shape {tuple(t.shape)}")
-        strides = t.stride()
-        if strides[2] != 1:
-            raise ValueError(f"{what}: the head dimension must be contiguous")
-        return samkv_rows_t(t.data_ptr(), strides[0], strides[1])
+        return None if t is None else samkv_rows_t(*self._rows(t, want, what, device))
 
 
 class Pages:
@@ -542,8 +572,8 @@ def samkv_packed_workspace_bytes(packed: Packed) -> int:
 
 def samkv_prefill(handle: Handle, packed: Packed, Q, K, V, scale: float, O, lse=None):
     dev, q, kv = packed.device(), packed._q, packed._kv
-    status = lib().samkv_prefill(handle._h, packed.c, packed.rows(Q, q, "Q", dev), packed.rows(K, kv, "K", dev),
-                                 packed.rows(V, kv, "V", dev), scale, packed.rows(O, q, "O", dev),
+    status = _call("samkv_prefill", handle._h.value, packed.c, packed._rows(Q, q, "Q", dev), packed._rows(K, kv, "K", dev),
+                                 packed._rows(V, kv, "V", dev), float(scale), packed._rows(O, q, "O", dev),
                                  _device_ptr(lse, "lse", torch.float32, packed._lse, dev), _raw_stream(dev))
     if status:
         raise SamkvError(status, "samkv_prefill")
@@ -552,22 +582,22 @@ def samkv_prefill(handle: Handle, packed: Packed, Q, K, V, scale: float, O, lse=
 def samkv_append(handle: Handle, packed: Packed, K, V, pages: Optional[Pages] = None, cache_len=None,
                  rope: Optional[Rope] = None, positions=None, Q=None, Q_out=None, K_out=None, V_out=None):
     dev, q, kv = packed.device(), packed._q, packed._kv
-    status = lib().samkv_append(handle._h, packed.c, packed.rows(K, kv, "K", dev), packed.rows(V, kv, "V", dev),
+    status = _call("samkv_append", handle._h.value, packed.c, packed._rows(K, kv, "K", dev), packed._rows(V, kv, "V", dev),
                                 None if pages is None else pages.checked(packed),
                                 _device_ptr(cache_len, "cache_len", torch.int32, packed._per_seq, dev),
                                 None if rope is None else rope.c,
                                 _device_ptr(positions, "positions", torch.int32, packed._per_token, dev),
-                                packed.rows(Q, q, "Q", dev), packed.rows(Q_out, q, "Q_out", dev),
-                                packed.rows(K_out, kv, "K_out", dev), packed.rows(V_out, kv, "V_out", dev), _raw_stream(dev))
+                                packed._rows(Q, q, "Q", dev), packed._rows(Q_out, q, "Q_out", dev),
+                                packed._rows(K_out, kv, "K_out", dev), packed._rows(V_out, kv, "V_out", dev), _raw_stream(dev))
     if status:
         raise SamkvError(status, "samkv_append")
 
 
 def samkv_paged_attn(handle: Handle, packed: Packed, pages: Pages, cache_len, Q, scale: float, causal: bool, O, lse=None):
     dev, q = packed.device(), packed._q
-    status = lib().samkv_paged_attn(handle._h, packed.c, pages.checked(packed),
+    status = _call("samkv_paged_attn", handle._h.value, packed.c, pages.checked(packed),
                                     _device_ptr(cache_len, "cache_len", torch.int32, packed._per_seq, dev),
-                                    packed.rows(Q, q, "Q", dev), scale, bool(causal), packed.rows(O, q, "O", dev),
+                                    packed._rows(Q, q, "Q", dev), float(scale), bool(causal), packed._rows(O, q, "O", dev),
                                     _device_ptr(lse, "lse", torch.float32, packed._lse, dev), _raw_stream(dev))
     if status:
         raise SamkvError(status, "samkv_paged_attn")
@@ -587,7 +617,7 @@ def samkv_page_tables(handle: Handle, packed: Packed, cache_len, page_size: int,
     dev, i32 = packed.device(), torch.int32
     table, width = _table(block_table, packed.n_seq, dev)
     n_pages = free_pages.shape[0]
-    status = lib().samkv_page_tables(handle._h, packed.c, _device_ptr(cache_len, "cache_len", i32, packed._per_seq, dev), page_size,
+    status = _call("samkv_page_tables", handle._h.value, packed.c, _device_ptr(cache_len, "cache_len", i32, packed._per_seq, dev), page_size,
                                      n_pages, table, width, _device_ptr(free_pages, "free_pages", i32, (n_pages,), dev),
                                      _device_ptr(n_free, "n_free", i32, (1,), dev),
                                      _device_ptr(n_free_out, "n_free_out", i32, (1,), dev),
@@ -605,7 +635,7 @@ def samkv_release_pages(handle: Handle, block_table, page_size: int, lengths, do
     n_seq, n_pages = block_table.shape[0], free_pages.shape[0]
     if done.dtype not in (torch.bool, torch.uint8):
         raise ValueError("done: expected bool or uint8")
-    status = lib().samkv_release_pages(handle._h, n_seq, table, width, page_size, n_pages,
+    status = _call("samkv_release_pages", handle._h.value, n_seq, table, width, page_size, n_pages,
                                        _device_ptr(lengths, "lengths", i32, (n_seq,), dev),
                                        _device_ptr(done, "done", done.dtype, (n_seq,), dev),
                                        _device_ptr(free_pages, "free_pages", i32, (n_pages,), dev),
@@ -647,14 +677,14 @@ def samkv_append_axes(handle: Handle, packed: Packed, K, V, pages: Optional[Page
             want = (positions.shape[0], packed.n_tokens)
         else:
             want = packed._per_token
-    status = lib().samkv_append_axes(handle._h, packed.c, packed.rows(K, kv, "K", dev), packed.rows(V, kv, "V", dev),
+    status = _call("samkv_append_axes", handle._h.value, packed.c, packed._rows(K, kv, "K", dev), packed._rows(V, kv, "V", dev),
                                      None if pages is None else pages.checked(packed),
                                      _device_ptr(cache_len, "cache_len", torch.int32, packed._per_seq, dev),
                                      _device_ptr(slots, "slots", torch.int32, packed._per_token, dev),
                                      None if rope is None else rope.c,
                                      None if positions is None else _device_ptr(positions, "positions", torch.int32, want, dev),
-                                     stride, packed.rows(Q, q, "Q", dev), packed.rows(Q_out, q, "Q_out", dev),
-                                     packed.rows(K_out, kv, "K_out", dev), packed.rows(V_out, kv, "V_out", dev), _raw_stream(dev))
+                                     stride, packed._rows(Q, q, "Q", dev), packed._rows(Q_out, q, "Q_out", dev),
+                                     packed._rows(K_out, kv, "K_out", dev), packed._rows(V_out, kv, "V_out", dev), _raw_stream(dev))
     if status:
         raise SamkvError(status, "samkv_append_axes")
 
@@ -687,9 +717,9 @@ def samkv_scores_workspace_bytes(packed: Packed) -> int:
 
 def samkv_prefill_scores(handle: Handle, packed: Packed, Q, K, V, scale: float, scores: Optional[Scores], O, lse=None):
     dev, q, kv = packed.device(), packed._q, packed._kv
-    status = lib().samkv_prefill_scores(handle._h, packed.c, packed.rows(Q, q, "Q", dev), packed.rows(K, kv, "K", dev),
-                                        packed.rows(V, kv, "V", dev), scale, None if scores is None else scores.checked(packed),
-                                        packed.rows(O, q, "O", dev),
+    status = _call("samkv_prefill_scores", handle._h.value, packed.c, packed._rows(Q, q, "Q", dev), packed._rows(K, kv, "K", dev),
+                                        packed._rows(V, kv, "V", dev), float(scale), None if scores is None else scores.checked(packed),
+                                        packed._rows(O, q, "O", dev),
                                         _device_ptr(lse, "lse", torch.float32, packed._lse, dev), _raw_stream(dev))
     if status:
         raise SamkvError(status, "samkv_prefill_scores")
@@ -698,10 +728,10 @@ def samkv_prefill_scores(handle: Handle, packed: Packed, Q, K, V, scale: float, 
 def samkv_paged_attn_scores(handle: Handle, packed: Packed, pages: Pages, cache_len, Q, scale: float, causal: bool,
                             scores: Optional[Scores], O, lse=None):
     dev, q = packed.device(), packed._q
-    status = lib().samkv_paged_attn_scores(handle._h, packed.c, pages.checked(packed),
+    status = _call("samkv_paged_attn_scores", handle._h.value, packed.c, pages.checked(packed),
                                            _device_ptr(cache_len, "cache_len", torch.int32, packed._per_seq, dev),
-                                           packed.rows(Q, q, "Q", dev), scale, bool(causal),
-                                           None if scores is None else scores.checked(packed), packed.rows(O, q, "O", dev),
+                                           packed._rows(Q, q, "Q", dev), float(scale), bool(causal),
+                                           None if scores is None else scores.checked(packed), packed._rows(O, q, "O", dev),
                                            _device_ptr(lse, "lse", torch.float32, packed._lse, dev), _raw_stream(dev))
     if status:
         raise SamkvError(status, "samkv_paged_attn_scores")

@@ -1,4 +1,4 @@
-"""Builds libsamkv.so (sm_100a only) in-tree with nvcc.  `python -m paper_2508_11661_b200.build`."""
+"""Builds libsamkv.so (sm_100a only) in-tree with nvcc, and the binding's extension module with g++.  `python -m paper_2508_11661_b200.build`."""
 from __future__ import annotations
 
 import os
@@ -11,6 +11,7 @@ ROOT = os.path.dirname(PKG_DIR)
 CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "libsamkv.so")
 DEBUG_LIB_PATH = os.path.join(PKG_DIR, "libsamkv_debug.so")   # same sources with -DSAMKV_DEBUG_CHECKS (test hooks)
+MARSHAL_PATH = os.path.join(PKG_DIR, "_marshal.so")
 SOURCES = ["api.cu", "score.cu", "score_static.cu", "select.cu", "topp.cu", "align.cu", "means.cu", "compact.cu", "attn.cu", "attn_mma.cu", "attn_tc2.cu", "attn_tc3.cu", "attn_tc4.cu",
            "packed_api.cu", "packed_append.cu", "packed_pages.cu", "packed_scores.cu", "packed_attn.cu", "packed_tc.cu", "packed_tc_mask.cu", "packed_tc_cap.cu", "packed_tc_bias.cu", "packed_score_plan.cu", "packed_decode.cu", "packed_decode_scores.cu", "packed_f32.cu", "packed_f32_scores.cu"]
 
@@ -22,17 +23,36 @@ def nvcc_path() -> str:
     raise RuntimeError("nvcc not found")
 
 
+def build_marshal(force: bool = False) -> str:
+    """The binding's argument checks (csrc/marshal.cpp) as an extension module next to it."""
+    import sysconfig
+
+    import torch
+    src = os.path.join(CSRC, "marshal.cpp")
+    if not force and os.path.exists(MARSHAL_PATH) and os.path.getmtime(MARSHAL_PATH) >= os.path.getmtime(src):
+        return MARSHAL_PATH
+    t = os.path.dirname(torch.__file__)
+    subprocess.check_call(["g++", "-O2", "-std=c++17", "-shared", "-fPIC",
+                           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+                           "-I", sysconfig.get_paths()["include"], "-I", os.path.join(t, "include"),
+                           "-I", os.path.join(t, "include", "torch", "csrc", "api", "include"), src, "-o", MARSHAL_PATH,
+                           "-L", os.path.join(t, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10",
+                           f"-Wl,-rpath,{os.path.join(t, 'lib')}"])
+    return MARSHAL_PATH
+
+
 def _stale(lib_path: str = LIB_PATH) -> bool:
     if not os.path.exists(lib_path):
         return True
     t = os.path.getmtime(lib_path)
-    deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(ROOT, "include", "samkv.h")]
+    deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f != "marshal.cpp"] + [os.path.join(ROOT, "include", "samkv.h")]
     return any(os.path.getmtime(d) > t for d in deps)
 
 
 def build_library(force: bool = False, verbose: bool = False, debug: bool = False) -> str:
     """debug=True builds libsamkv_debug.so: the same library plus the hooks a test needs to make a bounded wait run out."""
     lib_path = DEBUG_LIB_PATH if debug else LIB_PATH
+    build_marshal(force)
     if not force and not _stale(lib_path):
         return lib_path
     objs = []
