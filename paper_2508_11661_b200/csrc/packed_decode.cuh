@@ -143,8 +143,8 @@ packed_decode_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
 
   if (warp == kConsumers) {
     // ================= producer: plan, Q, K and V =================
-    std::conditional_t<kMod, TileWalker, Walker> w;
-    if constexpr (kMod) w.begin(p.seqs, p.mods, p.cfg, p.plan, p.d_status);
+    std::conditional_t<kMod, PieceWindow, Walker> w;
+    if constexpr (kMod) w.begin(p.seqs, p.mods, p.cfg, p.plan, true, p.d_status);
     else w.begin(p.seqs, p.cfg, &plan, chunk, p.d_status);
     __syncwarp();
     P pc;
@@ -152,12 +152,24 @@ packed_decode_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
     bool bad = false;
     while (true) {
       bool have = *s_fail == 0;
-      if constexpr (kMod) have = have && w.next(p.seqs, p.cfg, p.plan, true, &pc);
-      else have = have && w.next(p.seqs, p.cfg, &pc);
+      int from = 0;                                       // the lane that has the piece
+      if constexpr (kMod) {
+        from = have ? w.take(p.seqs, p.mods, p.cfg, p.plan, true, p.d_status) : -1;
+        from = __shfl_sync(0xffffffffu, from, 0);
+        have = from >= 0;
+      } else {
+        have = have && w.next(p.seqs, p.cfg, &pc);
+      }
       if (f >= kRing) wait(FR_FREE + f % kRing, f / kRing - 1);
+      if constexpr (kMod) {
+        if (lane == max(from, 0)) ring[f % kRing] = w.mine;
+        __syncwarp();
+        pc = ring[f % kRing];
+        __syncwarp();
+      }
       if (lane == 0) {
         if (!have) pc.tile0 = -1;
-        ring[f % kRing] = pc;
+        if (!kMod || !have) ring[f % kRing] = pc;
         if (have) {                                       // descriptor and queries complete one barrier
           const uint32_t dst = base + L::kQ + (f % kRing) * L::kQTile;
           mbar_expect_tx(bar(FR_FULL + f % kRing), p.cfg.tokens * G * kD * 2);

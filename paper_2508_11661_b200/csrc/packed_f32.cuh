@@ -100,22 +100,25 @@ packed_f32_kernel(const __grid_constant__ pf32::Params p) {
   const int G = p.cfg.G;
   pdl_wait();
   long long chunk = 0;
-  std::conditional_t<kMod, TileWalker, Walker> w;
+  std::conditional_t<kMod, PieceWindow, Walker> w;
   w.more = false;
   if constexpr (kMod) {
-    if (warp == 0) w.begin(p.seqs, p.mods, p.cfg, p.plan, p.d_status);
+    if (warp == 0) w.begin(p.seqs, p.mods, p.cfg, p.plan, kPaged, p.d_status);
   } else {
     if (p.seqs.n_seq > kWarpPlanSeqs) plan_block<kThreads>(p.seqs, p.cfg, &plan, &chunk, p.d_status, tid);
     if (warp == 0) w.begin(p.seqs, p.cfg, &plan, chunk, p.d_status);
   }
   bool bad = false;
   auto next_piece = [&](int at) {
-    P next;
-    bool have;
-    if constexpr (kMod) have = w.next(p.seqs, p.cfg, p.plan, kPaged, &next);
-    else have = w.next(p.seqs, p.cfg, &next);
-    if (!have) next.tile0 = -1;
-    if (lane == 0) s_piece[at] = next;
+    if constexpr (kMod) {
+      const int from = w.take(p.seqs, p.mods, p.cfg, p.plan, kPaged, p.d_status);
+      if (lane == from) s_piece[at] = w.mine;
+      if (from < 0 && lane == 0) s_piece[at].tile0 = -1;
+    } else {
+      P next;
+      if (!w.next(p.seqs, p.cfg, &next)) next.tile0 = -1;
+      if (lane == 0) s_piece[at] = next;
+    }
   };
   // slot that a tile begins with, by its number in the piece's list of tiles (from the first to the last: results are rescaled
   // at every tile anyway)

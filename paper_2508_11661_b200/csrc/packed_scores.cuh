@@ -2,10 +2,13 @@
 //
 // With masks the tiles of a row tile have no closed form any more.  A plan is made first: a record per row tile of a sequence
 // (all its heads share it) with the slots that its tokens see, and the lengths of all row tiles before it.  CTA c then takes
-// the stretch [c, c + 1) * chunk of the axis as in packed_plan.cuh, finds its place by a search over those lengths, and walks
-// the records; pieces, borders, workspace slots and tickets are those of packed_plan.cuh.
+// the stretch [c, c + 1) * chunk of the axis as in packed_plan.cuh, finds its place by a search over those lengths, and one of
+// its warps works its pieces out 32 at a time, a piece per lane; borders, workspace slots and tickets are those of packed_plan.cuh.
+// (Walking from piece to piece as there, with the records in registers, made a call on 20 documents 4 % slower: the warp that
+// does it also has the key tiles to load.)
 // The plan is a kernel of one block in front of the attention kernel.  Where a call has at most 32 row tiles by the sizes
-// the host knows, the warp that walks the plan makes it in its registers, a record per lane, and there is no such kernel.
+// the host knows, the warp makes it in its registers, a record per lane, and there is no such kernel; such calls run in waves
+// by the rules of packed_plan.cuh.
 //
 // Token i of a row tile sees the slots below the sequence's prefix and those of [low_i, end_i): low_i is the largest of 0,
 // its document's start and the window's edge, end_i rises with i.  A row tile's key tiles are those of the prefix and those
@@ -109,7 +112,7 @@ struct MaskedPiece {
   int seen;                    // slots behind which no token sees anything
   short h_, n_tok;
   short slot, slot0;           // workspace slot of the partial result (-1: the piece is the whole item), and of the first one
-  short ticket, n_pieces;
+  unsigned char ticket, n_pieces, slot_step, unused;   // slot_step 0: slots as in piece_slot, else so far apart
   __device__ __forceinline__ int h() const { return (unsigned short)h_; }
   // tile that is taken i-th, of so many slots
   template <bool kDown>
@@ -119,7 +122,9 @@ struct MaskedPiece {
   }
 };
 static_assert(sizeof(MaskedPiece) == 56, "descriptors");
-__device__ __forceinline__ int piece_slot(const MaskedPiece& p, int k) { return p.slot0 + 2 * k - (k > 0 ? 1 : 0); }
+__device__ __forceinline__ int piece_slot(const MaskedPiece& p, int k) {
+  return p.slot_step > 0 ? p.slot0 + k * p.slot_step : p.slot0 + 2 * k - (k > 0 ? 1 : 0);
+}
 __device__ __forceinline__ int any1_of(const Seqs& q, const MaskedPiece& p) { return end_of(q, p.end0, p.n_tok - 1); }
 // Some token sees some slot of [j0, j1).
 __device__ __forceinline__ bool any_sees(const MaskedPiece& p, int any1, int j0, int j1) {
@@ -152,45 +157,19 @@ __device__ __forceinline__ RowView row_view(const Seqs& q, const ScoreMods& m, c
   return v;
 }
 
-// Walks the pieces of this CTA; run by one whole warp.
-struct TileWalker {
-  long long chunk, p1, item_start, total_len;
-  int n_tiles, w0, h, i;                       // row tiles of the call, first one in the lanes, head, current row tile
-  RowTile mine, cur;                           // lane k: row tile w0 + k
-  int first_piece_tile;
-  bool more;
+// The pieces of this CTA, 32 items (or units of a call in waves) at a time; run by one whole warp.
+struct PieceWindow {
+  MaskedPiece mine;                            // of item (unit) next - 32 + lane
+  unsigned left;                               // lanes whose pieces are still to be taken
+  int next;                                    // first item (unit of this CTA) behind the window
+  int n_tiles;                                 // row tiles of the call
+  int wave_tiles, wave_blocks;                 // a call in waves: tiles of a block, blocks; 0: contiguous stretches
+  long long chunk, p0, p1;                     // this CTA's stretch of the axis
+  bool more;                                   // there may be items behind the window
 
-  __device__ __forceinline__ RowTile from_lane(int k) const {
-    RowTile t;
-    const int* a = reinterpret_cast<const int*>(&mine);
-    int* b = reinterpret_cast<int*>(&t);
-#pragma unroll
-    for (int x = 0; x < kRowTileInts; ++x) b[x] = __shfl_sync(0xffffffffu, a[x], k);
-    return t;
-  }
-  __device__ __forceinline__ void fetch(const ScorePlan& plan, int at) {
-    if (at < w0 || at >= w0 + 32) {
-      w0 = at;
-      const int k = min(at + (int)(threadIdx.x & 31), n_tiles - 1);
-      const int4* src = reinterpret_cast<const int4*>(plan.tiles + k);
-      static_assert(sizeof(RowTile) == 48, "three vectors");
-      int4* dst = reinterpret_cast<int4*>(&mine);
-#pragma unroll
-      for (int x = 0; x < 3; ++x) dst[x] = src[x];
-    }
-    cur = from_lane(at - w0);
-    i = at;
-  }
-  __device__ __forceinline__ int border(const SplitCfg& c, long long p, int nt) const {
-    const long long y = p - item_start - c.fixed;
-    if (y <= 0) return 0;
-    const long long t = (y + c.tile / 2) >> (31 - __clz(c.tile));
-    if (t < 2) return 0;
-    if (t > nt - 2) return nt;
-    return (int)t;
-  }
-  // Lays a call of at most 32 row tiles out; the lanes keep the records.
-  __device__ __forceinline__ long long plan_in_warp(const Seqs& q, const ScoreMods& m, const SplitCfg& c, int* d_status) {
+  // A call of at most 32 row tiles: lane i gets the record of row tile i, its length and those before it.
+  __device__ __forceinline__ void plan_in_warp(const Seqs& q, const ScoreMods& m, const SplitCfg& c, RowTile& t, long long& before,
+                                               long long& len, int* d_status) {
     const int lane = threadIdx.x & 31;
     Seq x = {0, 0, 0, false, false};
     if (lane < q.n_seq) x = load_seq(q, lane);
@@ -215,128 +194,225 @@ struct TileWalker {
     sq.n = __shfl_sync(0xffffffffu, x.n, from);
     sq.base = __shfl_sync(0xffffffffu, x.base, from);
     const int r = lane - __shfl_sync(0xffffffffu, incl - R, from);
-    long long len = 0;
-    w0 = 0;
+    len = 0;
     if (lane < n_tiles) {
-      mine = make_row_tile(q, m, c, s, sq, r);
-      len = (long long)mine.nt * c.tile + c.fixed;
+      t = make_row_tile(q, m, c, s, sq, r);
+      len = (long long)t.nt * c.tile + c.fixed;
     }
-    return len;
-  }
-  __device__ __forceinline__ void begin(const Seqs& q, const ScoreMods& m, const SplitCfg& c, const ScorePlan& plan, int* d_status) {
-    const int lane = threadIdx.x & 31;
-    long long in_lane = 0, before = 0;         // lengths of the row tiles in the lanes, of those before them
-    const bool small = plan.at == nullptr;
-    if (small) {
-      long long incl = plan_in_warp(q, m, c, d_status);
-      in_lane = incl;
+    before = len;
 #pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const long long v = __shfl_up_sync(0xffffffffu, incl, o);
-        if (lane >= o) incl += v;
-      }
-      before = incl - in_lane;
-      total_len = c.Hkv * __shfl_sync(0xffffffffu, incl, 31);
-    } else {
-      n_tiles = *plan.n_tiles;
-      total_len = c.Hkv * plan.at[n_tiles];
-      w0 = -64;
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long v = __shfl_up_sync(0xffffffffu, before, o);
+      if (lane >= o) before += v;
     }
-    chunk = stretch(c, total_len, c.Hkv * n_tiles);
-    const long long p0 = chunk * blockIdx.x;
-    more = p0 < total_len;
-    if (!more) return;
-    p1 = min(p0 + chunk, total_len);
-    auto at = [&](int k) { return small ? __shfl_sync(0xffffffffu, before, k) : plan.at[k]; };
-    // last row tile of [lo, lo + n) that starts at or before x (of one head): 32 candidates at a time
-    auto search = [&](int lo, int n, long long scale, long long x) {
-      if (small) {
-        const unsigned fits = __ballot_sync(0xffffffffu, lane >= lo && lane < lo + n && scale * before <= x);
-        return 31 - __clz(fits);
-      }
-#pragma unroll 1
-      while (n > 1) {
-        const int step = (n + 31) >> 5, k = lane * step;
-        const unsigned fits = __ballot_sync(0xffffffffu, k < n && scale * plan.at[lo + min(k, n - 1)] <= x);
-        const int skip = (__popc(fits) - 1) * step;
-        lo += skip;
-        n = min(step, n - skip);
-      }
-      return lo;
-    };
-    fetch(plan, search(0, n_tiles, c.Hkv, p0));          // some row tile of the sequence that holds p0
-    const int r0 = i - cur.r, R = cur.R;
-    const long long start = at(r0);
-    const long long end = !small ? plan.at[r0 + R]
-                                 : __shfl_sync(0xffffffffu, before, r0 + R - 1) + __shfl_sync(0xffffffffu, in_lane, r0 + R - 1);
-    const long long per_head = end - start;
-    long long rem = p0 - c.Hkv * start;
-    h = (int)quotient(rem, per_head);
-    rem -= h * per_head;
-    const int k = search(r0, R, 1, start + rem);
-    item_start = c.Hkv * start + h * per_head + (at(k) - start);
-    fetch(plan, k);
-    first_piece_tile = border(c, p0, cur.nt);
+    before -= len;
   }
-  __device__ __forceinline__ bool next(const Seqs& q, const SplitCfg& c, const ScorePlan& plan, bool paged, MaskedPiece* out) {
+  // Whether such a call runs in waves: the rules of packed_plan.cuh, by the tiles that the masks leave.
+  __device__ __forceinline__ void choose_waves(const SplitCfg& c, const RowTile& t, long long total) {
+    const int lane = threadIdx.x & 31;
+    wave_tiles = wave_blocks = 0;
+    if (c.wave_slots == 0 || c.Hkv * n_tiles > kMaxTickets || total <= 2 * c.wave_slots) return;
+    const int nt = lane < n_tiles ? t.nt : 0, most = __reduce_max_sync(0xffffffffu, nt);
+    // (of a sequence's row tiles the last one sees most)
+    const long long distinct = (long long)c.Hkv * c.tile * __reduce_add_sync(0xffffffffu, lane < n_tiles && t.r + 1 == t.R ? nt : 0);
+    if (distinct <= c.wave_slots || total <= 2 * distinct) return;
+    long long best = -1;
 #pragma unroll 1
-    while (more) {
-      const int nt = cur.nt;
-      const long long end = item_start + (long long)nt * c.tile + c.fixed;
-      const int t0 = first_piece_tile >= 0 ? first_piece_tile : 0;
-      const bool starts_inside = first_piece_tile > 0;
-      first_piece_tile = -1;
-      const int t1 = p1 >= end ? nt : border(c, p1, nt);
-      const bool ends_inside = t1 < nt;
-      const bool emit = t0 < t1;
-      if (emit) {
-        out->kv = paged ? cur.s : cur.first;
-        out->tok0 = cur.tok0;
-        out->pos0 = cur.pos0;
-        out->end0 = cur.end0;
-        out->pre = cur.pre;
-        out->any0 = cur.any0;
-        out->all0 = cur.all0;
-        const int any1 = end_of(q, cur.end0, cur.n_tok - 1);
-        const TileList l = tile_list(cur.pre, cur.any0, any1, c.tile);
-        out->gap = l.gap;
-        out->seen = max(cur.pre, cur.any0 < any1 ? any1 : 0);
-        out->tile0 = t0;
-        out->tile1 = t1;
-        out->h_ = (short)h;
-        out->n_tok = (short)cur.n_tok;
-        out->slot = -1;
-        out->slot0 = 0;
-        out->ticket = 0;
-        out->n_pieces = 1;
-        if (starts_inside || ends_inside) {
-          // borders inside the item, after they have been moved to tile borders
-          long long ca = quotient(item_start, chunk) + 1, cb = quotient(end - 1, chunk);
-#pragma unroll 1
-          while (ca <= cb && border(c, ca * chunk, nt) == 0) ++ca;
-#pragma unroll 1
-          while (cb >= ca && border(c, cb * chunk, nt) >= nt) --cb;
-          out->slot = (short)(2 * (int)blockIdx.x + (starts_inside ? 0 : 1));
-          out->ticket = (short)ca;
-          out->n_pieces = (short)((int)(cb - ca) + 2);
-          out->slot0 = (short)(2 * ((int)ca - 1) + 1);
-        }
+    for (int k = 1; k <= kWaveTries; ++k) {
+      const int bt = (most + k - 1) / k;
+      const int units = c.Hkv * __reduce_add_sync(0xffffffffu, (nt + bt - 1) / bt);
+      if (c.Hkv * k * n_tiles > kMaxUnits || bt < 8) continue;
+      const long long cost = (long long)((units + gridDim.x - 1) / gridDim.x) * (bt * c.tile + c.fixed);
+      if (best < 0 || cost < best) {
+        best = cost;
+        wave_tiles = bt;
+        wave_blocks = (most + bt - 1) / bt;
       }
-      if (p1 <= end) {
-        more = false;
-      } else {
-        item_start = end;
-        int next_tile = i + 1;
-        if (cur.r + 1 == cur.R) {
-          if (++h == c.Hkv) h = 0;
-          else next_tile = i + 1 - cur.R;
-        }
-        if (next_tile < n_tiles) fetch(plan, next_tile);
-        else more = false;
-      }
-      if (emit) return true;
     }
-    return false;
+    // (an uneven mix of lengths leaves holes in the waves; the keys are fetched again instead)
+    if (best > total / (long long)gridDim.x * 3 / 2) wave_tiles = 0;
+  }
+  // Tile border of an item nearest to position p of the axis; pieces shorter than two tiles are not worth their merge.
+  static __device__ __forceinline__ int border(const SplitCfg& c, long long p, long long item_start, int nt) {
+    const long long y = p - item_start - c.fixed;
+    if (y <= 0) return 0;
+    const long long t = (y + c.tile / 2) >> (31 - __clz(c.tile));
+    if (t < 2) return 0;
+    if (t > nt - 2) return nt;
+    return (int)t;
+  }
+  // The lane's piece of row tile t and head h, tiles [tile0, tile1).
+  __device__ __forceinline__ void describe(const Seqs& q, const SplitCfg& c, const RowTile& t, int h, bool paged, int tile0, int tile1) {
+    mine.kv = paged ? t.s : t.first;
+    mine.tok0 = t.tok0;
+    mine.pos0 = t.pos0;
+    mine.end0 = t.end0;
+    mine.pre = t.pre;
+    mine.any0 = t.any0;
+    mine.all0 = t.all0;
+    const int any1 = end_of(q, t.end0, t.n_tok - 1);
+    mine.gap = tile_list(t.pre, t.any0, any1, c.tile).gap;
+    mine.seen = max(t.pre, t.any0 < any1 ? any1 : 0);
+    mine.tile0 = tile0;
+    mine.tile1 = tile1;
+    mine.h_ = (short)h;
+    mine.n_tok = (short)t.n_tok;
+    mine.slot = -1;
+    mine.slot0 = 0;
+    mine.ticket = mine.slot_step = mine.unused = 0;
+    mine.n_pieces = 1;
+  }
+  // tile_at(k): record of row tile k (each lane its own k); before(k): lengths before it, k = n_tiles: all.
+  template <typename TileAt, typename Before>
+  __device__ __forceinline__ void fill(const Seqs& q, const SplitCfg& c, bool paged, TileAt tile_at, Before before) {
+    const int lane = threadIdx.x & 31, g = next + lane;
+    next += 32;
+    bool emit;
+    if (wave_tiles > 0) {
+      // unit ((h * blocks) + b) * n_tiles + i is block b of row tile i and head h
+      const int u = g * (int)gridDim.x + (int)blockIdx.x, units = c.Hkv * wave_blocks * n_tiles;
+      const int x = min(u, units - 1), rest = x / n_tiles, i = x - rest * n_tiles, h = rest / wave_blocks, b = rest - h * wave_blocks;
+      const RowTile t = tile_at(i);
+      emit = u < units && b * wave_tiles < t.nt;
+      describe(q, c, t, h, paged, b * wave_tiles, min((b + 1) * wave_tiles, t.nt));
+      mine.n_pieces = (unsigned char)((t.nt + wave_tiles - 1) / wave_tiles);
+      mine.ticket = (unsigned char)(h * n_tiles + i);
+      mine.slot0 = (short)(u - b * n_tiles);
+      mine.slot_step = (unsigned char)n_tiles;
+      if (mine.n_pieces > 1) mine.slot = (short)u;
+      more = __all_sync(0xffffffffu, u < units);
+    } else {
+      // items run sequence by sequence, head by head, row tile by row tile: item g is among those of row tile g / Hkv's sequence
+      const int last = c.Hkv * n_tiles - 1, x = min(g, last);
+      const RowTile some = tile_at(x / c.Hkv);
+      const int r0 = x / c.Hkv - some.r, rest = x - c.Hkv * r0, h = rest / some.R, k = r0 + rest - h * some.R;
+      const RowTile t = tile_at(k);
+      const long long at0 = before(r0);
+      const long long start = c.Hkv * at0 + h * (before(r0 + some.R) - at0) + (before(k) - at0);
+      const long long end = start + (long long)t.nt * c.tile + c.fixed;
+      const bool in = g <= last && start < p1;
+      const int t0 = border(c, p0, start, t.nt), t1 = p1 >= end ? t.nt : border(c, p1, start, t.nt);
+      emit = in && t0 < t1;
+      describe(q, c, t, h, paged, t0, t1);
+      if (emit && (t0 > 0 || t1 < t.nt)) {
+        // borders inside the item, after they have been moved to tile borders
+        long long ca = quotient(start, chunk) + 1, cb = quotient(end - 1, chunk);
+#pragma unroll 1
+        while (ca <= cb && border(c, ca * chunk, start, t.nt) == 0) ++ca;
+#pragma unroll 1
+        while (cb >= ca && border(c, cb * chunk, start, t.nt) >= t.nt) --cb;
+        mine.slot = (short)(2 * (int)blockIdx.x + (t0 > 0 ? 0 : 1));
+        mine.ticket = (unsigned char)ca;
+        mine.n_pieces = (unsigned char)((int)(cb - ca) + 2);
+        mine.slot0 = (short)(2 * ((int)ca - 1) + 1);
+      }
+      more = __all_sync(0xffffffffu, in);
+    }
+    left = __ballot_sync(0xffffffffu, emit);
+  }
+  // The next window; the first one if `begin`.
+  __device__ __forceinline__ void refill(const Seqs& q, const ScoreMods& m, const SplitCfg& c, const ScorePlan& plan, bool paged, bool begin,
+                                         int* d_status) {
+    const int lane = threadIdx.x & 31;
+    if (plan.at == nullptr) {
+      RowTile t = {};
+      long long at, len;
+      plan_in_warp(q, m, c, t, at, len, d_status);         // (again for every window: few calls have a second one)
+      const long long total = __shfl_sync(0xffffffffu, at + len, 31);
+      auto tile_at = [&](int k) {
+        RowTile x;
+        const int* from = reinterpret_cast<const int*>(&t);
+        int* to = reinterpret_cast<int*>(&x);
+#pragma unroll
+        for (int i = 0; i < kRowTileInts; ++i) to[i] = __shfl_sync(0xffffffffu, from[i], k);
+        return x;
+      };
+      if (begin) {
+        choose_waves(c, t, c.Hkv * total);
+        next = 0;
+        more = n_tiles > 0;
+        left = 0;
+        if (wave_tiles == 0 && more) {
+          place(c, c.Hkv * total);
+          if (more) {
+            // the last row tile that starts at or before p0, were there one head; then that of p0's head
+            const int some = 31 - __clz(__ballot_sync(0xffffffffu, lane < n_tiles && c.Hkv * at <= p0));
+            const int r0 = some - __shfl_sync(0xffffffffu, t.r, some), R = __shfl_sync(0xffffffffu, t.R, some);
+            const long long start = __shfl_sync(0xffffffffu, at, r0), per_head = __shfl_sync(0xffffffffu, at + len, r0 + R - 1) - start;
+            const int h = (int)quotient(p0 - c.Hkv * start, per_head);
+            const long long rest = p0 - c.Hkv * start - h * per_head;
+            const int k = 31 - __clz(__ballot_sync(0xffffffffu, lane >= r0 && lane < r0 + R && at - start <= rest));
+            next = c.Hkv * r0 + h * R + (k - r0);
+          }
+        }
+        if (!more) return;
+      }
+      // (a shuffle is for all lanes: the sum of all lengths stands behind the last row tile)
+      auto before_any = [&](int k) {
+        const long long v = __shfl_sync(0xffffffffu, at, min(k, 31));
+        return k < n_tiles ? v : total;
+      };
+      fill(q, c, paged, tile_at, before_any);
+    } else {
+      if (begin) {
+        n_tiles = *plan.n_tiles;
+        wave_tiles = wave_blocks = 0;
+        left = 0;
+        more = n_tiles > 0;
+        if (more) place(c, c.Hkv * plan.at[n_tiles]);
+        if (!more) return;
+        // last row tile of [lo, lo + n) that starts at or before x (of one head): 32 candidates at a time
+        auto search = [&](int lo, int n, long long scale, long long x) {
+#pragma unroll 1
+          while (n > 1) {
+            const int step = (n + 31) >> 5, k = lane * step;
+            const unsigned fits = __ballot_sync(0xffffffffu, k < n && scale * plan.at[lo + min(k, n - 1)] <= x);
+            const int skip = (__popc(fits) - 1) * step;
+            lo += skip;
+            n = min(step, n - skip);
+          }
+          return lo;
+        };
+        const int some = search(0, n_tiles, c.Hkv, p0);
+        const int r0 = some - plan.tiles[some].r, R = plan.tiles[some].R;
+        const long long start = plan.at[r0], per_head = plan.at[r0 + R] - start;
+        const int h = (int)quotient(p0 - c.Hkv * start, per_head);
+        next = c.Hkv * r0 + h * R + (search(r0, R, 1, p0 - (c.Hkv - 1) * start - h * per_head) - r0);
+      }
+      auto tile_at = [&](int k) {
+        RowTile t;
+        const int4* src = reinterpret_cast<const int4*>(plan.tiles + k);
+        static_assert(sizeof(RowTile) == 48, "three vectors");
+        int4* dst = reinterpret_cast<int4*>(&t);
+#pragma unroll
+        for (int i = 0; i < 3; ++i) dst[i] = src[i];
+        return t;
+      };
+      fill(q, c, paged, tile_at, [&](int k) { return plan.at[k]; });
+    }
+  }
+  // This CTA's stretch.
+  __device__ __forceinline__ void place(const SplitCfg& c, long long total) {
+    chunk = stretch(c, total, c.Hkv * n_tiles);
+    p0 = chunk * blockIdx.x;
+    p1 = min(p0 + chunk, total);
+    more = p0 < total;
+  }
+  __device__ __forceinline__ void begin(const Seqs& q, const ScoreMods& m, const SplitCfg& c, const ScorePlan& plan, bool paged,
+                                        int* d_status) {
+    refill(q, m, c, plan, paged, true, d_status);
+  }
+  // The lane that holds the next piece, -1: there is none.
+  __device__ __forceinline__ int take(const Seqs& q, const ScoreMods& m, const SplitCfg& c, const ScorePlan& plan, bool paged,
+                                      int* d_status) {
+#pragma unroll 1
+    while (left == 0) {
+      if (!more) return -1;
+      refill(q, m, c, plan, paged, false, d_status);
+    }
+    const int k = __ffs(left) - 1;
+    left &= left - 1;
+    return k;
   }
 };
 

@@ -392,9 +392,9 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOther));
     if (warp == kWarpK) {
       // ================= plan and K =================
-      std::conditional_t<kAny, TileWalker, Walker> w;
+      std::conditional_t<kAny, PieceWindow, Walker> w;
       if constexpr (kAny) {
-        w.begin(p.seqs, p.mods, p.cfg, p.plan, p.d_status);
+        w.begin(p.seqs, p.mods, p.cfg, p.plan, kPaged, p.d_status);
       } else {
         w.begin(p.seqs, p.cfg, &plan, chunk, p.d_status);
         __syncwarp();
@@ -405,17 +405,27 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
       uint32_t f = 0, T = 0;                // pieces, key tiles so far
       bool bad = false;
       while (true) {
-        bool have = *s_fail == 0;
-        if constexpr (kAny) have = have && w.next(p.seqs, p.cfg, p.plan, kPaged, &pc);
-        else have = have && w.next(p.seqs, p.cfg, &pc);
+        int from = 0;                       // the lane that has the piece, -1: no more
+        if constexpr (kAny) {
+          from = *s_fail == 0 ? w.take(p.seqs, p.mods, p.cfg, p.plan, kPaged, p.d_status) : -1;
+          from = __shfl_sync(0xffffffffu, from, 0);
+        } else {
+          if (!(*s_fail == 0 && w.next(p.seqs, p.cfg, &pc))) from = -1;
+        }
         if (f >= kRing) wait(FR_FREE + f % kRing, f / kRing - 1);
+        if constexpr (kAny) {
+          if (lane == max(from, 0)) ring[f % kRing] = w.mine;
+          __syncwarp();
+        } else {
+          if (lane == 0) ring[f % kRing] = pc;
+        }
         if (lane == 0) {
-          if (!have) pc.tile0 = -1;
-          ring[f % kRing] = pc;
+          if (from < 0) ring[f % kRing].tile0 = -1;
           mbar_arrive(bar(FR_FULL + f % kRing));
         }
         __syncwarp();
-        if (!have) break;
+        if (from < 0) break;
+        if constexpr (kAny) pc = ring[f % kRing];
         int page = 0;
         if constexpr (kPaged) page = tile_page(p, pc, tile_of<kDown>(pc, 0), &bad);
         if (f >= kQStages) wait(Q_FREE + f % kQStages, f / kQStages - 1);
