@@ -537,7 +537,9 @@ typedef struct {
  * partial results.  0 on a bad description. */
 size_t samkv_scores_workspace_bytes(const samkv_packed_t* packed);
 
-/* samkv_prefill with modified scores.  scores == NULL, or a description that modifies nothing: samkv_prefill itself. */
+/* samkv_prefill with modified scores.  scores == NULL, or a description that modifies nothing: samkv_prefill itself.
+ * Precision as there; the cap is good to 2^-20 of its value.  bf16 prompts and chunks: products of weights and values are formed
+ * with weights of 2^-16 at least for a row's largest score (and up to 2^16), so that values of V below about 2^-100 can be lost. */
 samkv_status_t samkv_prefill_scores(samkv_handle_t h, const samkv_packed_t* packed, const samkv_rows_t* Q,
                                     const samkv_rows_t* K, const samkv_rows_t* V, float scale, const samkv_scores_t* scores,
                                     const samkv_rows_t* O, float* lse, void* stream);

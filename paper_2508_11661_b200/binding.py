@@ -505,6 +505,7 @@ class Packed:
         self._dtype = _TORCH_DTYPES.get(code)
         self._q, self._kv = (n_tokens, n_q_heads, head_dim), (n_tokens, n_kv_heads, head_dim)
         self._lse, self._per_token, self._per_seq = (n_tokens, n_q_heads), (n_tokens,), (self.n_seq,)
+        self._pages = (self._device, self._dtype, n_kv_heads, head_dim, self.n_seq)
 
     def ref(self):
         return ctypes.byref(self.c)
@@ -538,9 +539,12 @@ class Pages:
             raise ValueError("pages: expected tensors on one device")
         self.K, self.V, self.block_table = K, V, block_table
         self.c = samkv_pages_t(K.data_ptr(), V.data_ptr(), block_table.data_ptr(), K.shape[2], K.shape[0], block_table.shape[1])
+        self._fits = (K.get_device(), K.dtype, K.shape[1], K.shape[3], block_table.shape[0])
 
     def checked(self, packed: Packed):
         """The description for a call with these sequences."""
+        if self._fits == packed._pages:
+            return self.c
         if self.K.get_device() != packed._device:
             raise ValueError("pages: expected CUDA tensors on the current device")
         shape = self.K.shape
@@ -606,9 +610,10 @@ def samkv_paged_attn(handle: Handle, packed: Packed, pages: Pages, cache_len, Q,
 # ------------------------------------------------------------------ pages handed out on the GPU
 def _table(t: torch.Tensor, n_seq: Optional[int], device: int):
     """Pointer and width of an int32 block table [n_seq, width]."""
-    if t.dim() != 2 or (n_seq is not None and t.shape[0] != n_seq):
+    shape = t.shape
+    if len(shape) != 2 or (n_seq is not None and shape[0] != n_seq):
         raise ValueError(f"block_table: expected {'n_seq' if n_seq is None else n_seq} rows")
-    return _device_ptr(t, "block_table", torch.int32, t.shape, device), t.shape[1]
+    return _device_ptr(t, "block_table", torch.int32, shape, device), shape[1]
 
 
 def samkv_page_tables(handle: Handle, packed: Packed, cache_len, page_size: int, block_table, free_pages, n_free, n_free_out,

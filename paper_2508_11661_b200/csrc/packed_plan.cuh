@@ -21,7 +21,7 @@
 // share keys that the L2 cache cannot hold, every one of them would fetch them from HBM again; such calls are laid out in
 // waves instead: keys are cut into blocks of one length, a unit is a row tile times a block, units run block by block
 // with the row tiles next to one another, and CTA c takes units c, c + grid, ...: the row tiles of a block run at the same
-// time and share its keys through L2 (128 tokens over 102400, 8 row tiles per KV head: see packed_tc.cu).  Calls of more
+// time and share its keys through L2 (128 tokens over 102400, 8 row tiles per KV head: see packed_tc.cuh).  Calls of more
 // than 240 items (kMaxTickets; 8 KV heads with 8 query heads each: 480 tokens) keep the contiguous layout.
 //
 // A sequence that ends before it starts also ends the list of sequences: those behind it could own the same rows again,

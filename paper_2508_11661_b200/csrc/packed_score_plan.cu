@@ -55,13 +55,18 @@ score_plan_kernel(const __grid_constant__ Seqs q, const __grid_constant__ ScoreM
     for (int i0 = 0; i0 < chunk; i0 += kPlanThreads) {
       const int i = i0 + tid;
       long long len = 0;
+      RowTile t = {};
       if (i < chunk) {
         int lo = 0, hi = count - 1;            // last sequence that starts at or before i: the one that owns it
         while (lo < hi) {
           const int mid = (lo + hi + 1) >> 1;
           if (s_off[mid] <= i) lo = mid; else hi = mid - 1;
         }
-        const RowTile t = make_row_tile(q, m, c, s0 + lo, load_seq(q, s0 + lo), i - s_off[lo]);
+        t = make_row_tile(q, m, c, s0 + lo, load_seq(q, s0 + lo), i - s_off[lo]);
+      }
+      if (chunk > 256 && c.tokens > 8) finish_row_tiles<true>(q, m, c, i < chunk, t);
+      else finish_row_tiles<false>(q, m, c, i < chunk, t);
+      if (i < chunk) {
         plan.tiles[n_tiles + i] = t;
         len = (long long)t.nt * c.tile + c.fixed;
       }

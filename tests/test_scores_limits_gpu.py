@@ -138,3 +138,22 @@ def test_other_integer_types_and_tensors_are_refused_or_understood():
         B.samkv_prefill_scores(h, p, x, x[:, :1], x[:, :1], 0.0, B.Scores(slopes=torch.zeros(3, device=DEV)), torch.zeros_like(x))
     with pytest.raises(ValueError):
         B.samkv_prefill_scores(h, p, x.float(), x[:, :1], x[:, :1], 0.0, None, torch.zeros_like(x))
+
+
+@pytest.mark.parametrize("dtype,n", [("bf16", 10500), ("f32", 5300)])
+def test_plans_of_many_row_tiles(dtype, n):
+    """Hundreds of row tiles with documents: the plan kernel goes through their tokens with several lanes each."""
+    Hq, Hkv, d = 8, 2, 64
+    q, k, v = (randn(n + 7, h, d, dtype=dtype, seed=i + 250) for i, h in enumerate((Hq, Hkv, Hkv)))
+    r = np.random.default_rng(5)
+    lens = [3, n - 3]
+    p = np.concatenate([np.arange(x) for x in lens])
+    doc = p // 777 * 777
+    doc[n - 900:] = r.integers(-5, n, 900)                    # some tokens see nothing of their own
+    mods = Mods(softcap=8.0, prefix=[1, 20], doc=np.concatenate([doc, np.zeros(7, dtype=np.int64)]))
+    O, lse = prompt(q, k, v, lens, dtype, mods)
+    rows = np.unique(np.concatenate([[0, 1, 776, 777, 778, 5000, n - 4, n - 904], r.integers(0, n - 3, 24), n - 4 - r.integers(0, 900, 16)]))
+    ok = mods.seen(1, 3, 0, n - 3, n - 3)[rows]
+    ref = attend64(f64(q)[3 + rows], f64(k)[3:n].swapaxes(0, 1), f64(v)[3:n].swapaxes(0, 1), ok, rows, mods, d ** -0.5)
+    check(f64(O)[3 + rows], f64(lse)[3 + rows], ref, dtype, n)
+    assert bool((O[n:] == 7.0).all())
