@@ -121,7 +121,10 @@ packed_decode_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
   __syncthreads();
   pdl_wait();
   long long chunk = 0;
-  if constexpr (!kMod) {
+  ScorePlan tiles = {};
+  if constexpr (kMod) {
+    tiles = plan_of_block<kThreads>(p.seqs, p.mods, p.cfg, p.plan, smem_raw + L::kO, p.d_status);
+  } else {
     if (p.seqs.n_seq > kWarpPlanSeqs) plan_block<kThreads>(p.seqs, p.cfg, &plan, &chunk, p.d_status, tid);
   }
   // tile that is taken i-th: with slopes from the last to the first, where the scores are highest
@@ -144,7 +147,7 @@ packed_decode_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
   if (warp == kConsumers) {
     // ================= producer: plan, Q, K and V =================
     std::conditional_t<kMod, PieceWindow, Walker> w;
-    if constexpr (kMod) w.begin(p.seqs, p.mods, p.cfg, p.plan, true, p.d_status);
+    if constexpr (kMod) w.begin(p.seqs, p.mods, p.cfg, tiles, true, p.d_status);
     else w.begin(p.seqs, p.cfg, &plan, chunk, p.d_status);
     __syncwarp();
     P pc;
@@ -154,7 +157,7 @@ packed_decode_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
       bool have = *s_fail == 0;
       int from = 0;                                       // the lane that has the piece
       if constexpr (kMod) {
-        from = have ? w.take(p.seqs, p.mods, p.cfg, p.plan, true, p.d_status) : -1;
+        from = have ? w.take(p.seqs, p.mods, p.cfg, tiles, true, p.d_status) : -1;
         from = __shfl_sync(0xffffffffu, from, 0);
         have = from >= 0;
       } else {

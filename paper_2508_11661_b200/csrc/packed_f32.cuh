@@ -102,8 +102,10 @@ packed_f32_kernel(const __grid_constant__ pf32::Params p) {
   long long chunk = 0;
   std::conditional_t<kMod, PieceWindow, Walker> w;
   w.more = false;
+  ScorePlan tiles = {};
   if constexpr (kMod) {
-    if (warp == 0) w.begin(p.seqs, p.mods, p.cfg, p.plan, kPaged, p.d_status);
+    tiles = plan_of_block<kThreads>(p.seqs, p.mods, p.cfg, p.plan, smem_raw + L::kKv, p.d_status);
+    if (warp == 0) w.begin(p.seqs, p.mods, p.cfg, tiles, kPaged, p.d_status);
   } else {
     if (p.seqs.n_seq > kWarpPlanSeqs) plan_block<kThreads>(p.seqs, p.cfg, &plan, &chunk, p.d_status, tid);
     if (warp == 0) w.begin(p.seqs, p.cfg, &plan, chunk, p.d_status);
@@ -111,7 +113,7 @@ packed_f32_kernel(const __grid_constant__ pf32::Params p) {
   bool bad = false;
   auto next_piece = [&](int at) {
     if constexpr (kMod) {
-      const int from = w.take(p.seqs, p.mods, p.cfg, p.plan, kPaged, p.d_status);
+      const int from = w.take(p.seqs, p.mods, p.cfg, tiles, kPaged, p.d_status);
       if (lane == from) s_piece[at] = w.mine;
       if (from < 0 && lane == 0) s_piece[at].tile0 = -1;
     } else {

@@ -6,9 +6,10 @@
 // its warps works its pieces out 32 at a time, a piece per lane; borders, workspace slots and tickets are those of packed_plan.cuh.
 // (Walking from piece to piece as there, with the records in registers, made a call on 20 documents 4 % slower: the warp that
 // does it also has the key tiles to load.)
-// The plan is a kernel of one block in front of the attention kernel.  Where a call has at most 32 row tiles by the sizes
-// the host knows, the warp makes it in its registers, a record per lane, and there is no such kernel; such calls run in waves
-// by the rules of packed_plan.cuh.
+// Who makes the plan goes by the sizes that the host knows.  Up to 32 row tiles: that warp, in its registers, a record per lane;
+// such calls run in waves by the rules of packed_plan.cuh.  Up to 256: every CTA for itself, all of its threads, in a part of
+// the workspace of its own, which takes 3 us less than a kernel in front (5 us and the step to the next kernel) although all CTAs
+// do the same.  More: a kernel of one block in front of the attention kernel.
 //
 // Token i of a row tile sees the slots below the sequence's prefix and those of [low_i, end_i): low_i is the largest of 0,
 // its document's start and the window's edge, end_i rises with i.  A row tile's key tiles are those of the prefix and those
@@ -23,6 +24,7 @@ namespace samkv {
 
 constexpr int kPlanThreads = 1024;
 constexpr int kWarpTiles = 32;                 // row tiles that one warp plans by itself
+constexpr int kBlockTiles = 256, kBlockSeqs = 1024;      // most of a call whose CTAs make their plans themselves
 
 struct alignas(16) RowTile {
   int s, r, R;                 // sequence, row tile of it, its row tiles
@@ -35,12 +37,20 @@ struct alignas(16) RowTile {
 };
 constexpr int kRowTileInts = sizeof(RowTile) / 4;
 
-// What the plan kernel leaves in the workspace.
+// A plan in the workspace.
 struct ScorePlan {
-  long long* at;               // [n_tiles + 1] lengths before each row tile (of one head)
+  long long* at;               // [n_tiles + 1] lengths before each row tile (of one head); null: a warp makes the plan
   int* n_tiles;
   RowTile* tiles;
+  long long own_bytes;         // every CTA makes a plan of its own, so far apart; 0: there is one, made before
 };
+__device__ __forceinline__ ScorePlan own_plan(ScorePlan p) {
+  const long long by = p.own_bytes * blockIdx.x;
+  p.at = reinterpret_cast<long long*>(reinterpret_cast<char*>(p.at) + by);
+  p.n_tiles = reinterpret_cast<int*>(reinterpret_cast<char*>(p.n_tiles) + by);
+  p.tiles = reinterpret_cast<RowTile*>(reinterpret_cast<char*>(p.tiles) + by);
+  return p;
+}
 
 __device__ __forceinline__ int end_of(const Seqs& q, int end0, int i) {
   return q.causal ? (int)min((unsigned)end0 + (unsigned)i, (unsigned)q.limit) : end0;
@@ -141,6 +151,116 @@ __device__ __forceinline__ void finish_row_tiles(const Seqs& q, const ScoreMods&
     t.all0 = highest;
     t.nt = tile_list(t.pre, t.any0, any1, c.tile).nt;
   }
+}
+
+template <int kThreads>
+struct PlanScratch {
+  int off[kThreads];           // row tiles of the chunk's sequences before each
+  int warp[32];
+  unsigned lo[32], hi[32];     // lengths, by halves
+  int end;
+};
+// Records and lengths of all row tiles of a call, by kThreads threads of a block; report: this block records clamped values.
+template <int kThreads>
+__device__ __forceinline__ void make_plan(const Seqs& q, const ScoreMods& m, const SplitCfg& c, const ScorePlan& plan,
+                                          PlanScratch<kThreads>& sh, bool report, int* d_status) {
+  constexpr int kWarps = kThreads / 32;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  if (tid == 0) sh.end = q.n_seq;
+  __syncthreads();
+  for (int s = tid; s < q.n_seq; s += kThreads) {
+    const Seq x = load_seq(q, s);
+    if (x.backwards) atomicMin(&sh.end, s);
+    if (x.clamped && report) atomicMax(d_status, (int)CHECK_SEQ_RANGE);
+  }
+  __syncthreads();
+  const int n_seq = sh.end;
+  int n_tiles = 0;                             // so far
+  long long total = 0;
+#pragma unroll 1
+  for (int s0 = 0; s0 < n_seq; s0 += kThreads) {
+    // row tiles of these sequences
+    int R = 0;
+    if (s0 + tid < n_seq) R = row_tiles(c, load_seq(q, s0 + tid).n);
+    int incl = R;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int v = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += v;
+    }
+    __syncthreads();
+    if (lane == 31) sh.warp[warp] = incl;
+    __syncthreads();
+    int w = (lane < kWarps ? sh.warp[lane] : 0);
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int v = __shfl_up_sync(0xffffffffu, w, o);
+      if (lane >= o) w += v;
+    }
+    const int chunk = __shfl_sync(0xffffffffu, w, 31);
+    const int before = __shfl_sync(0xffffffffu, w, (warp + 31) & 31);
+    sh.off[tid] = (warp > 0 ? before : 0) + incl - R;
+    __syncthreads();
+    const int count = min(kThreads, n_seq - s0);
+    // their records, and the lengths
+#pragma unroll 1
+    for (int i0 = 0; i0 < chunk; i0 += kThreads) {
+      const int i = i0 + tid;
+      long long len = 0;
+      RowTile t = {};
+      if (i < chunk) {
+        int lo = 0, hi = count - 1;            // last sequence that starts at or before i: the one that owns it
+        while (lo < hi) {
+          const int mid = (lo + hi + 1) >> 1;
+          if (sh.off[mid] <= i) lo = mid; else hi = mid - 1;
+        }
+        t = make_row_tile(q, m, c, s0 + lo, load_seq(q, s0 + lo), i - sh.off[lo]);
+      }
+      if (chunk > 256 && c.tokens > 8) finish_row_tiles<true>(q, m, c, i < chunk, t);
+      else finish_row_tiles<false>(q, m, c, i < chunk, t);
+      if (i < chunk) {
+        plan.tiles[n_tiles + i] = t;
+        len = (long long)t.nt * c.tile + c.fixed;
+      }
+      long long li = len;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const long long v = __shfl_up_sync(0xffffffffu, li, o);
+        if (lane >= o) li += v;
+      }
+      __syncthreads();
+      if (lane == 31) {
+        sh.lo[warp] = (unsigned)li;
+        sh.hi[warp] = (unsigned)(li >> 32);
+      }
+      __syncthreads();
+      long long wl = lane < kWarps ? (long long)((unsigned long long)sh.hi[lane] << 32 | sh.lo[lane]) : 0;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const long long v = __shfl_up_sync(0xffffffffu, wl, o);
+        if (lane >= o) wl += v;
+      }
+      const long long all = __shfl_sync(0xffffffffu, wl, 31);
+      const long long bw = __shfl_sync(0xffffffffu, wl, (warp + 31) & 31);
+      if (i < chunk) plan.at[n_tiles + i] = total + (warp > 0 ? bw : 0) + li - len;
+      total += all;
+    }
+    n_tiles += chunk;
+  }
+  if (tid == 0) {
+    plan.at[n_tiles] = total;
+    *plan.n_tiles = n_tiles;
+  }
+}
+// In front of the roles of an attention kernel, by all of its threads: the plan of a call whose CTAs make their own.
+template <int kThreads>
+__device__ __forceinline__ ScorePlan plan_of_block(const Seqs& q, const ScoreMods& m, const SplitCfg& c, const ScorePlan& plan,
+                                                   void* scratch, int* d_status) {
+  if (plan.own_bytes == 0) return plan;
+  const ScorePlan own = own_plan(plan);
+  make_plan<kThreads>(q, m, c, own, *static_cast<PlanScratch<kThreads>*>(scratch), blockIdx.x == 0, d_status);
+  __syncthreads();
+  return own;
 }
 
 // A piece of a masked item, as the kernels hand it around (14 words: shared memory is full).
@@ -461,8 +581,8 @@ inline long long most_row_tiles(const samkv_packed_t& p, int tokens) {
   const long long a = p.n_tokens, b = ((long long)p.n_tokens + (long long)p.n_seq * (tokens - 1)) / tokens;
   return a < b ? a : b;
 }
-inline size_t score_plan_bytes(long long tiles) { return 256 + (size_t)tiles * (sizeof(RowTile) + 8) + 16; }
-// Lays a call out: its plan's place in the workspace (null where the warps make it themselves); enqueues the plan's kernel.
+inline size_t plan_bytes(long long tiles) { return ((size_t)tiles * (sizeof(RowTile) + 8) + 16 + 255) & ~(size_t)255; }
+// Where the plan of a call lies, and who makes it; enqueues the plan's kernel where there is one.
 cudaError_t make_score_plan(const samkv_packed_t& p, const Seqs& seqs, const ScoreMods& mods, const SplitCfg& cfg,
                             const samkv_ctx_impl& h, ScorePlan* plan, cudaStream_t stream);
 

@@ -382,7 +382,10 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
   const uint32_t tmem = *s_tmem;
   pdl_wait();                               // everything below reads what earlier kernels may have written
   long long chunk = 0;
-  if constexpr (!kAny) {
+  ScorePlan tiles = {};
+  if constexpr (kAny) {
+    tiles = plan_of_block<kThreads>(p.seqs, p.mods, p.cfg, p.plan, smem_raw + L::kK, p.d_status);
+  } else {
     if (p.seqs.n_seq > kWarpPlanSeqs) plan_block<kThreads>(p.seqs, p.cfg, &plan, &chunk, p.d_status, tid);
   }
 
@@ -394,12 +397,12 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
       // ================= plan and K =================
       std::conditional_t<kAny, PieceWindow, Walker> w;
       if constexpr (kAny) {
-        w.begin(p.seqs, p.mods, p.cfg, p.plan, kPaged, p.d_status);
+        w.begin(p.seqs, p.mods, p.cfg, tiles, kPaged, p.d_status);
       } else {
         w.begin(p.seqs, p.cfg, &plan, chunk, p.d_status);
-        __syncwarp();
-        fence_proxy_async();                // the plan's memory becomes the destination of copies
       }
+      __syncwarp();
+      fence_proxy_async();                  // the plan's memory becomes the destination of copies
       __syncwarp();
       P pc;
       uint32_t f = 0, T = 0;                // pieces, key tiles so far
@@ -407,7 +410,7 @@ packed_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
       while (true) {
         int from = 0;                       // the lane that has the piece, -1: no more
         if constexpr (kAny) {
-          from = *s_fail == 0 ? w.take(p.seqs, p.mods, p.cfg, p.plan, kPaged, p.d_status) : -1;
+          from = *s_fail == 0 ? w.take(p.seqs, p.mods, p.cfg, tiles, kPaged, p.d_status) : -1;
           from = __shfl_sync(0xffffffffu, from, 0);
         } else {
           if (!(*s_fail == 0 && w.next(p.seqs, p.cfg, &pc))) from = -1;
