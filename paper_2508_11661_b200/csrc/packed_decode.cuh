@@ -12,6 +12,9 @@
 // 32 requests over 20480 slots, 32/8 heads of 128: 0.405 ms, 6.63 TB/s, the rate of a plain copy (1.03 of the measured
 // one); one request over 102400 slots, 64/8 heads: 78 us, 5.4 TB/s (start-up, the ring's first fill and the merge of 19
 // pieces per KV head are about 12 us of it).  The tensor-memory kernel takes 0.42-0.43 ms and 155 us for the same calls.
+// Modified scores (kMod; see packed_scores.cuh) change a warp's 16 x 16 scores in registers, one kernel for all kinds: all slots
+// of the 32 requests capped 0.40 ms as well; a window of 4096 behind a prefix of 64 0.10 ms (5.3 TB/s: start-up and 2.7 ends of pieces
+// per CTA); 102400 slots with slopes 78 us.
 // Every wait is bounded; a wait that runs out ends the others and is recorded as a device check.
 #pragma once
 

@@ -16,6 +16,8 @@
 // an item costs about 2 us besides its tiles (a third until its first tile is there, 0.5 us to join the warps' results);
 // 6 sequences of 1 to 64 tokens, 4/2 heads of 64: 16 us (22 us with 16 rows).  Starting the next item's loads before the
 // results leave made every shape 4 to 8 % slower (the code grew), so it is not done.
+// Modified scores (kMod; see packed_scores.cuh): 4 documents of 256 tokens and a question of 32 in one sequence, slopes, 4/2 heads of 64:
+// 33 us; 4 prompts of 256 with a window 25 us (21 us plain: the plan, and partly seen tiles slot by slot).
 #pragma once
 
 #include <math.h>
