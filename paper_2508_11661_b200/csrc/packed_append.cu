@@ -4,6 +4,8 @@
 // reduction of far positions costs one integer multiplication and loses nothing.  The top two bits are the quadrant,
 // the rest an angle in [-1/8, 1/8] turns whose fp32 sine and cosine are good to an ulp.  Sines and cosines of a token
 // are formed once per CTA in shared memory and shared by all its heads.
+// Bound by HBM: 20480 tokens, 32/8 heads of 128: 85 us (a copy of the same bytes 83), with three axes and a slot map 88 us.  A
+// thread's first two items are fetched before the positions are looked up (92 and 99 us without; 3 items 93, 4 97, 6 110).
 #include "packed.cuh"
 
 namespace samkv {
