@@ -27,12 +27,18 @@ bool five(Py_ssize_t n) {
   return n == 5;
 }
 
+// Asking a tensor may throw (one without storage, inside a function transform, has no address); an exception that leaves a C
+// function would end the process, so it counts as "not as it should be", and the Python form raises its own.
+
 // Address of a contiguous tensor, None for None.
 PyObject* device_ptr(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (!five(n)) return nullptr;
   if (a[0] == Py_None) Py_RETURN_NONE;
-  const at::Tensor* x = as_wanted(a[0], a[2], a[3], a[4]);
-  if (x != nullptr && x->is_contiguous()) return PyLong_FromVoidPtr(x->data_ptr());
+  try {
+    const at::Tensor* x = as_wanted(a[0], a[2], a[3], a[4]);
+    if (x != nullptr && x->is_contiguous()) return PyLong_FromVoidPtr(x->data_ptr());
+  } catch (...) {
+  }
   PyErr_Clear();
   return PyObject_Vectorcall(g_device_ptr, a, 5, nullptr);
 }
@@ -40,9 +46,14 @@ PyObject* device_ptr(PyObject*, PyObject* const* a, Py_ssize_t n) {
 // (address, token stride, head stride) of a tensor of three dimensions whose last one is contiguous.
 PyObject* rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (!five(n)) return nullptr;
-  const at::Tensor* x = as_wanted(a[0], a[2], a[3], a[4]);
-  if (x != nullptr && x->dim() == 3 && x->stride(2) == 1)
-    return Py_BuildValue("(NLL)", PyLong_FromVoidPtr(x->data_ptr()), (long long)x->stride(0), (long long)x->stride(1));
+  try {
+    const at::Tensor* x = as_wanted(a[0], a[2], a[3], a[4]);
+    if (x != nullptr && x->dim() == 3 && x->stride(2) == 1) {
+      void* data = x->data_ptr();
+      return Py_BuildValue("(NLL)", PyLong_FromVoidPtr(data), (long long)x->stride(0), (long long)x->stride(1));
+    }
+  } catch (...) {
+  }
   PyErr_Clear();
   return PyObject_Vectorcall(g_rows, a, 5, nullptr);
 }
