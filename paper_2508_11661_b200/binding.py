@@ -466,7 +466,7 @@ def _rows(t: torch.Tensor, what: str, dtype: torch.dtype, shape: tuple, device: 
 
 
 def _call(name: str, *args) -> int:
-    """Status of a packed call: integers, None, one float, descriptions (ctypes structures), packed tensors (what _rows says)."""
+    """Status of a packed call: integers, None, floats, descriptions (ctypes structures), packed tensors (what _rows says)."""
     return getattr(lib(), name)(*[samkv_rows_t(*a) if type(a) is tuple else a for a in args])
 
 
@@ -476,7 +476,7 @@ try:        # the same without Python's and ctypes' overhead, where build.py has
     _device_ptr, _rows = _marshal.device_ptr, _marshal.rows
 
     def _call(name: str, *args) -> int:  # noqa: F811
-        return _marshal.call(_addresses.get(name) or _address(name), *args)
+        return getattr(_marshal, name)(_addresses.get(name) or _address(name), *args)
 except ImportError:
     pass
 

@@ -29,12 +29,13 @@ def build_marshal(force: bool = False) -> str:
 
     import torch
     src = os.path.join(CSRC, "marshal.cpp")
-    if not force and os.path.exists(MARSHAL_PATH) and os.path.getmtime(MARSHAL_PATH) >= os.path.getmtime(src):
+    newest = max(os.path.getmtime(f) for f in (src, os.path.join(ROOT, "include", "samkv.h")))
+    if not force and os.path.exists(MARSHAL_PATH) and os.path.getmtime(MARSHAL_PATH) >= newest:
         return MARSHAL_PATH
     t = os.path.dirname(torch.__file__)
     subprocess.check_call(["g++", "-O2", "-std=c++17", "-shared", "-fPIC",
                            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
-                           "-I", sysconfig.get_paths()["include"], "-I", os.path.join(t, "include"),
+                           "-I", os.path.join(ROOT, "include"), "-I", sysconfig.get_paths()["include"], "-I", os.path.join(t, "include"),
                            "-I", os.path.join(t, "include", "torch", "csrc", "api", "include"), src, "-o", MARSHAL_PATH,
                            "-L", os.path.join(t, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10",
                            f"-Wl,-rpath,{os.path.join(t, 'lib')}"])

@@ -5,6 +5,11 @@
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/Dtype.h>
 
+#include <tuple>
+#include <utility>
+
+#include "samkv.h"
+
 namespace {
 
 PyObject* g_device_ptr = nullptr;    // the Python forms
@@ -71,91 +76,142 @@ PyObject* otherwise(PyObject*, PyObject* const* a, Py_ssize_t n) {
   Py_RETURN_NONE;
 }
 
-// Arguments of a call that are not numbers: descriptions (ctypes structures, by their memory) and packed tensors (tuples made by
-// `rows`).
-struct Rows {
-  void* data;
-  int64_t token_stride, head_stride;
-};
-constexpr int kMostArgs = 16;
-struct Args {
-  long value[kMostArgs] = {};
-  Rows rows[kMostArgs];
-  Py_buffer buffers[kMostArgs];
-  int n_buffers = 0;
-  float scale = 0.f;           // the one argument of the library's packed calls that is no integer
-  int n = 0;
-  ~Args() {
-    for (int i = 0; i < n_buffers; ++i) PyBuffer_Release(&buffers[i]);
+// A Python value as a parameter of type T; take() says what is wrong by a Python exception.
+bool not_a(const char* what) {
+  PyErr_Format(PyExc_TypeError, "call: expected %s", what);
+  return false;
+}
+template <typename T>
+struct Arg;
+// Integers: int, bool and what has __index__ (numpy's), but no float.
+template <typename T>
+struct Integer {
+  T v = 0;
+  T get() const { return v; }
+  bool take(PyObject* x) {
+    if (!PyIndex_Check(x)) return not_a("an integer");
+    PyObject* whole = PyNumber_Index(x);
+    if (whole == nullptr) return false;
+    const long long wide = PyLong_AsLongLong(whole);
+    Py_DECREF(whole);
+    if (wide == -1 && PyErr_Occurred()) return false;
+    v = static_cast<T>(wide);
+    if (v == wide) return true;
+    PyErr_SetString(PyExc_OverflowError, "call: an integer has more than 32 bits");
+    return false;
   }
-  bool add(PyObject* x) {
-    if (PyFloat_Check(x)) {
-      scale = static_cast<float>(PyFloat_AS_DOUBLE(x));
-      return true;
-    }
-    if (n == kMostArgs) {
-      PyErr_SetString(PyExc_TypeError, "call: too many arguments");
-      return false;
-    }
-    long& v = value[n];
-    if (x == Py_None) {
-      v = 0;
-    } else if (PyLong_Check(x)) {
-      v = static_cast<long>(PyLong_AsUnsignedLongLongMask(x));
-      if (PyErr_Occurred()) return false;
-    } else if (PyIndex_Check(x)) {           // numpy's integers, which are buffers as well
-      PyObject* whole = PyNumber_Index(x);
-      if (whole == nullptr) return false;
-      v = static_cast<long>(PyLong_AsUnsignedLongLongMask(whole));
-      Py_DECREF(whole);
-      if (PyErr_Occurred()) return false;
-    } else if (PyTuple_Check(x)) {
-      Rows& r = rows[n];
-      long long ts, hs;
-      PyObject* p;
-      if (!PyArg_ParseTuple(x, "OLL", &p, &ts, &hs)) return false;
-      r.data = PyLong_AsVoidPtr(p);
-      r.token_stride = ts;
-      r.head_stride = hs;
-      if (PyErr_Occurred()) return false;
-      v = reinterpret_cast<long>(&r);
-    } else {
-      if (PyObject_GetBuffer(x, &buffers[n_buffers], PyBUF_SIMPLE) != 0) return false;
-      v = reinterpret_cast<long>(buffers[n_buffers++].buf);
-    }
-    ++n;
+};
+template <>
+struct Arg<int32_t> : Integer<int32_t> {};
+template <>
+struct Arg<int64_t> : Integer<int64_t> {};
+template <>
+struct Arg<float> {
+  float v = 0.f;
+  float get() const { return v; }
+  bool take(PyObject* x) {
+    if (!PyFloat_Check(x)) return not_a("a float");
+    v = static_cast<float>(PyFloat_AS_DOUBLE(x));
     return true;
   }
 };
-
-// call(address, arguments ...): the status of a library function whose arguments are integers, pointers and at most one float.
-// Integers and floats travel in registers of their own on x86-64, integers behind the sixth on the stack in their order, and
-// arguments that a function does not look at do no harm, so that one function type serves all of them.
-PyObject* call(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  if (n < 1 || !PyLong_Check(a[0])) {
-    PyErr_SetString(PyExc_TypeError, "call: expected an address and arguments");
-    return nullptr;
+// Memory of the device, streams and handles: their address, None for null.
+template <typename T>
+struct Arg<T*> {
+  void* v = nullptr;
+  T* get() const { return static_cast<T*>(v); }
+  bool take(PyObject* x) {
+    if (x == Py_None) return true;
+    if (!PyLong_Check(x)) return not_a("an address");
+    v = PyLong_AsVoidPtr(x);
+    return v != nullptr || !PyErr_Occurred();
   }
-  Args args;
-  for (Py_ssize_t i = 1; i < n; ++i)
-    if (!args.add(a[i])) return nullptr;
-  using Fn = int (*)(float, long, long, long, long, long, long, long, long, long, long, long, long, long, long, long, long);
-  const Fn f = reinterpret_cast<Fn>(PyLong_AsVoidPtr(a[0]));
-  const long* v = args.value;
-  int status;
-  Py_BEGIN_ALLOW_THREADS;
-  status = f(args.scale, v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7], v[8], v[9], v[10], v[11], v[12], v[13], v[14], v[15]);
-  Py_END_ALLOW_THREADS;
-  return PyLong_FromLong(status);
-}
+};
+// Packed tensors: what `rows` makes.
+template <>
+struct Arg<const samkv_rows_t*> {
+  samkv_rows_t v = {};
+  bool given = false;
+  const samkv_rows_t* get() const { return given ? &v : nullptr; }
+  bool take(PyObject* x) {
+    if (x == Py_None) return true;
+    if (!PyTuple_Check(x) || PyTuple_GET_SIZE(x) != 3) return not_a("a packed tensor");
+    Arg<void*> data;
+    Arg<int64_t> token, head;
+    if (!data.take(PyTuple_GET_ITEM(x, 0)) || !token.take(PyTuple_GET_ITEM(x, 1)) || !head.take(PyTuple_GET_ITEM(x, 2))) return false;
+    v.data = data.v;
+    v.token_stride = token.v;
+    v.head_stride = head.v;
+    given = true;
+    return true;
+  }
+};
+// Descriptions: ctypes structures of the same size, by their memory.
+template <typename S>
+struct Description {
+  Py_buffer b = {};
+  Description() = default;
+  Description(const Description&) = delete;
+  ~Description() { PyBuffer_Release(&b); }     // (nothing to do where there is none)
+  const S* get() const { return static_cast<const S*>(b.buf); }
+  bool take(PyObject* x) {
+    if (x == Py_None) return true;
+    if (PyObject_GetBuffer(x, &b, PyBUF_SIMPLE) != 0) return false;
+    return b.len == sizeof(S) || not_a("another description");
+  }
+};
+template <>
+struct Arg<const samkv_packed_t*> : Description<samkv_packed_t> {};
+template <>
+struct Arg<const samkv_pages_t*> : Description<samkv_pages_t> {};
+template <>
+struct Arg<const samkv_rope_t*> : Description<samkv_rope_t> {};
+template <>
+struct Arg<const samkv_rope_axes_t*> : Description<samkv_rope_axes_t> {};
+template <>
+struct Arg<const samkv_scores_t*> : Description<samkv_scores_t> {};
+
+// name(address, arguments ...): the status of the library function at that address, whose type is that of the header's
+// declaration, so that every argument has its place and its type.
+template <typename F>
+struct Call;
+template <typename... T>
+struct Call<samkv_status_t (*)(T...)> {
+  template <size_t... I>
+  static PyObject* with(samkv_status_t (*f)(T...), PyObject* const* a, std::index_sequence<I...>) {
+    std::tuple<Arg<T>...> args;
+    if (!(std::get<I>(args).take(a[I]) && ...)) return nullptr;
+    int status;
+    Py_BEGIN_ALLOW_THREADS;
+    status = f(std::get<I>(args).get()...);
+    Py_END_ALLOW_THREADS;
+    return PyLong_FromLong(status);
+  }
+  static PyObject* call(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (n != 1 + (Py_ssize_t)sizeof...(T) || !PyLong_Check(a[0]))
+      return not_a("an address and the library function's arguments"), nullptr;
+    void* f = PyLong_AsVoidPtr(a[0]);
+    if (f == nullptr) return PyErr_Occurred() || not_a("an address"), nullptr;
+    return with(reinterpret_cast<samkv_status_t (*)(T...)>(f), a + 1, std::index_sequence_for<T...>{});
+  }
+};
 
 PyCFunction fast(PyObject* (*f)(PyObject*, PyObject* const*, Py_ssize_t)) {
   return reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f));
 }
 PyMethodDef kMethods[] = {{"device_ptr", fast(device_ptr), METH_FASTCALL, nullptr},
                           {"rows", fast(rows), METH_FASTCALL, nullptr},
-                          {"call", fast(call), METH_FASTCALL, nullptr},
                           {"otherwise", fast(otherwise), METH_FASTCALL, nullptr},
+#define SAMKV_CALL(name) {#name, fast(Call<decltype(&name)>::call), METH_FASTCALL, nullptr}
+                          SAMKV_CALL(samkv_prefill),
+                          SAMKV_CALL(samkv_append),
+                          SAMKV_CALL(samkv_paged_attn),
+                          SAMKV_CALL(samkv_page_tables),
+                          SAMKV_CALL(samkv_release_pages),
+                          SAMKV_CALL(samkv_append_axes),
+                          SAMKV_CALL(samkv_prefill_scores),
+                          SAMKV_CALL(samkv_paged_attn_scores),
+#undef SAMKV_CALL
                           {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 

@@ -82,3 +82,84 @@ with FakeTensorMode():
     fake = torch.zeros(T, Hq, d)
 assert outcome(B.samkv_prefill, handle, packed, fake, K, V, 0.0, O, lse) not in ("OK", "SAMKV_ERR_CUDA")
 """, module)
+
+
+@no_gpu
+@both
+def test_arguments_of_other_types(module):
+    """A number that is no integer, or nothing that could be meant, is refused before the library sees any argument."""
+    run("""
+free, n_free, n_out, table = i32(16), i32(1), i32(1), i32(2, 3)
+lengths, done = i32(2), torch.zeros(2, dtype=torch.bool)
+def tables(page_size, scale=0.0):
+    return outcome(B.samkv_page_tables, handle, packed, None, page_size, table, free, n_free, n_out)
+def release(page_size):
+    return outcome(B.samkv_release_pages, handle, table, page_size, lengths, done, free, n_free, n_out)
+for f in (tables, release):
+    for good in (16, np.int64(16), np.int32(16)):
+        assert f(good) == "SAMKV_ERR_CUDA" or (not MODULE and type(good) is not int), (f, good)
+    assert f(17) == "SAMKV_ERR_UNSUPPORTED"
+    for bad in (16.0, np.float32(16.0), 2.5, "16", b"16", (16, 0, 0), packed.c, [16], 16j):
+        assert f(bad) in ("TypeError", "ArgumentError"), (f, bad, f(bad))
+assert outcome(B.samkv_prefill, handle, packed, Q, K, V, 1, O) == "SAMKV_ERR_CUDA"           # scale: any real number
+assert outcome(B.samkv_prefill, handle, packed, Q, K, V, "1", O) in ("ValueError", "TypeError", "SAMKV_ERR_CUDA")
+assert outcome(B.samkv_prefill, handle, packed, Q, K, V, [1], O) == "TypeError"
+""", module)
+
+
+def test_every_argument_arrives_in_its_place():
+    """Each packed call of the extension module against a function that writes down what it gets."""
+    run("""
+NAMES = [n for n in dir(B._marshal) if n.startswith("samkv_")]
+assert set(NAMES) == {n for n in B.EXPORTS if n in (
+    "samkv_prefill", "samkv_append", "samkv_paged_attn", "samkv_page_tables", "samkv_release_pages", "samkv_append_axes",
+    "samkv_prefill_scores", "samkv_paged_attn_scores")}, NAMES
+for name in NAMES:
+    types = getattr(B.lib(), name).argtypes
+    got = []
+    def note(*args):
+        got[:] = [a if not isinstance(a, ctypes._Pointer) else bytes(a.contents) if a else None for a in args]
+        return 5
+    callback = ctypes.CFUNCTYPE(ctypes.c_int, *types)(note)
+    address, call = ctypes.cast(callback, ctypes.c_void_p).value, getattr(B._marshal, name)
+    args, want = [], []
+    for i, t in enumerate(types):
+        if t is ctypes.c_float:
+            args.append(0.5 + i)
+            want.append(0.5 + i)
+        elif t is ctypes.POINTER(B.samkv_rows_t):
+            args.append((4096 + i, 100 + i, 200 + i))
+            want.append(bytes(B.samkv_rows_t(*args[-1])))
+        elif hasattr(t, "contents"):
+            s = t._type_()
+            ctypes.memset(ctypes.byref(s), i + 1, ctypes.sizeof(s))
+            args.append(s)
+            want.append(bytes(s))
+        elif t is ctypes.c_void_p:
+            args.append((1 << 40) + i)
+            want.append((1 << 40) + i)
+        else:
+            args.append((1 << 35) + i if t is ctypes.c_int64 else -1000 - i)
+            want.append(args[-1])
+    assert call(address, *args) == 5 and got == want, (name, got, want)
+    # None is a null pointer, and nothing else
+    for i, t in enumerate(types):
+        now = list(args)
+        now[i] = None
+        if t in (ctypes.c_float, ctypes.c_int32, ctypes.c_int64):
+            assert outcome(call, address, *now) == "TypeError", (name, i)
+        else:
+            assert call(address, *now) == 5 and got == want[:i] + [None] + want[i + 1:], (name, i)
+        # what belongs elsewhere
+        for bad in (2.5, 7, (1, 2, 3), (1, 2), b"x", memory.numpy(), ctypes.c_int32(3), "3"):
+            now[i] = bad
+            fits = (t is ctypes.c_float and type(bad) is float) or (t is ctypes.POINTER(B.samkv_rows_t) and bad == (1, 2, 3)) if not hasattr(bad, "shape") else False
+            fits = fits or (type(bad) is int and t in (ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64))
+            assert (outcome(call, address, *now) == "OK") == fits, (name, i, t, bad)
+    for wrong in (args[:-1], args + [0], []):
+        assert outcome(call, address, *wrong) == "TypeError"
+    assert outcome(call) == "TypeError" and outcome(call, 1.0, *args) == "TypeError" and outcome(call, 0, *args) == "TypeError"
+    for i, t in enumerate(types):
+        if t is ctypes.c_int32:
+            assert outcome(call, address, *args[:i], 1 << 32, *args[i + 1:]) == "OverflowError"
+""", True)
