@@ -470,8 +470,10 @@ def _call(name: str, *args) -> int:
     return getattr(lib(), name)(*[samkv_rows_t(*a) if type(a) is tuple else a for a in args])
 
 
-try:        # the same without Python's and ctypes' overhead, where build.py has built it
+try:        # the same without Python's and ctypes' overhead, where build.py has built it for this torch
     from . import _marshal
+    if getattr(_marshal, "torch_version", None) != torch.__version__:
+        raise ImportError("_marshal was built for another torch")
     _marshal.otherwise(_device_ptr, _rows)
     _device_ptr, _rows = _marshal.device_ptr, _marshal.rows
 

@@ -5,13 +5,15 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
+import warnings
 
 PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG_DIR)
 CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "libsamkv.so")
 DEBUG_LIB_PATH = os.path.join(PKG_DIR, "libsamkv_debug.so")   # same sources with -DSAMKV_DEBUG_CHECKS (test hooks)
-MARSHAL_PATH = os.path.join(PKG_DIR, "_marshal.so")
+MARSHAL_PATH = os.path.join(PKG_DIR, "_marshal" + sysconfig.get_config_var("EXT_SUFFIX"))   # (names the interpreter it is for)
 SOURCES = ["api.cu", "score.cu", "score_static.cu", "select.cu", "topp.cu", "align.cu", "means.cu", "compact.cu", "attn.cu", "attn_mma.cu", "attn_tc2.cu", "attn_tc3.cu", "attn_tc4.cu",
            "packed_api.cu", "packed_append.cu", "packed_pages.cu", "packed_scores.cu", "packed_attn.cu", "packed_tc.cu", "packed_tc_mask.cu", "packed_tc_cap.cu", "packed_tc_bias.cu", "packed_score_plan.cu", "packed_decode.cu", "packed_decode_scores.cu", "packed_f32.cu", "packed_f32_scores.cu"]
 
@@ -24,22 +26,43 @@ def nvcc_path() -> str:
 
 
 def build_marshal(force: bool = False) -> str:
-    """The binding's argument checks (csrc/marshal.cpp) as an extension module next to it."""
-    import sysconfig
-
+    """The binding's argument checks (csrc/marshal.cpp) as an extension module next to it, for this interpreter and this torch
+    (a file beside it says for which; the binding looks, too)."""
     import torch
     src = os.path.join(CSRC, "marshal.cpp")
     newest = max(os.path.getmtime(f) for f in (src, os.path.join(ROOT, "include", "samkv.h")))
-    if not force and os.path.exists(MARSHAL_PATH) and os.path.getmtime(MARSHAL_PATH) >= newest:
-        return MARSHAL_PATH
-    t = os.path.dirname(torch.__file__)
-    subprocess.check_call(["g++", "-O2", "-std=c++17", "-shared", "-fPIC",
-                           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
-                           "-I", os.path.join(ROOT, "include"), "-I", sysconfig.get_paths()["include"], "-I", os.path.join(t, "include"),
-                           "-I", os.path.join(t, "include", "torch", "csrc", "api", "include"), src, "-o", MARSHAL_PATH,
-                           "-L", os.path.join(t, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10",
-                           f"-Wl,-rpath,{os.path.join(t, 'lib')}"])
+    made_for = MARSHAL_PATH + ".torch"
+    if not force and os.path.exists(MARSHAL_PATH) and os.path.exists(made_for) and os.path.getmtime(MARSHAL_PATH) >= newest:
+        with open(made_for) as f:
+            if f.read() == torch.__version__:
+                return MARSHAL_PATH
+    for old in (MARSHAL_PATH, made_for):                 # one that does not fit must not stay where a build fails
+        if os.path.exists(old):
+            os.remove(old)
+    t, part = os.path.dirname(torch.__file__), f"{MARSHAL_PATH}.{os.getpid()}"
+    try:
+        subprocess.check_call(["g++", "-O2", "-std=c++17", "-shared", "-fPIC",
+                               f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+                               f'-DSAMKV_TORCH_VERSION="{torch.__version__}"',
+                               "-I", os.path.join(ROOT, "include"), "-I", sysconfig.get_paths()["include"],
+                               "-I", os.path.join(t, "include"), "-I", os.path.join(t, "include", "torch", "csrc", "api", "include"),
+                               src, "-o", part, "-L", os.path.join(t, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10",
+                               f"-Wl,-rpath,{os.path.join(t, 'lib')}"])
+        os.replace(part, MARSHAL_PATH)
+    finally:
+        if os.path.exists(part):
+            os.remove(part)
+    with open(made_for, "w") as f:
+        f.write(torch.__version__)
     return MARSHAL_PATH
+
+
+def _optional_marshal(force: bool) -> None:
+    """The library needs no extension module, and the binding does with its Python forms where there is none."""
+    try:
+        build_marshal(force)
+    except (ImportError, OSError, subprocess.CalledProcessError) as e:
+        warnings.warn(f"the binding's extension module (_marshal) was not built, its Python forms are used: {e}", RuntimeWarning)
 
 
 def _stale(lib_path: str = LIB_PATH) -> bool:
@@ -53,7 +76,7 @@ def _stale(lib_path: str = LIB_PATH) -> bool:
 def build_library(force: bool = False, verbose: bool = False, debug: bool = False) -> str:
     """debug=True builds libsamkv_debug.so: the same library plus the hooks a test needs to make a bounded wait run out."""
     lib_path = DEBUG_LIB_PATH if debug else LIB_PATH
-    build_marshal(force)
+    _optional_marshal(force)
     if not force and not _stale(lib_path):
         return lib_path
     objs = []

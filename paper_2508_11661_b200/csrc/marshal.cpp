@@ -217,4 +217,9 @@ PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, kMethods,
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__marshal() { return PyModule_Create(&kModule); }
+PyMODINIT_FUNC PyInit__marshal() {
+  PyObject* m = PyModule_Create(&kModule);
+  // (whose tensors this code knows)
+  if (m != nullptr && PyModule_AddStringConstant(m, "torch_version", SAMKV_TORCH_VERSION) != 0) Py_CLEAR(m);
+  return m;
+}
