@@ -525,7 +525,7 @@ samkv_status_t samkv_append_axes(samkv_handle_t h, const samkv_packed_t* packed,
  * sees all of them (doc_start 0), are one sequence; the initial tokens that a sliding window keeps are a prefix, too.
  * Slots a token does not see never reach it, infinities and NaN included; a token that sees none gets O = 0, lse = -inf. */
 typedef struct {
-  float softcap;               /* >= 0, finite; 0: scores are not capped.  scale / softcap must be finite */
+  float softcap;               /* 0: scores are not capped; else 2^-126 .. 1e30, and scale / softcap must be finite */
   int32_t window;              /* >= 0; 0: no window */
   const float* slopes;         /* device [n_q_heads], finite, any sign; NULL: none */
   const int32_t* prefix_len;   /* device [n_seq], any value (a sequence's own slots bound it); NULL: 0 */

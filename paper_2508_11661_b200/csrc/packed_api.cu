@@ -1,5 +1,6 @@
 // Entry points for packed sequences and the paged cache: argument validation and dispatch.  Arguments are checked before
 // the handle's device is, so that a refusal does not depend on the machine it is asked on.
+#include <float.h>
 #include <limits.h>
 #include <math.h>
 
@@ -225,8 +226,9 @@ samkv_status_t check_scores(const samkv_scores_t* s, const samkv_packed_t& p, fl
   if (!(s->softcap >= 0.f) || !isfinite(s->softcap) || s->window < 0) return SAMKV_ERR_INVALID_ARG;
   if (misaligned4(s->slopes) || misaligned4(s->prefix_len) || misaligned4(s->doc_start)) return SAMKV_ERR_INVALID_ARG;
   if (s->softcap > 0.f) {
+    // The kernels' factors: scale / softcap (bf16), 1 / softcap (fp32; finite from FLT_MIN on), softcap log2(e).
     const float sc = scale > 0.f ? scale : 1.0f / sqrtf((float)p.head_dim);
-    if (!isfinite(sc / s->softcap) || s->softcap > 1e30f) return SAMKV_ERR_INVALID_ARG;
+    if (!isfinite(sc / s->softcap) || s->softcap < FLT_MIN || s->softcap > 1e30f) return SAMKV_ERR_INVALID_ARG;
   }
   *out = {s->softcap, s->window > 0 ? s->window : INT_MAX, s->slopes, s->prefix_len, s->doc_start};
   *any = s->softcap > 0.f || s->window > 0 || s->slopes != nullptr || s->prefix_len != nullptr || s->doc_start != nullptr;
