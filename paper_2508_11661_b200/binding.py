@@ -8,6 +8,8 @@ has not been built, or a call returns a non-zero status, an exception is raised.
 from __future__ import annotations
 
 import ctypes
+import math
+import operator
 import os
 from typing import Optional, Sequence
 
@@ -208,6 +210,25 @@ def _stream() -> int:
 
 def _i32_array(values: Sequence[int]):
     return (ctypes.c_int32 * len(values))(*[int(v) for v in values])
+
+
+def _i32(value: int, what: str) -> int:
+    """An integer that an int32 field holds (ctypes would cut it off)."""
+    v = operator.index(value)
+    if not -2 ** 31 <= v < 2 ** 31:
+        raise OverflowError(f"{what}: {v} has more than 32 bits")
+    return v
+
+
+def _f32(value: float, what: str) -> float:
+    """A number that stays one, and stays other than 0, in a float field."""
+    if isinstance(value, (str, bytes)):                  # (float() would read it)
+        raise TypeError(f"{what}: expected a number")
+    v = float(value)
+    c = ctypes.c_float(v).value
+    if (c == 0.0 and v != 0.0) or (math.isinf(c) and not math.isinf(v)):
+        raise OverflowError(f"{what}: {v} is no fp32 number")
+    return v
 
 
 # ------------------------------------------------------------------ host helpers
@@ -662,7 +683,7 @@ class RopeAxes:
             raise ValueError("pair_axis: expected rot_dim / 2 axes")
         self._rope = Rope(rot_dim, base, interleaved, inv_freq)
         self.n_axes = max(int(a) for a in pair_axis) + 1
-        self._axis = _i32_array(pair_axis)
+        self._axis = _i32_array([_i32(int(a), "pair_axis") for a in pair_axis])
         self.c = samkv_rope_axes_t(self._rope.c, self.n_axes, ctypes.cast(self._axis, ctypes.POINTER(ctypes.c_int32)))
 
     @classmethod
@@ -707,7 +728,7 @@ class Scores:
                                (doc_start, "doc_start", torch.int32)):
             if t is not None and (t.dtype is not dtype or t.dim() != 1 or not t.is_contiguous()):
                 raise ValueError(f"{what}: expected a contiguous {dtype} tensor of one dimension")
-        self.c = samkv_scores_t(softcap, window, *(None if t is None else t.data_ptr() for t in (slopes, prefix_len, doc_start)))
+        self.c = samkv_scores_t(_f32(softcap, "softcap"), _i32(window, "window"), *(None if t is None else t.data_ptr() for t in (slopes, prefix_len, doc_start)))
 
     def checked(self, packed: Packed):
         """The description for a call with these sequences."""
