@@ -205,7 +205,8 @@ packed_decode_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_const
           page = p.pages.table[(size_t)seq_of(pc) * p.pages.width + (j >> p.pages.shift)];
           if ((unsigned)page >= (unsigned)p.pages.n_pages) {
             page = 0;
-            bad = true;
+            if constexpr (kMod) bad = bad || token_sees(p.seqs, p.mods, pc, j, j + p.box);
+            else bad = true;
           }
         }
       };

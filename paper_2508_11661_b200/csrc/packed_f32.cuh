@@ -112,7 +112,7 @@ packed_f32_kernel(const __grid_constant__ pf32::Params p) {
     if (p.seqs.n_seq > kWarpPlanSeqs) plan_block<kThreads>(p.seqs, p.cfg, &plan, &chunk, p.d_status, tid);
     if (warp == 0) w.begin(p.seqs, p.cfg, &plan, chunk, p.d_status);
   }
-  bool bad = false;
+  bool bad = false, lost = false;                        // a table entry that is no page; one that some token sees
   auto next_piece = [&](int at) {
     if constexpr (kMod) {
       const int from = w.take(p.seqs, p.mods, p.cfg, tiles, kPaged, p.d_status);
@@ -571,6 +571,18 @@ packed_f32_kernel(const __grid_constant__ pf32::Params p) {
         for (int c = 0; c < kC; ++c)
           *reinterpret_cast<ulonglong2*>(part + (ty * kR + i) * kD + c * 64 + tx * 4) = make_ulonglong2(o2[i][c * 2], o2[i][c * 2 + 1]);
     }
+    if constexpr (kMod && kPaged) {
+      if (__builtin_expect(bad, 0)) {                    // was it the entry of a page that some token sees?
+        bad = false;
+#pragma unroll 1
+        for (int i = pc.tile0 * kBN; i < pc.tile1 * kBN && !lost; ++i) {
+          const int j = slot0_of(pc, i / kBN) + i % kBN;
+          if (is_used(pc, j)) page_offset(p.pages, seq, j, head, p.cfg.Hkv, kD, &bad);
+          lost = bad && token_sees(p.seqs, p.mods, pc, j, j + 1);
+          bad = false;
+        }
+      }
+    }
     __syncthreads();
     // rows leave the CTA (or their parts do) as whole lines
     auto write_row = [&](int r, int c, float4 x, float M, float Ls) {
@@ -648,7 +660,7 @@ packed_f32_kernel(const __grid_constant__ pf32::Params p) {
       }
     }
   }
-  if (bad) atomicMax(p.d_status, (int)CHECK_PAGE_RANGE);
+  if (bad || lost) atomicMax(p.d_status, (int)CHECK_PAGE_RANGE);
   pdl_launch_dependents();
 }
 

@@ -318,6 +318,19 @@ __device__ __forceinline__ RowView row_view(const Seqs& q, const ScoreMods& m, c
   return v;
 }
 
+// Some token sees some slot of [j0, j1), by each token's own range: any_sees goes by the range from the lowest slot to the last
+// end, within which slots may be nobody's where tokens see nothing of their own.  Such a page is asked for like the others (what
+// it names is hidden from every row), but where its table entry is no page, that is nobody's concern: asked only then.
+__device__ __forceinline__ bool token_sees(const Seqs& q, const ScoreMods& m, const MaskedPiece& p, int j0, int j1) {
+  if (j0 < p.pre) return true;
+#pragma unroll 1
+  for (int i = 0; i < p.n_tok; ++i) {
+    const RowView v = row_view(q, m, p, i);
+    if (max(v.low, j0) < min(v.end, j1)) return true;
+  }
+  return false;
+}
+
 // The pieces of this CTA, 32 items (or units of a call in waves) at a time; run by one whole warp.
 struct PieceWindow {
   MaskedPiece mine;                            // of item (unit) next - 32 + lane

@@ -190,6 +190,12 @@ __device__ __forceinline__ bool wanted(const Params& p, const MaskedPiece& pc, i
   return j0 < pc.seen && any_sees(pc, any1_of(p.seqs, pc), j0, j1);
 }
 
+// Whether a bad table entry for these slots is to be recorded.
+__device__ __forceinline__ bool missed(const Params&, const Piece&, int, int) { return true; }
+__device__ __forceinline__ bool missed(const Params& p, const MaskedPiece& pc, int j0, int j1) {
+  return token_sees(p.seqs, p.mods, pc, j0, j1);
+}
+
 __device__ __forceinline__ int first_token(const Params& p, const Piece& pc) { return pc.first + pc.r * p.cfg.tokens; }
 __device__ __forceinline__ int first_token(const Params&, const MaskedPiece& pc) { return pc.tok0; }
 
@@ -256,7 +262,7 @@ __device__ __forceinline__ int tile_page(const Params& p, const P& pc, int tile,
     page = p.pages.table[(size_t)seq_of(pc) * p.pages.width + (j >> p.pages.shift)];
     if ((unsigned)page >= (unsigned)p.pages.n_pages) {
       page = 0;
-      *bad = true;
+      *bad = *bad || missed(p, pc, j, j + p.box);
     }
   }
   return page;

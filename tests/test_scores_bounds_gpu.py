@@ -1,6 +1,9 @@
 """Modified scores: the bounds of their parameters, rows beside one another, pages in the midst of a row tile."""
+import numpy as np
 import pytest
+import torch
 
+from paper_2508_11661_b200 import binding as B
 from scores_testlib import Mods
 from packed_testlib import PagedCase
 from test_scores_gpu import check_paged, check_prompt, paged, prompt, randn
@@ -24,3 +27,45 @@ def test_smallest_and_largest_cap(dtype, cap):
     c.Q[0] = 0
     O, lse = paged(c, mods, max_seq=1)
     check_paged(c, mods, O, lse)
+
+
+# tokens that see nothing in the midst of a row tile, or at its end
+GONE = {
+    # the first token sees what is before it, the last one itself: the pages of those between are nobody's
+    "midst": (64, 32, lambda n, c: [0] + [1 << 29] * (n - 2) + [c + n - 1]),
+    # only the first token sees anything: the pages behind its own are nobody's
+    "end": (40, 31, lambda n, c: [0] + [1 << 29] * (n - 1)),
+    "end of two": (2, 31, lambda n, c: [0, 1 << 29]),
+    # nobody sees anything but the prefix
+    "all": (40, 100, lambda n, c: [1 << 29] * n),
+}
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("where", list(GONE))
+@pytest.mark.parametrize("Hq,Hkv", [(2, 2), (8, 2), (16, 1)])
+def test_pages_that_no_token_sees_may_be_gone(dtype, where, Hq, Hkv):
+    """Whatever the tokens around them see, and however the call's row tiles lie."""
+    n, cached, starts = GONE[where]
+    page = 16
+    c = PagedCase([n, 3], [cached, 5], Hq, Hkv, 64, page, dtype, seed=210)
+    mods = Mods(softcap=9.0, doc=np.array(starts(n, cached) + [0, 1, 2]), prefix=[3, 0])
+    O, lse = paged(c, mods)
+    check_paged(c, mods, O, lse)
+    seen = mods.seen(0, 0, cached, n, cached + n).any(axis=0)
+    gone = [col for col in range(-(-(cached + n) // page)) if not seen[col * page:(col + 1) * page].any()]
+    assert gone
+    for i, col in enumerate(gone):
+        c.Kp[int(c.table[0, col])] = float("nan")
+        c.Vp[int(c.table[0, col])] = float("inf")
+        c.table[0, col] = [-1, 1 << 30, -(1 << 31)][i % 3]
+    for max_seq in (0, n):
+        O2, lse2 = paged(c, mods, max_seq=max_seq)        # (asks the device check word)
+        check_paged(c, mods, O2, lse2)
+    # one that a token does see is still recorded
+    col = int(np.flatnonzero(seen)[-1]) // page
+    c.table[0, col] = 1 << 30
+    p = B.Packed(Hq, Hkv, 64, c.offsets, c.T, 0, dtype)
+    h = B.Handle.for_scores(p)
+    B.samkv_paged_attn_scores(h, p, B.Pages(c.Kp, c.Vp, c.table), c.cache_len, c.Q, 0.0, True, mods.device(B, DEV), torch.empty_like(c.Q))
+    assert B.samkv_poll_status(h) == 7
