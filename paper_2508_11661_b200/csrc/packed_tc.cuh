@@ -318,13 +318,13 @@ __device__ __forceinline__ void mask_bits(float* v, unsigned bits) {
   for (int i = 0; i < kN; ++i)
     if (!(bits >> i & 1u)) v[i] = -INFINITY;
 }
-// x -> x mul - slope |pos - j|, slots j .. j + kN - 1.
+// x -> x mul - slope |pos - j|, slots j .. j + kN - 1: from the line slope (j + i - pos), with the same bits whatever the warp's
+// other rows see.
 template <int kN>
 __device__ __forceinline__ void bias_chunk(float* x, float mul, float slope, int pos, int j) {
-  const float d = (float)(pos - j);
+  const float d = (float)(pos - j), b = -slope * d;
   if (__all_sync(0xffffffffu, j + kN - 1 <= pos)) {                // all of them at or before the token: one line
     const f2 mul2_ = both(mul);
-    const float b = -slope * d;
 #pragma unroll
     for (int i = 0; i < kN; i += 2) {
       const float2 r = split2(fma2(join2(x[i], x[i + 1]), mul2_, join2(fmaf(slope, (float)i, b), fmaf(slope, (float)(i + 1), b))));
@@ -333,7 +333,10 @@ __device__ __forceinline__ void bias_chunk(float* x, float mul, float slope, int
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < kN; ++i) x[i] = fmaf(x[i], mul, -slope * fabsf(d - (float)i));
+    for (int i = 0; i < kN; ++i) {
+      const float line = fmaf(slope, (float)i, b);
+      x[i] = fmaf(x[i], mul, d >= (float)i ? line : -line);
+    }
   }
 }
 }  // namespace ptc

@@ -69,3 +69,22 @@ def test_pages_that_no_token_sees_may_be_gone(dtype, where, Hq, Hkv):
     h = B.Handle.for_scores(p)
     B.samkv_paged_attn_scores(h, p, B.Pages(c.Kp, c.Vp, c.table), c.cache_len, c.Q, 0.0, True, mods.device(B, DEV), torch.empty_like(c.Q))
     assert B.samkv_poll_status(h) == 7
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("softcap", [0.0, 3.0])
+def test_a_token_does_not_depend_on_those_beside_it(dtype, softcap):
+    """The token at position 63 as the last of a chunk and as the first of one: the same bits."""
+    Hq, d, n = 8, 64, 32
+    slopes = np.random.default_rng(11).uniform(0.01, 0.3, Hq)
+    results = []
+    pools = PagedCase([n], [63], Hq, Hq, d, 16, dtype, seed=220)
+    token = randn(1, Hq, d, dtype=dtype, seed=221, gain=3.0)
+    for cached, row in ((32, 31), (63, 0), (50, 13)):
+        c = PagedCase([n], [cached], Hq, Hq, d, 16, dtype, seed=222)
+        c.Kp, c.Vp, c.table, c.n_pages = pools.Kp, pools.Vp, pools.table, pools.n_pages
+        c.Q[row] = token[0]
+        O, lse = paged(c, Mods(softcap=softcap, slopes=slopes))
+        results.append((O[row], lse[row]))
+    for O, lse in results[1:]:
+        assert torch.equal(O, results[0][0]) and torch.equal(lse, results[0][1])
