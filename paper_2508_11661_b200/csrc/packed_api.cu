@@ -207,7 +207,7 @@ struct Array {
   long long bytes;
   bool output;
 };
-// Null where none is allowed, misaligned, or an output on another array's memory (n_free_out on n_free itself is allowed).
+// Refuses an output on another array's memory.  (n_free_out may be n_free itself: the caller leaves n_free out then.)
 samkv_status_t check_arrays(const Array* arrays, int n) {
   for (int i = 0; i < n; ++i)
     for (int j = 0; j < n; ++j) {

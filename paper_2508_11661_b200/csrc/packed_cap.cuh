@@ -8,7 +8,8 @@ namespace samkv {
 namespace tc {
 
 // x by `in` = scale / c to y, the result by `out` = c log2(e).  Up to |y| = 1, where heads spend their time, tanh(y) = y P(y^2),
-// P the polynomial of degree 5 with the least relative error on [0, 1]: 2^-20.4 with its evaluation in fp32.  It runs on the
+// P the polynomial of degree 5 with the least relative error on [0, 1]: 2^-20.6, with its scaled coefficients and its evaluation
+// in fp32 2^-20.3, with the roundings of `in`, `out` and y 2^-20.1 (the fp32 kernels' tanhf is good to 2^-23).  It runs on the
 // FMA pipe, two values an instruction; an exponential and a reciprocal would take twice the time of the softmax's own
 // exponentials on the special-function pipe, and serve larger scores, in the chunks that hold some.
 struct Cap {
