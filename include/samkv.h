@@ -521,8 +521,11 @@ samkv_status_t samkv_append_axes(samkv_handle_t h, const samkv_packed_t* packed,
  *   x = x - slopes[hq] * |p - j|                if slopes are given
  * and j is seen if j < prefix_len[s] (whatever p is), or if
  *   j <= p (j < cache_len[s] for samkv_paged_attn_scores without causal),  j >= doc_start[token],  and  p - j < window.
- * Documents that do not see one another, behind a shared instruction that all see (the prefix) and before a question that
- * sees all of them (doc_start 0), are one sequence; the initial tokens that a sliding window keeps are a prefix, too.
+ * The prefix's own tokens see one another in both directions (the prefix of a prefix language model).  In a causal model, put
+ * nothing into a prefix but slots that lie before the call's tokens, prefix_len[s] <= cache_len[s]: a shared instruction goes
+ * first, by a call without a prefix; documents that do not see one another (doc_start) and a question that sees all of them
+ * (doc_start 0) follow as one chunk of samkv_paged_attn_scores, with the instruction as their prefix.  So it is for the initial
+ * tokens that a sliding window keeps.
  * Slots a token does not see never reach it, infinities and NaN included; a token that sees none gets O = 0, lse = -inf. */
 typedef struct {
   float softcap;               /* 0: scores are not capped; else 2^-126 .. 1e30, and scale / softcap must be finite */

@@ -719,7 +719,8 @@ def samkv_append_axes(handle: Handle, packed: Packed, K, V, pages: Optional[Page
 
 # ------------------------------------------------------------------ attention with modified scores
 class Scores:
-    """A samkv_scores_t.  slopes fp32 [n_q_heads], prefix_len int32 [n_seq], doc_start int32 [n_tokens]: CUDA tensors, kept
+    """A samkv_scores_t (whose prefix is seen from before it, too: in causal models only slots that are in the cache already
+    belong there).  slopes fp32 [n_q_heads], prefix_len int32 [n_seq], doc_start int32 [n_tokens]: CUDA tensors, kept
     alive here; their values may change between calls."""
 
     def __init__(self, softcap: float = 0.0, window: int = 0, slopes=None, prefix_len=None, doc_start=None):

@@ -4,8 +4,8 @@ import pytest
 import torch
 
 from paper_2508_11661_b200 import binding as B
-from scores_testlib import Mods
-from packed_testlib import PagedCase
+from scores_testlib import Mods, attend64, check
+from packed_testlib import PagedCase, f64
 from test_scores_gpu import check_paged, check_prompt, paged, prompt, randn
 
 pytestmark = pytest.mark.gpu
@@ -88,3 +88,34 @@ def test_a_token_does_not_depend_on_those_beside_it(dtype, softcap):
         results.append((O[row], lse[row]))
     for O, lse in results[1:]:
         assert torch.equal(O, results[0][0]) and torch.equal(lse, results[0][1])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("window", [0, 70])
+def test_causal_instruction_documents_and_question(dtype, window):
+    """A causal model's instruction goes first, by a call without a prefix; documents that do not see one another and a question
+    that sees all follow as a chunk behind it, with the instruction as their prefix.  (With a window: initial tokens kept.)"""
+    pre, n, doc_len, tail, Hq, Hkv, d = 45, 400, 150, 30, 8, 2, 64
+    first = PagedCase([pre], [0], Hq, Hkv, d, 16, dtype, seed=230)
+    rest = PagedCase([n], [pre], Hq, Hkv, d, 16, dtype, seed=231)
+    first.Kp, first.Vp, first.table, first.table_cpu, first.n_pages = rest.Kp, rest.Vp, rest.table, rest.table_cpu, rest.n_pages
+    t = np.arange(n)
+    doc = np.zeros(n, dtype=np.int64) if window else np.where(t < n - tail, pre + t // doc_len * doc_len, 0)
+    mods = Mods(window=window, prefix=[pre], doc=doc)
+    O1, lse1 = paged(first, Mods(window=window))
+    O2, lse2 = paged(rest, mods)
+    # the model: every token of the one sequence sees what is at or before it, of the instruction or of its own document
+    p, j = np.arange(pre + n)[:, None], np.arange(pre + n)[None, :]
+    start = np.concatenate([np.zeros(pre, dtype=np.int64), doc])[:, None]
+    ok = (j <= p) & ((j < pre) | ((j >= start) & ((p - j < window) if window else True)))
+    q = np.concatenate([f64(first.Q), f64(rest.Q)])
+    ref = attend64(q, rest.slots(rest.Kp, 0, pre + n), rest.slots(rest.Vp, 0, pre + n), ok, np.arange(pre + n), mods, d ** -0.5)
+    check(np.concatenate([f64(O1), f64(O2)]), np.concatenate([f64(lse1), f64(lse2)]), ref, dtype, pre + n)
+    # in one call the instruction's tokens see one another in both directions
+    both = PagedCase([pre + n], [0], Hq, Hkv, d, 16, dtype, seed=231)
+    both.Kp, both.Vp, both.table, both.n_pages = rest.Kp, rest.Vp, rest.table, rest.n_pages
+    both.Q = torch.cat([first.Q, rest.Q])
+    O, lse = paged(both, Mods(window=window, prefix=[pre], doc=np.concatenate([np.zeros(pre, dtype=np.int64), doc])))
+    ok[:pre, :pre] = True
+    ref = attend64(q, rest.slots(rest.Kp, 0, pre + n), rest.slots(rest.Vp, 0, pre + n), ok, np.arange(pre + n), mods, d ** -0.5)
+    check(f64(O), f64(lse), ref, dtype, pre + n)
