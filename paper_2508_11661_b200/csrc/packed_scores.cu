@@ -17,7 +17,7 @@ cudaError_t launch_packed_f32_scores(const samkv_packed_t& d, const Seqs& seqs, 
                                      const ScoreMods& mods, const Rows& O, float* lse, int rows, const samkv_ctx_impl& h,
                                      cudaStream_t stream);
 
-// The rules of the plain calls.
+// The rules of the plain calls, whose borders were measured on plain calls (masks change how much work a row tile has).
 cudaError_t launch_scores_attn(const samkv_packed_t& d, const Seqs& seqs, const KvSource& kv, const Rows& Q, float scale,
                                const ScoreMods& mods, const Rows& O, float* lse, const samkv_ctx_impl& h, cudaStream_t stream) {
   if (scale <= 0.f) scale = 1.0f / sqrtf((float)d.head_dim);

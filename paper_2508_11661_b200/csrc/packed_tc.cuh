@@ -16,7 +16,7 @@
 // their probabilities before they hand them over.  A reference moves by whole steps of log2, so that rescaled
 // probabilities are not rounded again.  Which reference a row's tile starts from is fixed (the first tile's, or the one
 // its group ended the tile three before with), and each row decides for itself, so that results repeat bit for bit and
-// depend on no other row.
+// depend on no other row of the tile.
 // P(T) overlays the first half of S(T), so tensor memory holds three score buffers and O: 512 columns.
 // The group with a piece's last tile writes the result while the others are at the next piece's tiles.
 //
